@@ -355,7 +355,7 @@ def run(state):
             a = binding.accept_tree(s["tree"], s["target"])
             cache.commit(chunk, a.path, a.n_accepted)
             out.update(path=a.path, count=a.n_accepted, next=a.next_token)
-        out["rows"] = [cache.read(chunk, layer=n) for n in range(c["layers"])]
+        out["rows"] = [cache.read(chunk, len(k), layer=n) for n, k in enumerate(s["k"])]
         return out
     if c["family"] == "attend":
         return _plain_attend(c, s)

@@ -65,7 +65,8 @@ extern "C" {
 
 #define DT_ABI_VERSION 3
 
-typedef enum { DT_F32 = 0, DT_BF16 = 1 } dt_dtype;
+/* DT_F8: 8-bit floats (OCP e4m3); what a dt_cache can hold, no other tensor. */
+typedef enum { DT_F32 = 0, DT_BF16 = 1, DT_F8 = 2 } dt_dtype;
 
 typedef enum {
   DT_OK = 0,
@@ -366,6 +367,133 @@ dt_status dt_head_workspace_size(const dt_plan *plan, int batch, const dt_domino
 dt_status dt_build_tree_head(dt_plan *plan, const void *marginal_logits, int batch, const void *H,
                              const dt_domino_head *head, const float *h0, float T,
                              void *workspace, size_t ws_bytes, dt_tree *out, void *stream);
+
+/* ---- verification: the paged cache, attention over it, and the commit of a tree ----
+ *
+ * After a tree is built its verifier (section 3.5) writes the keys and values of
+ * the last committed token (the root) and of the tree's nodes into its cache, lets
+ * them attend to the cached context under the ancestor mask, takes the longest
+ * path of nodes that match the target's own tokens, and keeps that path's rows.
+ * The calls below do this, and the same for prompts in chunks and for plain
+ * decoding (chunks of one token).  All of them are stream-ordered, wait for
+ * nothing, allocate nothing and may be captured into a HIP graph.
+ *
+ * A cache is caller-owned device memory of dt_cache_size bytes.  Its contents
+ * are laid out in the operand order of the matrix instructions, so rows go in and
+ * out through dt_cache_append and dt_cache_read only; a page of a layer is one
+ * contiguous piece of dt_cache_size / (layers * pages) bytes, which may be copied
+ * as a whole (layer-major, pages in order).  Nothing has to be initialised.
+ *
+ * DT_F8 caches hold, for every token and kv head and for keys and values apart,
+ * D codes c = e4m3(x 2^-e) rounded to nearest even and one exponent e, the least
+ * integer with max|x| <= 448 2^e over the finite x (kept in [-120, 120]).  NaN and
+ * infinities are held as NaN.  A power of two scales exactly: the codes do not
+ * depend on how the division is rounded. */
+typedef struct {
+  void *data;    /* 256-byte aligned */
+  int layers;    /* >= 1 */
+  int pages;     /* >= 1, in each layer */
+  int page_size; /* tokens: 32, 64, 128 or 256 */
+  int kv_heads;  /* >= 1 */
+  int head_dim;  /* D: 64, 96, 128 or 256 */
+  int dtype;     /* DT_F32, DT_BF16 or DT_F8; the data type of k, v, q and out is DT_F32
+                    for DT_F32 and DT_BF16 for the others */
+} dt_cache;
+
+/* The new tokens of a batch of sequences and where they lie in a cache.  Sequence
+ * b has lens[b] tokens in the cache (the new ones included); the last
+ * n_b = starts[b + 1] - starts[b] of them are its chunk, rows starts[b] ..
+ * starts[b + 1] - 1 of the call's tensors.  Its token p (0-based) lies in slot
+ * p % page_size of page table[b * table_width + p / page_size].
+ * starts, lens and table are read by the kernels, at the time they run (a replay
+ * of a captured call takes what they hold then); 0 <= starts[b] <= starts[b + 1]
+ * <= rows, n_b <= max_chunk, n_b <= lens[b] <= max_len and 0 <= page < pages must
+ * hold.  Where they do not, no access leaves the tensors: a token whose page is out of
+ * range is not written, read as zeros and not seen. */
+typedef struct {
+  int batch;       /* 1 .. 65535 */
+  int rows;        /* rows of the call's tensors, >= 1 */
+  int max_chunk;   /* bound of n_b, 1 <= max_chunk <= rows */
+  int max_len;     /* bound of lens[b], 1 <= max_len <= table_width * page_size */
+  int table_width; /* pages of a table row; table_width * page_size < 2^30 */
+  const int32_t *starts; /* [batch + 1] */
+  const int32_t *lens;   /* [batch] */
+  const int32_t *table;  /* [batch, table_width] */
+} dt_chunk;
+
+/* A tensor of rows [rows, heads, D] at any strides (in elements, >= 0), D contiguous;
+ * element-aligned (16-byte aligned addresses and strides are read and written faster). */
+typedef struct {
+  void *data;
+  int64_t row_stride, head_stride;
+} dt_rows;
+
+/* Bytes of a cache (data is not looked at). */
+dt_status dt_cache_size(const dt_cache *cache, size_t *bytes);
+
+/* Write the chunk's keys and values ([rows, kv_heads, D], the data type) into a layer. */
+dt_status dt_cache_append(const dt_cache *cache, int layer, const dt_chunk *chunk, const dt_rows *k,
+                          const dt_rows *v, void *stream);
+
+/* The chunk's keys and values back out of a layer, as the values they stand for. */
+dt_status dt_cache_read(const dt_cache *cache, int layer, const dt_chunk *chunk, const dt_rows *k,
+                        const dt_rows *v, void *stream);
+
+/* What a query sees.  Row i of a chunk (token base + i, base = lens[b] - n_b) sees
+ * the keys j <= base + i; with a window only those of them with j > base + i - window
+ * or j < sinks.
+ * With tree_nodes = N > 0 the last N rows of every chunk are a tree's nodes (the
+ * rows before them, the root among them, see what is said above): node m sees node j
+ * where mask[b][m][j] is not 0, and of the keys before the nodes all, or with a window
+ * those that a token at position r + depth[b][m] sees, r the position of the last row
+ * before the nodes.  A row of a padding node (mask row 0) sees the keys before the
+ * nodes only; every chunk must hold at least N rows. */
+typedef struct {
+  float scale;         /* of q . k, finite */
+  int window;          /* 0: no window */
+  int sinks;           /* >= 0; looked at with a window only */
+  int tree_nodes;      /* 0: no tree; at most 256 */
+  const uint8_t *mask; /* [batch, N, N], dt_tree.mask; with a tree */
+  const int32_t *depth; /* [batch, N], dt_tree.depth; with a tree and a window (else not looked at) */
+} dt_attend_options;
+
+/* Workspace (bytes, may be 0) of dt_cache_attend for this shape (pointers are not
+ * looked at). */
+dt_status dt_attend_workspace_size(const dt_cache *cache, const dt_chunk *chunk, int heads,
+                                   const dt_attend_options *opts, size_t *bytes);
+
+/* Attention of the chunk's queries q [rows, heads, D] over a layer of the cache:
+ *   out[i, h] = sum_j p_j v_j,  p = softmax over the visible j of scale q[i, h] . k_j,
+ * head h reading kv head h / (heads / kv_heads).  heads is a multiple of kv_heads, at most
+ * 1024 heads per kv head.  The chunk's own keys and values have to be in the cache.
+ * A row that sees nothing gives zeros; NaN and infinities of keys and values that a
+ * row does not see leave it untouched, those it sees make its result (or those
+ * components of it) non-finite.  Scores, softmax and sums are fp32; with bf16
+ * data the probabilities are rounded to bf16 before their product with the
+ * values.  q and out may have different strides and must not overlap.
+ *   workspace: >= dt_attend_workspace_size bytes, 256-byte aligned (NULL where 0);
+ *   not to be shared by calls that can overlap. */
+dt_status dt_cache_attend(const dt_cache *cache, int layer, const dt_chunk *chunk, int heads,
+                          const dt_rows *q, const dt_rows *out, const dt_attend_options *opts,
+                          void *workspace, size_t ws_bytes, void *stream);
+
+/* The longest path of a tree that the target agrees with: from the root, the child
+ * whose token is the target's token at the present node, as long as there is one.
+ *   tree: tokens, parents and n_nodes of dt_tree ([batch, B]; the rest is not looked at);
+ *   target: [batch, B + 1] the target's token at the root (column 0) and at node i
+ *           (column i + 1), its argmax or a sample;
+ *   path: [batch, B] the accepted nodes in order, then -1;
+ *   n_accepted: [batch]; next_token: [batch] the target's token at the last of them.
+ * 1 <= B <= 256. */
+dt_status dt_tree_accept(const dt_tree *tree, int batch, int B, const int32_t *target, int32_t *path,
+                         int32_t *n_accepted, int32_t *next_token, void *stream);
+
+/* Move the rows of the accepted nodes together, in every layer: with N nodes as the last
+ * rows of each chunk, node path[b][i] to the place of node i for i < n_accepted[b].
+ * Rows past those keep what they hold.  path ([batch, N]) rises along each row, as
+ * dt_tree_accept writes it; entries below their index or out of range are left out. */
+dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int nodes, const int32_t *path,
+                          const int32_t *n_accepted, void *stream);
 
 #ifdef __cplusplus
 }

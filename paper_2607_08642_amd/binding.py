@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(PKG, "libdominotree.so")
 
 DT_F32 = 0
 DT_BF16 = 1
+DT_F8 = 2
 DT_NORM_TAIL = 0
 DT_NORM_SLICE = 1
 DT_SCORER_COND = 0
@@ -37,7 +38,8 @@ EXPORTS = ("dt_abi_version", "dt_status_string", "dt_last_error", "dt_plan_creat
            "dt_build_tree_head", "dt_build_tree_noalloc",
            "dt_plan_expand_stats", "dt_plan_set_adaptive_budget", "dt_model_create",
            "dt_model_destroy", "dt_plan_create_from_model", "dt_once_workspace_size",
-           "dt_build_tree_once")
+           "dt_build_tree_once", "dt_cache_size", "dt_cache_append", "dt_cache_read",
+           "dt_attend_workspace_size", "dt_cache_attend", "dt_tree_accept", "dt_cache_commit")
 STAGES = ("scan", "expand")
 
 
@@ -72,6 +74,27 @@ class dt_tree(ctypes.Structure):
                 ("depth", ctypes.c_void_p), ("position_ids", ctypes.c_void_p),
                 ("mask", ctypes.c_void_p), ("scores", ctypes.c_void_p),
                 ("n_nodes", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class dt_cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("layers", ctypes.c_int), ("pages", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("dtype", ctypes.c_int)]
+
+
+class dt_chunk(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("rows", ctypes.c_int), ("max_chunk", ctypes.c_int),
+                ("max_len", ctypes.c_int), ("table_width", ctypes.c_int), ("starts", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+
+
+class dt_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class dt_attend_options(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("window", ctypes.c_int), ("sinks", ctypes.c_int),
+                ("tree_nodes", ctypes.c_int), ("mask", ctypes.c_void_p), ("depth", ctypes.c_void_p)]
 
 
 _lib = None
@@ -132,6 +155,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.dt_build_tree_once.restype = ci
     lib.dt_build_tree_once.argtypes = [vp, ci, ci, ctypes.POINTER(dt_gru), ctypes.POINTER(dt_head)] + [ci] * 5 + \
         [vp, ci, vp, cf, ctypes.POINTER(dt_options), vp, sz, ctypes.POINTER(dt_tree), vp]
+    pc, pk, pr, po = (ctypes.POINTER(t) for t in (dt_cache, dt_chunk, dt_rows, dt_attend_options))
+    lib.dt_cache_size.restype = ci
+    lib.dt_cache_size.argtypes = [pc, ctypes.POINTER(sz)]
+    for f in (lib.dt_cache_append, lib.dt_cache_read):
+        f.restype = ci
+        f.argtypes = [pc, ci, pk, pr, pr, vp]
+    lib.dt_attend_workspace_size.restype = ci
+    lib.dt_attend_workspace_size.argtypes = [pc, pk, ci, po, ctypes.POINTER(sz)]
+    lib.dt_cache_attend.restype = ci
+    lib.dt_cache_attend.argtypes = [pc, ci, pk, ci, pr, pr, po, vp, sz, vp]
+    lib.dt_tree_accept.restype = ci
+    lib.dt_tree_accept.argtypes = [ctypes.POINTER(dt_tree), ci, ci, vp, vp, vp, vp, vp]
+    lib.dt_cache_commit.restype = ci
+    lib.dt_cache_commit.argtypes = [pc, pk, ci, vp, vp, vp]
     if lib.dt_abi_version() != ABI_VERSION:
         raise RuntimeError(f"ABI mismatch: library {lib.dt_abi_version()} vs binding {ABI_VERSION}")
     _lib = lib
@@ -448,3 +485,207 @@ def scan_topm(logits, M: int, T: float, stream=None):
                             _ptr(ids), _ptr(vals), _ptr(tail), _ptr(flags), _ptr(ws), n.value,
                             _stream(stream)))
     return ids, vals, tail, flags
+
+
+# ---- verification: the paged cache, attention over it, the commit of a tree ----------------
+
+def _want(t, name, shape, dtype):
+    """A contiguous device tensor of this shape and dtype, as the C ABI takes it."""
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name}: want a contiguous {dtype} device tensor of shape {shape}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+class Chunk:
+    """dt_chunk: the new tokens of a batch of sequences and where they lie in a cache.
+
+    starts [batch + 1], lens [batch] and table [batch, width]: int32 device tensors, read when the
+    kernels run, so a program may go on changing their contents in place; max_chunk and max_len
+    bound the chunks and the lengths they will hold.
+    """
+
+    def __init__(self, starts, lens, table, max_chunk: int, max_len: int):
+        import torch
+        batch, width = table.shape
+        self.starts = _want(starts, "starts", (batch + 1,), torch.int32)
+        self.lens = _want(lens, "lens", (batch,), torch.int32)
+        self.table = _want(table, "table", (batch, width), torch.int32)
+        self.batch, self.max_chunk, self.max_len = batch, max_chunk, max_len
+        self._c = dt_chunk(batch, 0, max_chunk, max_len, width, starts.data_ptr(), lens.data_ptr(), table.data_ptr())
+
+    def as_c(self, rows: int) -> dt_chunk:
+        self._c.rows = rows
+        return self._c
+
+
+@dataclasses.dataclass
+class Accepted:
+    """dt_tree_accept's results (device tensors)."""
+    path: "torch.Tensor"        # [b, B] int32 accepted nodes, then -1
+    n_accepted: "torch.Tensor"  # [b] int32
+    next_token: "torch.Tensor"  # [b] int32 the target's token after the path
+
+
+class Cache:
+    """dt_cache: keys and values of `layers` layers in pages, in the kernels' own order.
+
+    dtype: torch.float32, torch.bfloat16 or torch.float8_e4m3fn (bf16 data with one power-of-two
+    scale for each token and head).  Calls run on torch's current stream unless one is given;
+    outputs made here are allocated on the current stream and recorded on the one that is given.
+    """
+
+    def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype, layers: int = 1,
+                 device="cuda"):
+        import torch
+        codes = {torch.float32: DT_F32, torch.bfloat16: DT_BF16, torch.float8_e4m3fn: DT_F8}
+        if dtype not in codes:
+            raise TypeError(f"unsupported dtype {dtype}")
+        self._lib = load()
+        self.pages, self.page_size, self.kv_heads, self.head_dim, self.layers = (pages, page_size, kv_heads,
+                                                                                head_dim, layers)
+        self.dtype = dtype
+        self.data_dtype = torch.float32 if dtype == torch.float32 else torch.bfloat16
+        c = dt_cache(None, layers, pages, page_size, kv_heads, head_dim, codes[dtype])
+        n = ctypes.c_size_t()
+        _check(self._lib.dt_cache_size(ctypes.byref(c), ctypes.byref(n)))
+        self.storage = torch.empty(n.value, dtype=torch.uint8, device=device)
+        c.data = self.storage.data_ptr()
+        self._c = c
+        self._sizes = {}   # workspace bytes of a shape
+        self._ws = {}      # a workspace of each stream
+
+    def _rows(self, t, name: str, heads: Optional[int] = None) -> dt_rows:
+        if t.dtype != self.data_dtype or t.dim() != 3 or t.shape[2] != self.head_dim or not t.is_cuda or \
+                (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{name}: want a {self.data_dtype} device tensor [rows, {heads or 'heads'}, "
+                             f"{self.head_dim}], got {t.dtype} {tuple(t.shape)} on {t.device}")
+        s = t.stride()
+        if s[2] != 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous (stride {s[2]})")
+        return dt_rows(t.data_ptr(), s[0], s[1])
+
+    def append(self, chunk: Chunk, k, v, layer: int = 0, stream=None) -> None:
+        """dt_cache_append: the chunk's keys and values [rows, kv_heads, head_dim] into a layer."""
+        kr, vr = self._rows(k, "k", self.kv_heads), self._rows(v, "v", self.kv_heads)
+        if k.shape[0] != v.shape[0]:
+            raise ValueError(f"k and v have {k.shape[0]} and {v.shape[0]} rows")
+        st = self._lib.dt_cache_append(ctypes.byref(self._c), layer, ctypes.byref(chunk.as_c(k.shape[0])),
+                                       ctypes.byref(kr), ctypes.byref(vr), _stream(stream))
+        if st != 0:
+            _check(st)
+
+    def read(self, chunk: Chunk, rows: Optional[int] = None, layer: int = 0, out=None, stream=None):
+        """dt_cache_read: the chunk's keys and values as (k, v) [rows, kv_heads, head_dim].
+
+        rows: rows of the tensors made (starts' last); out = (k, v) takes given ones instead.
+        Rows that belong to no chunk are left as they are.
+        """
+        import torch
+        if out is None:
+            if rows is None:
+                raise ValueError("read needs the number of rows, or out")
+            out = tuple(torch.empty(rows, self.kv_heads, self.head_dim, dtype=self.data_dtype,
+                                    device=self.storage.device) for _ in range(2))
+            if stream is not None:
+                for t in out:
+                    t.record_stream(stream)
+        k, v = out
+        kr, vr = self._rows(k, "k", self.kv_heads), self._rows(v, "v", self.kv_heads)
+        if k.shape[0] != v.shape[0]:
+            raise ValueError(f"k and v have {k.shape[0]} and {v.shape[0]} rows")
+        st = self._lib.dt_cache_read(ctypes.byref(self._c), layer, ctypes.byref(chunk.as_c(k.shape[0])),
+                                     ctypes.byref(kr), ctypes.byref(vr), _stream(stream))
+        if st != 0:
+            _check(st)
+        return out
+
+    def workspace_size(self, chunk: Chunk, rows: int, heads: int, opts: dt_attend_options) -> int:
+        c = chunk.as_c(rows)
+        key = (c.batch, rows, c.max_chunk, c.max_len, c.table_width, heads, opts.window, opts.sinks, opts.tree_nodes)
+        n = self._sizes.get(key)
+        if n is None:
+            b = ctypes.c_size_t()
+            _check(self._lib.dt_attend_workspace_size(ctypes.byref(self._c), ctypes.byref(c), heads,
+                                                      ctypes.byref(opts), ctypes.byref(b)))
+            n = self._sizes[key] = b.value
+        return n
+
+    def _workspace(self, n: int, stream):
+        """The stream's workspace, grown to n bytes (calls on one stream follow one another)."""
+        import torch
+        ws = self._ws.get(stream)
+        if ws is None or ws.numel() < n:
+            ws = self._ws[stream] = torch.empty(n, dtype=torch.uint8, device=self.storage.device)
+        return ws
+
+    def attend(self, chunk: Chunk, q, scale: Optional[float] = None, layer: int = 0, window: int = 0,
+               sinks: int = 0, mask=None, depth=None, out=None, workspace=None, stream=None):
+        """dt_cache_attend: attention of the chunk's queries q [rows, heads, head_dim] over a layer.
+
+        scale: default head_dim ** -0.5; window (0: none) with `sinks` first tokens that stay visible;
+        mask [batch, N, N] uint8 (Tree.mask): the last N rows of every chunk are a tree's nodes, depth
+        [batch, N] (Tree.depth) their depths, needed with a window.
+        """
+        import torch
+        rows, heads = q.shape[0], q.shape[1]
+        qr = self._rows(q, "q")
+        if out is None:
+            out = torch.empty(rows, heads, self.head_dim, dtype=q.dtype, device=q.device)
+            if stream is not None:
+                out.record_stream(stream)
+        elif out.shape[0] != rows:
+            raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
+        outr = self._rows(out, "out", heads)
+        nodes = 0
+        if mask is not None:
+            nodes = mask.shape[-1]
+            _want(mask, "mask", (chunk.batch, nodes, nodes), torch.uint8)
+            if depth is not None:
+                _want(depth, "depth", (chunk.batch, nodes), torch.int32)
+        opts = dt_attend_options(self.head_dim ** -0.5 if scale is None else scale, window, sinks, nodes,
+                                 _ptr(mask), _ptr(depth))
+        s = _stream(stream)
+        if workspace is None:
+            n = self.workspace_size(chunk, rows, heads, opts)
+            workspace = self._workspace(n, s) if n else None
+        st = self._lib.dt_cache_attend(ctypes.byref(self._c), layer, ctypes.byref(chunk.as_c(rows)), heads,
+                                       ctypes.byref(qr), ctypes.byref(outr), ctypes.byref(opts), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), s)
+        if st != 0:
+            _check(st)
+        return out
+
+    def commit(self, chunk: Chunk, path, n_accepted, stream=None) -> None:
+        """dt_cache_commit: the rows of the accepted nodes (Accepted.path, .n_accepted) moved together, in
+        every layer; the nodes are the last path.shape[1] rows of each chunk."""
+        import torch
+        n = path.shape[1]
+        every = min(chunk.batch * chunk.max_chunk, 2 ** 31 - 1)   # (no tensor of rows here: starts' bound)
+        _want(path, "path", (chunk.batch, n), torch.int32)
+        _want(n_accepted, "n_accepted", (chunk.batch,), torch.int32)
+        st = self._lib.dt_cache_commit(ctypes.byref(self._c), ctypes.byref(chunk.as_c(every)), n,
+                                       path.data_ptr(), n_accepted.data_ptr(), _stream(stream))
+        if st != 0:
+            _check(st)
+
+
+def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None) -> Accepted:
+    """dt_tree_accept: the longest path of each tree that the target agrees with.
+
+    target [b, B + 1] int32: the target's token at the root and at every node.
+    """
+    import torch
+    b, B = tree.tokens.shape
+    _want(target, "target", (b, B + 1), torch.int32)
+    if out is None:
+        i32 = dict(dtype=torch.int32, device=target.device)
+        out = Accepted(torch.empty(b, B, **i32), torch.empty(b, **i32), torch.empty(b, **i32))
+        if stream is not None:
+            for t in (out.path, out.n_accepted, out.next_token):
+                t.record_stream(stream)
+    st = load().dt_tree_accept(ctypes.byref(tree.as_c()), b, B, target.data_ptr(), out.path.data_ptr(),
+                               out.n_accepted.data_ptr(), out.next_token.data_ptr(), _stream(stream))
+    if st != 0:
+        _check(st)
+    return out

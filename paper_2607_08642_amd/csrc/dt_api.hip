@@ -11,11 +11,10 @@
 #include "dt_internal.h"
 #include "dt_select.h"
 
-namespace {
+static thread_local std::string g_last_error;
 
-thread_local std::string g_last_error;
+namespace dt {
 
-dt_status fail(dt_status s, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 dt_status fail(dt_status s, const char *fmt, ...) {
   char buf[512];
   va_list ap;
@@ -29,6 +28,13 @@ dt_status fail(dt_status s, const char *fmt, ...) {
 dt_status hip_fail(hipError_t e, const char *what) {
   return fail(DT_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace dt
+
+using dt::fail;
+using dt::hip_fail;
+
+namespace {
 
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 

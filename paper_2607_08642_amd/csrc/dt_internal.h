@@ -43,6 +43,10 @@ constexpr int kProfSlots = 1024;     // profiled calls kept for stage averages
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// a call's failure: the thread's dt_last_error text; returns the status (dt_api.hip)
+dt_status fail(dt_status s, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+dt_status hip_fail(hipError_t e, const char *what);
+
 // ---------------------------------------------------------------------------
 // order-preserving 64-bit keys: (value desc, index asc) <=> key desc.
 // high word: IEEE bits mapped to an unsigned order (-0 folded onto +0);

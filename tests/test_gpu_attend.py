@@ -1,0 +1,314 @@
+"""Attention over the paged cache against the plain 64-bit form on the values that the cache holds.
+
+Tolerance, element by element, with A = sum p |v| (the size of the sum that gives it):
+- a score's error is at most (D + 8) 2^-24 scale sum |q||k| (fp32 products and sums, and the rounding of
+  scale log2 e and of the exponent's argument), so a probability's relative error at most twice that;
+- the exponential, the sums over n keys and the division: (n + 16) 2^-23;
+- bf16 (8 significant bits, so a rounding errs by up to 2^-8): each probability rounded, and the result.
+"""
+import numpy as np
+import pytest
+import torch
+
+import verify_ref as ref
+from paper_2607_08642_amd import binding
+from test_gpu_cache import Setup, held, i32, random_tree, same
+
+pytestmark = pytest.mark.gpu
+
+
+def allowed(q, k, v, scale, ok, data_dtype):
+    """[n, H, D] of the tolerance above for one sequence."""
+    n, H, D = q.shape
+    A = ref.attend(q, k, v.abs(), scale, ok)
+    g = H // k.shape[1]
+    qk = torch.einsum("nhd,jhd->nhj", q.double().abs(), k.double().abs().repeat_interleave(g, 1))
+    qk = torch.where(torch.from_numpy(ok)[:, None], qk, 0.0).amax(-1) if ok.shape[1] else torch.zeros(n, H)
+    rel = 2 * (D + 8) * 2.0 ** -24 * abs(scale) * qk + (ok.shape[1] + 16) * 2.0 ** -23
+    if data_dtype == torch.bfloat16:
+        rel = rel + 2.0 ** -7
+    return A * rel[..., None]
+
+
+class Attend(Setup):
+    def __init__(self, dtype, sizes, heads, page=32, kv=2, D=64, seed=0, sharp=1.5):
+        super().__init__(dtype, sizes, page, kv, D, seed=seed)
+        self.heads = heads
+        every = self.make([(n, n) for n, _ in sizes])
+        total = sum(n for n, _ in sizes)
+        self.k, self.v = self.randn(total), self.randn(total)
+        self.cache.append(every, self.k.cuda(), self.v.cuda())
+        self.q = (self.randn(max(self.rows, 1), heads).float() * sharp).to(self.cache.data_dtype)
+
+    def check(self, got, scale=None, window=0, sinks=0, masks=None, depths=None):
+        scale = self.D ** -0.5 if scale is None else scale
+        at = 0
+        k, v = held(self, self.k), held(self, self.v)
+        worst = 0.0
+        for b, (n, m) in enumerate(self.sizes):
+            r0 = self.starts[b]
+            ok = ref.visible(m, n - m, n, window, sinks, None if masks is None else masks[b],
+                             None if depths is None else depths[b])
+            q, kk, vv = self.q[r0:r0 + m], k[at:at + n], v[at:at + n]
+            want = ref.attend(q, kk, vv, scale, ok)
+            tol = allowed(q, kk, vv, scale, ok, self.cache.data_dtype)
+            err = (got[r0:r0 + m].double().cpu() - want).abs()
+            assert bool((err <= tol + 1e-30).all()), f"sequence {b}: {float((err / (tol + 1e-30)).max()):.3g} x allowed"
+            worst = max(worst, float((err / (tol + 1e-30)).max()) if m else 0.0)
+            at += n
+        return worst
+
+    def run(self, **kw):
+        return self.cache.attend(self.chunk, self.q.cuda(), **kw)
+
+
+TYPES = ["f32", "bf16", "f8"]
+# sizes (length, chunk), heads, kv heads
+SHAPES = {
+    "one": ([(1, 1)], 2, 1),
+    "tokens": ([(1, 1), (31, 1), (32, 1), (33, 1), (257, 1), (700, 1)], 8, 2),
+    "tokens_group1": ([(65, 1), (130, 1)], 3, 3),
+    "short_chunks": ([(40, 7), (9, 9), (64, 3), (100, 0)], 10, 2),
+    "chunks": ([(300, 37), (129, 129), (70, 1), (513, 64)], 8, 2),
+    "wide_group": ([(90, 5), (33, 33)], 24, 1),
+}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,page", [(64, 32), (96, 64), (128, 32), (256, 128)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_causal(dtype, D, page, shape):
+    sizes, heads, kv = SHAPES[shape]
+    print(f"[attend] {dtype} D={D} page={page} {shape}", flush=True)
+    a = Attend(dtype, sizes, heads, page, kv, D, seed=len(shape) + D)
+    a.check(a.run())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (32, 0), (33, 1), (50, 32), (64, 40), (5000, 4), (2 ** 31 - 1, 2 ** 31 - 1)])
+@pytest.mark.parametrize("shape", ["tokens", "chunks"])
+def test_window(dtype, window, sinks, shape):
+    sizes, heads, kv = SHAPES[shape]
+    print(f"[attend] window {dtype} {window}/{sinks} {shape}", flush=True)
+    a = Attend(dtype, sizes, heads, 32, kv, 64, seed=window % 1000)
+    a.check(a.run(window=window, sinks=sinks), window=window, sinks=sinks)
+
+
+def trees(sizes, N, seed):
+    """A tree for each sequence (every third one of fewer nodes, padded): masks and depths."""
+    import random
+    rng = random.Random(seed)
+    masks, depths = [], []
+    for b in range(len(sizes)):
+        n = N if b % 3 != 1 else N // 2
+        _, par, dep = random_tree(rng, n, N)
+        m = np.zeros((N, N), np.uint8)
+        for i in range(n):
+            if par[i] >= 0:
+                m[i] = m[par[i]]
+            m[i, i] = 1
+        masks.append(m)
+        depths.append(dep)
+    return masks, depths
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,lead", [(1, 1), (16, 1), (16, 0), (31, 2), (64, 1), (150, 40)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 5)])
+def test_trees(dtype, N, lead, window, sinks):
+    sizes = [(n + N + lead, N + lead) for n in (0, 1, 31, 200, 64)]
+    print(f"[attend] tree {dtype} N={N} lead={lead} window={window}", flush=True)
+    a = Attend(dtype, sizes, 8, 64, 2, 64, seed=N)
+    masks, depths = trees(sizes, N, N)
+    got = a.run(mask=torch.from_numpy(np.stack(masks)).cuda(), depth=i32(depths), window=window, sinks=sinks)
+    a.check(got, window=window, sinks=sinks, masks=masks, depths=depths)
+    if lead == 0 and N == 16:   # no context and a padding row: nothing seen, zeros
+        a2 = Attend(dtype, [(N, N)], 8, 64, 2, 64, seed=1)
+        masks[0][5] = 0
+        got = a2.run(mask=torch.from_numpy(masks[0][None]).cuda())
+        assert not got[5].any()
+        a2.check(got, masks=masks[:1], depths=depths[:1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_and_split(dtype):
+    """One sequence far beyond a split, alone and beside short ones."""
+    for sizes in ([(9001, 1)], [(9001, 5), (3, 1), (640, 2)]):
+        print(f"[attend] long {dtype} {sizes}", flush=True)
+        a = Attend(dtype, sizes, 4, 128, 1, 128, seed=3)
+        a.check(a.run())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1.0])
+def test_scale(dtype, scale):
+    a = Attend(dtype, [(50, 4), (200, 1)], 4, 32, 2, 64, seed=9)
+    a.check(a.run(scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_scores(dtype):
+    """Scores of hundreds: nothing overflows, the softmax picks."""
+    a = Attend(dtype, [(300, 3), (65, 40)], 4, 32, 2, 64, seed=11, sharp=60.0)
+    got = a.run()
+    assert bool(torch.isfinite(got).all())
+    a.check(got)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [16, 64])
+def test_unseen_nonfinite_values_stay_out(dtype, N):
+    """NaN and infinities in nodes that a row does not see, in later tokens and before a window change
+    nothing; rows that see them are not finite."""
+    sizes = [(N + 41, N + 1), (N + 200, N + 1)]
+    masks, depths = trees(sizes, N, 4)
+    mask = torch.from_numpy(np.stack(masks)).cuda()
+    a = Attend(dtype, sizes, 8, 32, 2, 64, seed=2)
+    clean = a.run(mask=mask)
+    bad = 3       # node 3 of each tree
+    k, v = a.k.clone(), a.v.clone()
+    for b, end in enumerate(np.cumsum([n for n, _ in sizes])):
+        k[end - N + bad] = float("nan") if b else float("inf")
+        v[end - N + bad, :, 5] = float("inf") if b else float("nan")
+    a.cache.append(a.make([(n, n) for n, _ in sizes]), k.cuda(), v.cuda())
+    got = a.run(mask=mask)
+    for b in range(2):
+        first = a.starts[b + 1] - N
+        for i in range(-1, N):
+            seen = i >= 0 and masks[b][i][bad]
+            row, old = got[first + i], clean[first + i]
+            if seen:
+                assert not bool(torch.isfinite(row).all())
+            else:
+                assert same(row, old), (b, i)
+    # values alone: only their components go
+    a.cache.append(a.make([(n, n) for n, _ in sizes]), a.k.cuda(), v.cuda())
+    got = a.run(mask=mask)
+    for b in range(2):
+        first = a.starts[b + 1] - N
+        for i in range(N):
+            row, old = got[first + i], clean[first + i]
+            if masks[b][i][bad]:
+                fin = torch.isfinite(row)
+                assert not fin[:, 5].any()
+                if dtype != "f8":     # (in 8 bits the row's scale is the same: finite values alone make it)
+                    assert bool(fin[:, :5].all()) and bool(fin[:, 6:].all())
+            else:
+                assert same(row, old)
+
+
+def test_unseen_tokens_of_the_window():
+    a = Attend("bf16", [(200, 1), (97, 1)], 4, 32, 2, 64, seed=6)
+    clean = a.run(window=40, sinks=2)
+    k, v = a.k.clone(), a.v.clone()
+    for first, n in ((0, 200), (200, 97)):
+        k[first + 2:first + n - 40] = float("nan")
+        v[first + 2:first + n - 40] = float("inf")
+    a.cache.append(a.make([(n, n) for n, _ in a.sizes]), k.cuda(), v.cuda())
+    assert same(a.run(window=40, sinks=2), clean)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides(dtype):
+    """Queries from a fused tensor, heads before rows, odd addresses; outputs likewise: the same bits."""
+    a = Attend(dtype, [(70, 7), (33, 2)], 4, 32, 2, 64, seed=8)
+    want = a.run()
+    dt = a.cache.data_dtype
+    fused = torch.randn(9, 6, 64, device="cuda").to(dt)
+    fused[:, 1:5] = a.q.cuda()
+    turned = torch.empty(4, 9, 64, dtype=dt, device="cuda").transpose(0, 1).copy_(a.q)
+    off = torch.empty(9 * 256 + 1, dtype=dt, device="cuda")[1:].view(9, 4, 64).copy_(a.q)
+    for q in (fused[:, 1:5], turned, off):
+        for out in (torch.empty(9, 4, 64, dtype=dt, device="cuda"),
+                    torch.empty(4, 9, 64, dtype=dt, device="cuda").transpose(0, 1),
+                    torch.empty(9 * 256 + 1, dtype=dt, device="cuda")[1:].view(9, 4, 64)):
+            a.cache.attend(a.chunk, q, out=out)
+            assert same(out, want)
+
+
+def test_pages_out_of_range_are_not_seen():
+    a = Attend("bf16", [(96, 1)], 4, 32, 2, 64, seed=12)
+    table = a.table.clone()
+    table[0, 1] = -7
+    chunk = binding.Chunk(a.chunk.starts, a.chunk.lens, table.cuda(), 1, 96)
+    got = a.cache.attend(chunk, a.q.cuda())
+    keep = torch.cat([torch.arange(32), torch.arange(64, 96)])
+    ok = np.ones((1, 64), bool)
+    want = ref.attend(a.q, a.k[keep], a.v[keep], 0.125, ok)
+    tol = allowed(a.q, a.k[keep], a.v[keep], 0.125, ok, torch.bfloat16)
+    assert bool(((got.double().cpu() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f8"])
+def test_repeatable_on_streams(dtype):
+    """Two streams at once and many calls: the same bits each time."""
+    a = Attend(dtype, [(3000, 1), (2500, 3)], 8, 64, 2, 128, seed=13)
+    q = a.q.cuda()
+    want = a.run()
+    torch.cuda.synchronize()
+    outs = []
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for n in range(20):
+        outs.append(a.cache.attend(a.chunk, q, stream=streams[n % 2]))
+    torch.cuda.synchronize()
+    for o in outs:
+        assert same(o, want)
+
+
+def test_graph_replays():
+    """Captured once, replayed with other contents (queries, lengths) and eager work in between."""
+    a = Attend("bf16", [(2000, 1), (900, 1)], 8, 64, 2, 128, seed=14)
+    q = a.q.cuda()
+    out = torch.empty_like(q)
+    k, v = a.randn(2).cuda(), a.randn(2).cuda()
+    a.cache.append(a.chunk, k, v)
+    a.cache.attend(a.chunk, q, out=out)      # (the workspace exists)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a.cache.attend(a.chunk, q, out=out)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            a.cache.append(a.chunk, k, v)
+            a.cache.attend(a.chunk, q, out=out)
+    for n in range(4):
+        q.copy_(torch.randn_like(q))
+        k.copy_(torch.randn_like(k))
+        a.chunk.lens.copy_(i32([2000 - 37 * n, 900 - 411 * (n % 2)]))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        a.cache.append(a.chunk, k, v)
+        assert same(a.cache.attend(a.chunk, q), got)
+
+
+def test_refusals():
+    a = Attend("bf16", [(40, 5)], 4, 32, 2, 64)
+    q = a.q.cuda()
+    mask = torch.ones(1, 5, 5, dtype=torch.uint8, device="cuda")
+
+    def status(**kw):
+        with pytest.raises(binding.DTError) as e:
+            a.cache.attend(a.chunk, kw.pop("q", q), **kw)
+        return e.value.status
+
+    assert status(q=torch.zeros(5, 3, 64, dtype=torch.bfloat16, device="cuda")) == -2   # heads % kv_heads
+    assert status(window=-1) == -2
+    assert status(sinks=-1) == -2
+    assert status(scale=float("inf")) == -2
+    assert status(scale=float("nan")) == -2
+    assert status(layer=3) == -2
+    assert status(mask=mask, window=4) == -1                                             # no depths
+    assert status(mask=torch.ones(1, 6, 6, dtype=torch.uint8, device="cuda")) == -2      # more nodes than rows
+    with pytest.raises(ValueError):
+        a.cache.attend(a.chunk, q.float())
+    with pytest.raises(ValueError):
+        a.cache.attend(a.chunk, q, mask=mask.bool())
+    with pytest.raises(ValueError):
+        a.cache.attend(a.chunk, q, out=torch.empty(4, 4, 64, dtype=torch.bfloat16, device="cuda"))
+    long = Attend("bf16", [(9000, 1)], 4, 32, 2, 64)
+    assert long.cache.workspace_size(long.chunk, 1, 4, binding.dt_attend_options(0.1, 0, 0, 0, None, None)) > 0
+    with pytest.raises(binding.DTError) as e:
+        long.cache.attend(long.chunk, long.q.cuda(), workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == -5

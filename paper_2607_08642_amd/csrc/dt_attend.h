@@ -27,20 +27,20 @@ constexpr float kFloor = -1e30f;
 constexpr int kTreeWords = (kMaxB + 2 * kBlk - 2) / kBlk;  // blocks that a tree's nodes touch
 constexpr int kMaxSplits = 64;                              // (one lane each where they are joined)
 
-__device__ inline float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }  // (NaN stays)
-__device__ inline float max3(float a, float b, float c) { return max2(max2(a, b), c); }
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }  // (NaN stays)
+__device__ __forceinline__ float max3(float a, float b, float c) { return max2(max2(a, b), c); }
 // x of this lane and of lane ^ 32
-__device__ inline float2 halves(float x) {
+__device__ __forceinline__ float2 halves(float x) {
   const uint32_t u = __float_as_uint(x);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ inline bf16x8 as_bf16x8(u32x4 v) {
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) {
   bf16x8 r;
   __builtin_memcpy(&r, &v, 16);
   return r;
 }
-__device__ inline uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : ~(~0u << n); }
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : ~(~0u << n); }
 
 // A workgroup's rows and the key blocks that they see.
 struct Tile {
@@ -52,7 +52,7 @@ struct Tile {
   __device__ int block(int it) const { return it < nsb ? it : wb + it - nsb; }
 };
 // false: the tile has no rows
-__device__ inline bool tile_of(const AttendArgs &a, int b, int r0, int tile_rows, Tile *t) {
+__device__ __forceinline__ bool tile_of(const AttendArgs &a, int b, int r0, int tile_rows, Tile *t) {
   t->q = seq_of(a.chunk, a.cache.page_shift, b);
   t->rows = t->q.n * a.group;
   t->r0 = r0;
@@ -76,22 +76,26 @@ __device__ inline bool tile_of(const AttendArgs &a, int b, int r0, int tile_rows
 }
 // workgroups that share the tile's blocks (those after them have none; the last takes
 // what the host's bound left out)
-__device__ inline int active_splits(const AttendArgs &a, const Tile &t) {
+__device__ __forceinline__ int active_splits(const AttendArgs &a, const Tile &t) {
   return min(a.splits, max(1, (t.n_iter + a.split_blocks - 1) / a.split_blocks));
 }
 
 // The rows' nodes as bits: word w of query i0 + t holds its mask over block
 // tree0 / 32 + w, into words[t * kTreeWords + w].  Every thread of the workgroup.
-__device__ inline void tree_words(const AttendArgs &a, const Tile &t, int b, uint32_t *words, int threads) {
+__device__ __forceinline__ void tree_words(const AttendArgs &a, const Tile &t, int b, uint32_t *words, int threads) {
   const int lead = t.q.n - a.nodes, tb0 = max(t.tree0, 0) / kBlk, n = (t.i1 - t.i0 + 1) * kTreeWords;
   for (int x = threadIdx.x; x < n; x += threads) {
     const int m = t.i0 + x / kTreeWords - lead, j0 = (tb0 + x % kTreeWords) * kBlk - t.tree0;
     uint32_t w = 0;
     if (m >= 0 && j0 < a.nodes) {
       const uint8_t *row = a.mask + ((int64_t)b * a.nodes + m) * a.nodes;
-#pragma unroll 8
-      for (int j = 0; j < kBlk; ++j)
-        if (j0 + j >= 0 && j0 + j < a.nodes && row[j0 + j]) w |= 1u << j;
+      uint32_t v[kBlk];  // (bytes outside the row are read as its ends and not taken)
+#pragma unroll
+      for (int j = 0; j < kBlk; ++j) v[j] = row[min(max(j0 + j, 0), a.nodes - 1)];
+      __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is looked at)
+#pragma unroll
+      for (int j = 0; j < kBlk; ++j) w |= (v[j] != 0 ? 1u : 0u) << j;
+      w &= ~low_bits(-j0) & low_bits(a.nodes - j0);
     }
     words[x] = w;
   }
@@ -105,11 +109,11 @@ struct Row {
   // over the wave: bounds that settle most blocks without looking at a lane
   int min_hi, max_lo, min_lo, reach, tree_from;
 };
-__device__ inline int wave_min(int x) {
+__device__ __forceinline__ int wave_min(int x) {
   for (int o = 1; o < 64; o <<= 1) x = min(x, __shfl_xor(x, o));
   return __builtin_amdgcn_readfirstlane(x);
 }
-__device__ inline Row row_of(const AttendArgs &a, const Tile &t, int b, int r, const uint32_t *words) {
+__device__ __forceinline__ Row row_of(const AttendArgs &a, const Tile &t, int b, int r, const uint32_t *words) {
   Row w;
   w.r = min(r, t.rows - 1);
   w.i = w.r / a.group;
@@ -123,22 +127,33 @@ __device__ inline Row row_of(const AttendArgs &a, const Tile &t, int b, int r, c
   w.hi = min(node ? t.tree0 - 1 : t.q.base + w.i, last);
   w.lo = a.window > 0 ? pos - a.window : -1;
   w.words = node ? words + (w.i - t.i0) * kTreeWords : nullptr;
-  const bool nodes = __ballot(node) != 0;
-  w.min_hi = wave_min(w.hi);
-  w.max_lo = -wave_min(-w.lo);
-  w.min_lo = wave_min(w.lo);
-  w.reach = nodes ? last : -wave_min(-w.hi);
+  // the bounds, from the wave's first and last query where they follow from them
+  const int ia = __builtin_amdgcn_readfirstlane(w.i), ib = __builtin_amdgcn_readlane(w.i, 63);
+  const bool nodes = a.nodes > 0 && ib >= lead;
+  const int hi_a = min(nodes && ia >= lead ? t.tree0 - 1 : t.q.base + ia, last);
+  w.min_hi = hi_a;
+  w.reach = nodes ? last : min(t.q.base + ib, last);
   w.tree_from = nodes ? t.tree0 : 0x7fffffff;
+  w.min_lo = w.max_lo = -1;
+  if (a.window > 0) {
+    if (nodes) {
+      w.max_lo = -wave_min(-w.lo);
+      w.min_lo = wave_min(w.lo);
+    } else {
+      w.min_lo = t.q.base + ia - a.window;
+      w.max_lo = t.q.base + ib - a.window;
+    }
+  }
   return w;
 }
-__device__ inline bool sees_all(const AttendArgs &a, const Row &w, int k0) {
+__device__ __forceinline__ bool sees_all(const AttendArgs &a, const Row &w, int k0) {
   return k0 + kBlk - 1 <= w.min_hi && (k0 > w.max_lo || (a.window > 0 && k0 + kBlk <= a.sinks));
 }
-__device__ inline bool sees_none(const AttendArgs &a, const Row &w, int k0) {
+__device__ __forceinline__ bool sees_none(const AttendArgs &a, const Row &w, int k0) {
   return k0 > w.reach || (k0 + kBlk - 1 <= w.min_lo && k0 >= a.sinks && k0 + kBlk <= w.tree_from);
 }
 // bit j: the lane's row sees token j of block k0
-__device__ inline uint32_t seen_word(const AttendArgs &a, const Tile &t, const Row &w, int k0) {
+__device__ __forceinline__ uint32_t seen_word(const AttendArgs &a, const Tile &t, const Row &w, int k0) {
   uint32_t v = low_bits(w.hi - k0 + 1);
   if (a.window > 0) v &= ~low_bits(w.lo + 1 - k0) | low_bits(a.sinks - k0);
   if (w.words) {
@@ -151,71 +166,82 @@ __device__ inline uint32_t seen_word(const AttendArgs &a, const Tile &t, const R
 // token of a block in register i of a lane's half of S^T
 __device__ constexpr int reg_token(int i) { return 8 * (i / 4) + i % 4; }  // + 4 h
 
+template <int T>
+__device__ __forceinline__ void rescale(f32x16 (&o)[T], float f) {
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] *= f;
+}
+
 // One block's scores into probabilities (masked: bits of `seen`, already shifted by 4 h).
-// m: running maximum, l: this lane's part of the sum.  Returns the factor of what was
-// summed before, and whether any row of the wave needs it.
-template <bool MASKED>
-__device__ inline float softmax_block(const f32x16 &s, uint32_t seen, float c, float &m, float &l, float (&p)[16]) {
+// m: the reference that exponents are taken against, l: this lane's part of the sum.  m
+// is raised, and what was summed scaled, only once a row's maximum lies more than kSlack
+// above it: probabilities up to 2^kSlack do no harm in fp32, nor rounded to bf16, and after a
+// tile's first blocks the scaling (as many products as there are sums) hardly ever runs.
+constexpr float kSlack = 8.0f;
+template <bool MASKED, int T>
+__device__ __forceinline__ void softmax_block(const f32x16 &s, uint32_t seen, float c, float &m, float &l,
+                                              f32x16 (&o)[T], float (&p)[16]) {
   float x[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = MASKED && !(seen >> reg_token(i) & 1) ? -__builtin_huge_valf() : s[i];
   float top = max3(x[0], x[1], x[2]);
 #pragma unroll
   for (int i = 3; i < 15; i += 2) top = max3(top, x[i], x[i + 1]);
-  const float2 th = halves(max3(top, x[15], x[15]));
-  const float now = max3(m, max3(th.x, th.y, th.y) * c, kFloor);
-  const float f = __builtin_amdgcn_exp2f(m - now);
-  m = now;
+  const float2 th = halves(max2(top, x[15]));
+  const float now = max2(th.x, th.y) * c;
+  if (__ballot(now > m + kSlack)) {
+    const float to = now > m ? now : m, f = __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    l *= f;
+    rescale(o, f);
+  }
   float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -now));
+    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m));
     if (MASKED) p[i] = seen >> reg_token(i) & 1 ? p[i] : 0.0f;
     if (i & 1)
       sum1 += p[i];
     else
       sum0 += p[i];
   }
-  l = l * f + (sum0 + sum1);
-  return f;
+  l += sum0 + sum1;
 }
 
 // eight probabilities (registers 8 s .. 8 s + 7) as the second operand of step s
-__device__ inline bf16x8 pack_p(const float (&p)[16], int s) {
+__device__ __forceinline__ bf16x8 pack_p(const float (&p)[16], int s) {
   f32x8 v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = p[8 * s + i];
   return __builtin_convertvector(v, bf16x8);
 }
-__device__ inline bf16x8 pack_seen(uint32_t seen, int s) {  // 1 where a token is seen
+__device__ __forceinline__ bf16x8 pack_seen(uint32_t seen, int s) {  // 1 where a token is seen
   f32x8 v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = seen >> reg_token(8 * s + i) & 1 ? 1.0f : 0.0f;
   return __builtin_convertvector(v, bf16x8);
 }
-// values with their NaN and infinities as 0, and 1 in their places
-__device__ inline void split_bad(u32x4 v, u32x4 &clean, u32x4 &bad) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool lo = (v[i] & 0x7f80u) == 0x7f80u, hi = (v[i] & 0x7f800000u) == 0x7f800000u;
-    clean[i] = v[i] & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-    bad[i] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
-  }
+// A word of values: all bits of its non-finite elements (`one` masked by them: 1 in their places).
+template <int DT>
+constexpr uint32_t kOnes = DT == DT_F32 ? 0x3f800000u : DT == DT_BF16 ? 0x3f803f80u : 0x38383838u;
+template <int DT>
+__device__ __forceinline__ uint32_t bad_bits(uint32_t v) {
+  if (DT == DT_F32) return (v & 0x7f800000u) == 0x7f800000u ? ~0u : 0u;
+  if (DT == DT_BF16)
+    return ((v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+  // a code of seven ones; a carry out of them is bit 7
+  const uint32_t t = ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (t >> 7) * 0xffu;
 }
-__device__ inline bool has_bad(u32x4 v) {
-  bool r = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
-  return r;
-}
-
-__device__ inline f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-__device__ inline f32x16 mfma(float a, float b, f32x16 c) {
+__device__ __forceinline__ f32x16 mfma(float a, float b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
 }
-__device__ inline f32x16 zero16() {
+__device__ __forceinline__ f32x16 zero16() {
   f32x16 z;
 #pragma unroll
   for (int i = 0; i < 16; ++i) z[i] = 0.0f;
@@ -231,39 +257,194 @@ struct QRegs {
 };
 // (scale < 0: the sign goes into q)
 template <int DT, int D>
-__device__ inline void load_q(const AttendArgs &a, const Tile &t, const Row &w, int head, int h, bool interleave8,
+__device__ __forceinline__ void load_q(const AttendArgs &a, const Tile &t, const Row &w, int head, int h, bool interleave8,
                               QRegs<DT, D> &q) {
   const int64_t at = (int64_t)(t.q.row0 + w.i) * a.q.row + (int64_t)(head * a.group + w.r % a.group) * a.q.head;
+  // first element of piece n: f32 pieces of 4, bf16 of 8; an 8-bit cache's pieces of 16
+  // elements are two operands
+  auto first = [&](int n) {
+    return DT == DT_F32 ? (2 * n + h) * 4 : interleave8 ? (2 * (n >> 1) + h) * 16 + 8 * (n & 1) : (2 * n + h) * 8;
+  };
+  if (a.q.vec) {
+#pragma unroll
+    for (int n = 0; n < QRegs<DT, D>::N; ++n)
+      q.v[n] = *reinterpret_cast<const u32x4 *>(a.q.p + (at + first(n)) * (DT == DT_F32 ? 4 : 2));
+  } else {
+#pragma unroll
+    for (int n = 0; n < QRegs<DT, D>::N; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (DT == DT_F32) {
+          q.v[n][j] = reinterpret_cast<const uint32_t *>(a.q.p)[at + first(n) + j];
+        } else {
+          const uint16_t *p = reinterpret_cast<const uint16_t *>(a.q.p) + at + first(n) + 2 * j;
+          q.v[n][j] = p[0] | (uint32_t)p[1] << 16;
+        }
+  }
   const uint32_t flip = a.scale_log2e < 0.0f ? (DT == DT_F32 ? 0x80000000u : 0x80008000u) : 0u;
 #pragma unroll
-  for (int n = 0; n < QRegs<DT, D>::N; ++n) {
-    // first element of piece n: f32 pieces of 4, bf16 of 8; an 8-bit cache's pieces of 16
-    // elements are two operands
-    const int d = DT == DT_F32 ? (2 * n + h) * 4 : interleave8 ? (2 * (n >> 1) + h) * 16 + 8 * (n & 1) : (2 * n + h) * 8;
-    u32x4 v;
-    if (DT == DT_F32) {
-      const float *p = reinterpret_cast<const float *>(a.q.p) + at + d;
-      if (a.q.vec)
-        v = *reinterpret_cast<const u32x4 *>(p);
-      else
+  for (int n = 0; n < QRegs<DT, D>::N; ++n)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(p[j]);
-    } else {
-      const uint16_t *p = reinterpret_cast<const uint16_t *>(a.q.p) + at + d;
-      if (a.q.vec)
-        v = *reinterpret_cast<const u32x4 *>(p);
-      else
+    for (int j = 0; j < 4; ++j) q.v[n][j] ^= flip;
+}
+
+// Waits of a wave for its copies from memory to LDS: at most N of them on their way, its LDS
+// reads done.  (Copies are not in the compiler's sight: no read moves over a wait.)
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N < 64, "");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | (N >> 4) << 14);  // vmcnt(N) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+// 64 lanes' 16 bytes (or 4) from their addresses to LDS, lane after lane
+__device__ __forceinline__ void copy16(const char *lane_src, char *dst) {
+  __builtin_amdgcn_global_load_lds(lane_src, (__attribute__((address_space(3))) char *)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void copy4(const char *lane_src, char *dst) {
+  __builtin_amdgcn_global_load_lds(lane_src, (__attribute__((address_space(3))) char *)dst, 4, 0, 0);
+}
+
+// eight 8-bit elements (words a, b) times a power of two
+__device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float scale) {
+  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false),
+               y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
+               z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false),
+               w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+  return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+__device__ __forceinline__ u32x4 lds16(const char *p) { return *reinterpret_cast<const u32x4 *>(p); }
+
+// S^T of a block: `keys` in LDS in the cache's order (DT_F8: `exps` their 32 exponents).
+template <int DT, int D>
+__device__ __forceinline__ f32x16 scores(const char *keys, const char *exps, const QRegs<DT, D> &q, int lane) {
+  f32x16 s = zero16();
+  const char *kp = keys + lane * 16;
+  if constexpr (DT == DT_F32) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = p[2 * j] | (uint32_t)p[2 * j + 1] << 16;
+    for (int n = 0; n < D / 8; ++n) {
+      const u32x4 k = lds16(kp + n * 1024);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = mfma(__uint_as_float(k[j]), __uint_as_float(q.v[n][j]), s);
     }
+  } else if constexpr (DT == DT_BF16) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q.v[n][j] = v[j] ^ flip;
+    for (int n = 0; n < D / 16; ++n) s = mfma(as_bf16x8(lds16(kp + n * 1024)), as_bf16x8(q.v[n]), s);
+  } else {
+    const float e = exp_of(reinterpret_cast<const uint8_t *>(exps)[lane & 31]);
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) {
+      const u32x4 k = lds16(kp + n * 1024);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s = mfma(widen8(k[2 * u], k[2 * u + 1], e), as_bf16x8(q.v[2 * n + u]), s);
+    }
+  }
+  return s;
+}
+
+// O^T += V^T P^T of a block: `vals` in LDS in the cache's order (DT_F8: `exps` their 32
+// exponents, which go to the probabilities: a product with a power of two, exact).
+// MASKED: non-finite values that not all rows see make NaN (of those components) of the rows
+// that do and are 0 for the others.
+template <int DT, int D, bool MASKED>
+__device__ __forceinline__ void add_values(const char *vals, const char *exps, float (&p)[16], uint32_t seen, int lane,
+                                           f32x16 (&o)[D / 32]) {
+  constexpr int T = D / 32, S = DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1;  // 16-byte pieces of a lane's tokens
+  const int h = lane >> 5, l32 = lane & 31;
+  const char *vp = vals + (h * D + l32) * 16;
+  auto piece = [&](int s, int t) { return lds16(vp + (2 * s * D + 32 * t) * 16); };
+  bf16x8 pf[2];
+  if constexpr (DT == DT_F8) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t w = *reinterpret_cast<const uint32_t *>(exps + 8 * t + 4 * h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = __uint_as_float((j == 3 ? w >> 1 : w << (23 - 8 * j)) & 0x7f800000u);
+        p[4 * t + j] = MASKED && !(seen >> reg_token(4 * t + j) & 1) ? 0.0f : p[4 * t + j] * e;
+      }
+    }
+  }
+  if constexpr (DT != DT_F32) {
+    pf[0] = pack_p(p, 0);
+    pf[1] = pack_p(p, 1);
+  }
+  // the products of one d tile with pieces v
+  auto products = [&](const u32x4 (&v)[S], f32x16 acc) {
+    if constexpr (DT == DT_F32) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = mfma(__uint_as_float(v[s][j]), p[4 * s + j], acc);
+    } else if constexpr (DT == DT_BF16) {
+      acc = mfma(as_bf16x8(v[0]), pf[0], acc);
+      acc = mfma(as_bf16x8(v[1]), pf[1], acc);
+    } else {
+      acc = mfma(widen8(v[0][0], v[0][1], 1.0f), pf[0], acc);
+      acc = mfma(widen8(v[0][2], v[0][3], 1.0f), pf[1], acc);
+    }
+    return acc;
+  };
+  if constexpr (MASKED) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int n = 0; n < S * T; ++n) {
+      const u32x4 v = piece(n / T, n % T);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= bad_bits<DT>(v[i]);
+      if (n % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight pieces at a time: registers)
+    }
+    const bool any = __ballot(bad != 0) != 0;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      u32x4 v[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) v[s] = piece(s, t);
+      if (any) {
+        u32x4 one[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = bad_bits<DT>(v[s][i]);
+            one[s][i] = x & kOnes<DT>;
+            v[s][i] &= ~x;
+          }
+        f32x16 hit = zero16();
+        if constexpr (DT == DT_F32) {
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              hit = mfma(__uint_as_float(one[s][j]), seen >> reg_token(4 * s + j) & 1 ? 1.0f : 0.0f, hit);
+        } else if constexpr (DT == DT_BF16) {
+          hit = mfma(as_bf16x8(one[0]), pack_seen(seen, 0), hit);
+          hit = mfma(as_bf16x8(one[1]), pack_seen(seen, 1), hit);
+        } else {
+          hit = mfma(widen8(one[0][0], one[0][1], 1.0f), pack_seen(seen, 0), hit);
+          hit = mfma(widen8(one[0][2], one[0][3], 1.0f), pack_seen(seen, 1), hit);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[t][i];
+      }
+      o[t] = products(v, o[t]);
+      __builtin_amdgcn_sched_barrier(0);  // (one d tile at a time: registers)
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      u32x4 v[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) v[s] = piece(s, t);
+      o[t] = products(v, o[t]);
+    }
   }
 }
 
 // A wave's 32 finished rows: the result, or one split's part of it.
 template <int DT, int D>
-__device__ inline void write_rows(const AttendArgs &a, const Tile &t, const Row &w, int head, int split, bool direct,
+__device__ __forceinline__ void write_rows(const AttendArgs &a, const Tile &t, const Row &w, int head, int split, bool direct,
                                   bool valid, int h, const f32x16 (&o)[D / 32], float m, float l) {
   if (!valid) return;
   const int hq = head * a.group + w.r % a.group;

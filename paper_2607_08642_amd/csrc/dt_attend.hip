@@ -1,186 +1,41 @@
 // Attention over the paged cache for few rows (single tokens, small trees; fp32 of any
 // size), the join of split calls, and the choice of kernel and split.
 //
-// stream_kernel: a workgroup of four waves holds 32 rows of one kv head; each wave
-// walks key blocks of its own (every fourth) with its own running softmax, the
-// blocks' pieces going from memory into the registers of the matrix operands.
-// Nothing passes through LDS and no wave waits for another until the four partial
-// results meet at the end.  Bound by memory: a block of 32 tokens (16 KB at bf16, D =
-// 128) takes about a thousand cycles of a wave, a CU's eight waves then ask for four
-// times the bytes that it can get.
+// stream_kernel: the waves of a workgroup hold the same 32 rows of one kv head; each walks key
+// blocks of its own (every W-th) with its own running softmax and its own ring of LDS slots,
+// which it fills by copies from memory that pass no registers: keys of block n + slots are
+// asked for when those of block n have been used, and the values after them.  No wave waits
+// for another until their partial results meet at the end.
 #include "dt_attend.h"
 
 namespace dt {
 namespace {
 using namespace att;
 
-constexpr int kStreamWaves = 4, kStreamRows = 32;
+constexpr int kStreamRows = 32;
 
-// One block's keys and values in a wave's registers.
-template <int DT, int D>
-struct BlockRegs {
-  static constexpr int N = D * (DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1) / 32;  // 16-byte pieces of a lane
-  u32x4 k[N], v[N];
-  uint32_t ke, ve[4];  // DT_F8: the key's exponent; of the values, tokens 8 t + 4 h + 0..3 in ve[t]
-};
-
+// Shape of a workgroup: waves, and blocks in a wave's ring, for at most 144 KB of LDS.
 template <int DT, int D>
 struct Stream {
-  static constexpr int N = BlockRegs<DT, D>::N, ES = DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1;
-  // (fp32 at D = 256: keys and values would not fit beside the sums)
-  static constexpr bool kAhead = N * 8 <= 128;
+  static constexpr int ES = DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1;
+  static constexpr int kPart = kBlk * D * ES;                       // a block's keys, or values
+  static constexpr int kExps = DT == DT_F8 ? 256 : 0;               // its exponents, as copied
+  static constexpr int kWaves = kPart <= 16384 ? 4 : 2;
+  static constexpr int kFit = 147456 / (kWaves * (2 * kPart + kExps));
+  static constexpr int kSlots = kFit > 4 ? 4 : kFit;
+  static constexpr int kLds = kWaves * kSlots * (2 * kPart + kExps);
+  static constexpr int kOps = kPart / 1024;                         // copies of a part
 };
-
-template <int DT, int D>
-__device__ inline void load_k(BlockRegs<DT, D> &r, const char *kb, const char *ex, int lane) {
-#pragma unroll
-  for (int n = 0; n < BlockRegs<DT, D>::N; ++n) r.k[n] = *reinterpret_cast<const u32x4 *>(kb + lane * 16 + n * 1024);
-  if (DT == DT_F8) r.ke = reinterpret_cast<const uint8_t *>(ex)[lane & 31];
-}
-// piece of values n: the n-th run of 32 d of the lane's tokens
-template <int DT, int D>
-__device__ inline int v_piece(int n, int h, int l32) {
-  constexpr int T = D / 32;
-  const int x = n / T, d = 32 * (n % T) + l32;  // bf16: step x; 8 bits: x = 0; fp32: tokens 8 x + 4 h ..
-  return ((DT == DT_F8 ? h : 2 * x + h) * D + d) * 16;
-}
-template <int DT, int D>
-__device__ inline void load_v(BlockRegs<DT, D> &r, const char *vb, const char *ex, int h, int l32) {
-#pragma unroll
-  for (int n = 0; n < BlockRegs<DT, D>::N; ++n)
-    r.v[n] = *reinterpret_cast<const u32x4 *>(vb + v_piece<DT, D>(n, h, l32));
-  if (DT == DT_F8)
-#pragma unroll
-    for (int t = 0; t < 4; ++t) r.ve[t] = *reinterpret_cast<const uint32_t *>(ex + 8 * t + 4 * h);
-}
-
-// eight 8-bit elements (words a, b) times a power of two
-__device__ inline bf16x8 widen8(uint32_t a, uint32_t b, float scale) {
-  const bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false),
-               y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
-               z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false),
-               w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
-  return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
-}
-
-template <int DT, int D>
-__device__ inline f32x16 scores(const BlockRegs<DT, D> &r, const QRegs<DT, D> &q) {
-  f32x16 s = zero16();
-  if constexpr (DT == DT_F32) {
-#pragma unroll
-    for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s = mfma(__uint_as_float(r.k[n][j]), __uint_as_float(q.v[n][j]), s);
-  } else if constexpr (DT == DT_BF16) {
-#pragma unroll
-    for (int n = 0; n < D / 16; ++n) s = mfma(as_bf16x8(r.k[n]), as_bf16x8(q.v[n]), s);
-  } else {
-    const float e = exp_of(r.ke);
-#pragma unroll
-    for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        s = mfma(widen8(r.k[n][2 * u], r.k[n][2 * u + 1], e), as_bf16x8(q.v[2 * n + u]), s);
-  }
-  return s;
-}
-
-// O^T += V^T P^T; with MASKED, non-finite values of tokens that a row does not see stay out
-template <int DT, int D, bool MASKED>
-__device__ inline void add_values(const BlockRegs<DT, D> &r, float (&p)[16], uint32_t seen, f32x16 (&o)[D / 32]) {
-  constexpr int T = D / 32;
-  if constexpr (DT == DT_F32) {
-    bool bad = false;
-    if (MASKED)
-#pragma unroll
-      for (int n = 0; n < 4 * T; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) bad |= (r.v[n][j] & 0x7f800000u) == 0x7f800000u;
-    if (MASKED && __ballot(bad)) {
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        f32x16 hit = zero16();
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t v = r.v[x * T + t][j];
-            const bool b = (v & 0x7f800000u) == 0x7f800000u;
-            o[t] = mfma(__uint_as_float(b ? 0u : v), p[4 * x + j], o[t]);
-            hit = mfma(b ? 1.0f : 0.0f, seen >> reg_token(4 * x + j) & 1 ? 1.0f : 0.0f, hit);
-          }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[t][i];
-      }
-      return;
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int t = 0; t < T; ++t) o[t] = mfma(__uint_as_float(r.v[x * T + t][j]), p[4 * x + j], o[t]);
-  } else {
-    if constexpr (DT == DT_F8) {
-      // the tokens' exponents go to the probabilities (a product with a power of two: exact)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = __uint_as_float((i % 4 == 3 ? r.ve[i / 4] >> 1 : r.ve[i / 4] << (23 - 8 * (i % 4))) & 0x7f800000u);
-        p[i] = MASKED ? (seen >> reg_token(i) & 1 ? p[i] * e : 0.0f) : p[i] * e;
-      }
-    }
-    bf16x8 pf[2] = {pack_p(p, 0), pack_p(p, 1)};
-    auto frag = [&](int s, int t) {
-      if constexpr (DT == DT_F8)
-        return widen8(r.v[t][2 * s], r.v[t][2 * s + 1], 1.0f);
-      else
-        return as_bf16x8(r.v[s * T + t]);
-    };
-    auto raw = [&](int s, int t) {
-      const bf16x8 f = frag(s, t);
-      u32x4 u;
-      __builtin_memcpy(&u, &f, 16);
-      return u;
-    };
-    if (MASKED) {
-      bool bad = false;
-#pragma unroll
-      for (int n = 0; n < 2 * T; ++n) bad |= has_bad(raw(n / T, n % T));
-      if (__ballot(bad)) {
-        const bf16x8 sf[2] = {pack_seen(seen, 0), pack_seen(seen, 1)};
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-          f32x16 hit = zero16();
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            u32x4 clean, b;
-            split_bad(raw(s, t), clean, b);
-            o[t] = mfma(as_bf16x8(clean), pf[s], o[t]);
-            hit = mfma(as_bf16x8(b), sf[s], hit);
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[t][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[t][i];
-        }
-        return;
-      }
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int t = 0; t < T; ++t) o[t] = mfma(frag(s, t), pf[s], o[t]);
-  }
-}
 
 // grid: kv head (fastest: the workgroups of a head share an XCD's cache where there are
 // eight heads), tile, split; sequence
 template <int DT, int D>
-__global__ __launch_bounds__(64 * kStreamWaves, DT != DT_F32 && D <= 128 ? 2 : 1) void stream_kernel(AttendArgs a,
-                                                                                                      int tiles) {
+__global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(AttendArgs a, int tiles) {
   using St = Stream<DT, D>;
-  constexpr int T = D / 32, ES = St::ES;
+  constexpr int T = D / 32, ES = St::ES, W = St::kWaves, NS = St::kSlots;
   __shared__ uint32_t words[kStreamRows * kTreeWords];
-  __shared__ float ml[kStreamWaves][2][32];
-  __shared__ float meet[2][D][32];
+  __shared__ float ml[W][2][32];
+  __shared__ __align__(16) char ring[St::kLds];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
   const int head = blockIdx.x % a.cache.kv, tile = blockIdx.x / a.cache.kv % tiles,
@@ -190,83 +45,113 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT != DT_F32 && D <= 128 ? 2 : 1
   const int active = active_splits(a, t);
   if (split >= active) return;
   const int it0 = split * a.split_blocks, it1 = split == active - 1 ? t.n_iter : it0 + a.split_blocks;
-  if (a.nodes > 0) {
-    tree_words(a, t, b, words, 64 * kStreamWaves);
-    __syncthreads();
-  }
+
+  // ---- its rows (q asked for before the blocks: it comes first)
   const Row w = row_of(a, t, b, t.r0 + l32, words);
   const float c = __builtin_fabsf(a.scale_log2e);
   QRegs<DT, D> q;
   load_q<DT, D>(a, t, w, head, h, DT == DT_F8, q);
+
+  // ---- the wave's blocks: copies into its ring
+  const int32_t *table = a.chunk.table + (int64_t)b * a.chunk.width;
+  const int shift = a.cache.page_shift;
+  auto page_of = [&](int it) { return it < it1 ? scalar_at(table, t.block(it) * kBlk >> shift) : 0; };
+  // head page of a block (out of range: page 0, whose tokens then count as unseen), token in it
+  auto place = [&](int it, int page, int *n) {
+    const int p = __builtin_amdgcn_readfirstlane(page);
+    *n = t.block(it) * kBlk & ((1 << shift) - 1);
+    return a.cache.base + (int64_t)((uint32_t)p < (uint32_t)a.cache.pages ? p : 0) * a.cache.page_bytes +
+           head * a.cache.head_bytes;
+  };
+  char *mine = ring + wave * (St::kLds / W);
+  auto keys = [&](int s) { return mine + s * (2 * St::kPart + St::kExps); };
+  auto copy_keys = [&](int it, int page, int s) {
+    int n;
+    const char *hp = place(it, page, &n);
+    if (DT == DT_F8)  // lanes 0-7 (mod 16): the keys' 32 exponents, 8-15: the values'
+      copy4(hp + a.cache.s_off + n + (lane & 7) * 4 + (lane & 8 ? 1 << shift : 0), keys(s) + 2 * St::kPart);
+    hp += (int64_t)n * D * ES + lane * 16;
+#pragma unroll
+    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, keys(s) + x * 1024);
+  };
+  auto copy_vals = [&](int it, int page, int s) {
+    int n;
+    const char *hp = place(it, page, &n);
+    hp += a.cache.v_off + (int64_t)n * D * ES + lane * 16;
+#pragma unroll
+    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, keys(s) + St::kPart + x * 1024);
+  };
+  constexpr int kK = St::kOps + (DT == DT_F8 ? 1 : 0), kV = St::kOps;
+  int it = it0 + wave;
+  int pages[NS + 1];  // of blocks it, it + W, ..
+#pragma unroll
+  for (int x = 0; x <= NS; ++x) pages[x] = page_of(it + x * W);
+#pragma unroll
+  for (int x = 0; x < NS; ++x)
+    if (it + x * W < it1) {
+      copy_keys(it + x * W, pages[x], x);
+      copy_vals(it + x * W, pages[x], x);
+    }
+
+  if (a.nodes > 0) {
+    tree_words(a, t, b, words, 64 * W);
+    __syncthreads();
+  }
   f32x16 o[T];
 #pragma unroll
   for (int n = 0; n < T; ++n) o[n] = zero16();
   float m = kFloor, l = 0.0f;
 
-  const int32_t *table = a.chunk.table + (int64_t)b * a.chunk.width;
-  const int shift = a.cache.page_shift;
-  auto page_of = [&](int it) { return it < it1 ? table[t.block(it) * kBlk >> shift] : 0; };
-  // the head page of a block (an out-of-range page: page 0, whose tokens then count as unseen)
-  auto page_at = [&](int page) {
-    const int p = __builtin_amdgcn_readfirstlane(page);
-    return a.cache.base + (int64_t)((uint32_t)p < (uint32_t)a.cache.pages ? p : 0) * a.cache.page_bytes +
-           head * a.cache.head_bytes;
-  };
-  auto in_page = [&](int it) { return t.block(it) * kBlk & ((1 << shift) - 1); };
-  BlockRegs<DT, D> r;
-  auto fetch_k = [&](int it, int page) {
-    const char *hp = page_at(page);
-    const int n = in_page(it);
-    load_k<DT, D>(r, hp + (int64_t)n * D * ES, hp + a.cache.s_off + n, lane);
-  };
-  auto fetch_v = [&](int it, int page) {
-    const char *hp = page_at(page);
-    const int n = in_page(it);
-    load_v<DT, D>(r, hp + a.cache.v_off + (int64_t)n * D * ES, hp + a.cache.s_off + (1 << shift) + n, h, l32);
-  };
-  int it = it0 + wave;
-  int page = page_of(it), next = page_of(it + kStreamWaves);
-  if (St::kAhead && it < it1) {
-    fetch_k(it, page);
-    fetch_v(it, page);
-  }
-  for (; it < it1; it += kStreamWaves) {
-    const int after = page_of(it + 2 * kStreamWaves), k0 = t.block(it) * kBlk;
-    const bool more = it + kStreamWaves < it1, skip = sees_none(a, w, k0);
-    const bool all = sees_all(a, w, k0) && (uint32_t)page < (uint32_t)a.cache.pages;
-    if (!St::kAhead && !skip) {
-      fetch_k(it, page);
-      fetch_v(it, page);
-    }
+  int slot = 0;
+  for (; it < it1; it += W) {
+    const int after = page_of(it + (NS + 1) * W), k0 = t.block(it) * kBlk;
+    // (all slots asked for: the block's keys are there when this many copies are not; else wait for all)
+    const bool steady = it + (NS - 1) * W < it1, more = it + NS * W < it1;
+    const bool skip = sees_none(a, w, k0), there = (uint32_t)pages[0] < (uint32_t)a.cache.pages;
+    const bool all = there && sees_all(a, w, k0);
+    const char *kp = keys(slot), *ex = kp + 2 * St::kPart;
+    if (steady)
+      wait_copies<kV + (NS - 1) * (kK + kV)>();
+    else
+      wait_copies<0>();
     f32x16 s;
-    if (!skip) s = scores<DT, D>(r, q);
-    if (St::kAhead && more) fetch_k(it + kStreamWaves, next);
+    if (!skip) s = scores<DT, D>(kp, ex, q, lane);
+    wait_copies<63>();  // (LDS reads done: the keys' place is free)
+    // (DT_F8: the exponents' place is not, the values' are still to be read; they come with
+    // the next block's keys, so those are asked for after the values)
+    if (DT != DT_F8 && more) copy_keys(it + NS * W, pages[NS], slot);
+    float p[16];
+    uint32_t seen = 0;
     if (!skip) {
-      float p[16];
-      uint32_t seen = 0;
-      float f;
       if (all) {
-        f = softmax_block<false>(s, 0, c, m, l, p);
+        softmax_block<false>(s, 0, c, m, l, o, p);
       } else {
-        seen = (uint32_t)page < (uint32_t)a.cache.pages ? seen_word(a, t, w, k0) >> (4 * h) : 0;
-        f = softmax_block<true>(s, seen, c, m, l, p);
+        seen = there ? seen_word(a, t, w, k0) >> (4 * h) : 0;
+        softmax_block<true>(s, seen, c, m, l, o, p);
       }
-      if (__ballot(f != 1.0f))
-#pragma unroll
-        for (int n = 0; n < T; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[n][i] *= f;
-      if (all)
-        add_values<DT, D, false>(r, p, 0, o);
-      else
-        add_values<DT, D, true>(r, p, seen, o);
     }
-    if (St::kAhead && more) fetch_v(it + kStreamWaves, next);
-    page = next;
-    next = after;
+    if (steady && more)
+      wait_copies<(NS - 1) * (kK + kV) + (DT != DT_F8 ? kK : 0)>();
+    else
+      wait_copies<0>();
+    if (!skip) {
+      if (all)
+        add_values<DT, D, false>(kp + St::kPart, ex + 32, p, 0, lane, o);
+      else
+        add_values<DT, D, true>(kp + St::kPart, ex + 32, p, seen, lane, o);
+    }
+    wait_copies<63>();
+    if (more) {
+      if (DT == DT_F8) copy_keys(it + NS * W, pages[NS], slot);
+      copy_vals(it + NS * W, pages[NS], slot);
+    }
+#pragma unroll
+    for (int x = 0; x < NS; ++x) pages[x] = pages[x + 1];
+    pages[NS] = after;
+    slot = slot == NS - 1 ? 0 : slot + 1;
   }
 
-  // the four waves' results meet: each scaled to the common maximum, then 2 + 2 and 1 + 1
+  // ---- the waves' results meet, each scaled to the common maximum: upper half to lower half
   const float2 lh = halves(l);
   l = lh.x + lh.y;
   if (h == 0) {
@@ -274,34 +159,37 @@ __global__ __launch_bounds__(64 * kStreamWaves, DT != DT_F32 && D <= 128 ? 2 : 1
     ml[wave][1][l32] = l;
   }
   __syncthreads();
-  const float top = max2(max2(ml[0][0][l32], ml[1][0][l32]), max2(ml[2][0][l32], ml[3][0][l32]));
+  float top = ml[0][0][l32];
+#pragma unroll
+  for (int x = 1; x < W; ++x) top = max2(top, ml[x][0][l32]);
   l = 0.0f;
 #pragma unroll
-  for (int x = 0; x < kStreamWaves; ++x) l += ml[x][1][l32] * __builtin_amdgcn_exp2f(ml[x][0][l32] - top);
+  for (int x = 0; x < W; ++x) l += ml[x][1][l32] * __builtin_amdgcn_exp2f(ml[x][0][l32] - top);
   const float f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
   for (int n = 0; n < T; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[n][i] *= f;
-  auto put = [&](int slot) {
+  // (every wave is past its last block: the rings are free.  [D][32 rows] fp32 of a wave.)
+  static_assert(W / 2 * D * 128 <= St::kLds, "");
+  float *meet = reinterpret_cast<float *>(ring);
 #pragma unroll
-    for (int n = 0; n < T; ++n)
+  for (int half = W / 2; half > 0; half >>= 1) {
+    float *at = meet + (wave & (half - 1)) * (D * 32) + 4 * h * 32 + l32;
+    if (wave >= half && wave < 2 * half)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) meet[slot][32 * n + reg_token(i) + 4 * h][l32] = o[n][i];
-  };
-  auto add = [&](int slot) {
+      for (int n = 0; n < T; ++n)
 #pragma unroll
-    for (int n = 0; n < T; ++n)
+        for (int i = 0; i < 16; ++i) at[(32 * n + reg_token(i)) * 32] = o[n][i];
+    __syncthreads();
+    if (wave < half)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[n][i] += meet[slot][32 * n + reg_token(i) + 4 * h][l32];
-  };
-  if (wave >= 2) put(wave - 2);
-  __syncthreads();
-  if (wave < 2) add(wave);
-  if (wave == 1) put(1);  // (slot 1 is its own)
-  __syncthreads();
+      for (int n = 0; n < T; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[n][i] += at[(32 * n + reg_token(i)) * 32];
+    __syncthreads();
+  }
   if (wave > 0) return;
-  add(1);
   write_rows<DT, D>(a, t, w, head, split, active == 1, t.r0 + l32 < t.rows, h, o, top, l);
 }
 
@@ -346,39 +234,57 @@ hipError_t launch_stream(const AttendArgs &a, const AttendPlan &p, hipStream_t s
            : a.cache.D == 96  ? stream_kernel<DT, 96>
            : a.cache.D == 128 ? stream_kernel<DT, 128>
                               : stream_kernel<DT, 256>;
-  f<<<grid, 64 * kStreamWaves, 0, s>>>(a, p.tiles);
+  f<<<grid, 64 * p.waves, 0, s>>>(a, p.tiles);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// (as Stream::kWaves)
+static int stream_waves(int dtype, int D) { return kBlk * D * elem_bytes(dtype) <= 16384 ? 4 : 2; }
+
 AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int heads, int window, int sinks, int nodes) {
-  const int group = heads / c.kv, rows = k.max_chunk * group;
+  const int group = heads / c.kv, rows = k.max_chunk * group, sets = (rows + 31) / 32;
   AttendPlan p;
-  p.tile_rows = kStreamRows;
-  p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+  // few rows, or fp32: every wave its own blocks; more rows share them through LDS
+  const bool stream = dtype == DT_F32 || sets == 1;
+  p.waves = stream ? stream_waves(dtype, c.D) : sets <= 12 ? 4 : 8;
+  p.stream = stream;
+  const int full = stream ? 1 : p.waves;
+  p.tiles = (sets + full - 1) / full;
+  p.tile_rows = (sets + p.tiles - 1) / p.tiles * 32;  // (even tiles: 9 sets of 32 rows are 3 + 3 + 3, not 4 + 4 + 1)
   // blocks of a tile at most
   const int all = (k.max_len + kBlk - 1) / kBlk;
   int most = all;
   if (window > 0) {
-    const int span = window + (p.tile_rows + group - 1) / group + 1 + nodes;
+    const int64_t span = (int64_t)window + (p.tile_rows + group - 1) / group + 1 + nodes;
     const int64_t near = (span + kBlk - 1) / kBlk + 1 + (sinks + kBlk - 1) / kBlk;
     most = near < all ? (int)near : all;
   }
-  // enough workgroups for two rounds of the chip (512 slots), a split no shorter than two
-  // blocks a wave
-  const int64_t wgs = (int64_t)c.kv * p.tiles * k.batch;
-  int64_t want = (1024 + wgs - 1) / wgs;
-  if (want > kMaxSplits) want = kMaxSplits;
-  int blocks = (int)((most + want - 1) / want);
-  if (blocks < 2 * kStreamWaves) blocks = 2 * kStreamWaves;
-  p.splits = (most + blocks - 1) / blocks;
-  p.blocks = blocks;
+  // The number of splits whose estimate is least, in units of one block's time: rounds of
+  // the chip's slots x (a split's blocks + what starting and ending a workgroup costs), and the join.
+  const int64_t wgs = (int64_t)c.kv * p.tiles * k.batch, slots = p.waves == 8 ? 256 : 512;
+  const int unit = stream ? p.waves : 1;  // blocks that a workgroup takes at a time
+  double best = 1e30;
+  p.splits = 1;
+  p.blocks = most;
+  for (int s = 1; s <= kMaxSplits && (s == 1 || (most + s - 1) / s >= 2 * unit); ++s) {
+    const int blocks = ((most + s - 1) / s + unit - 1) / unit * unit;
+    const int n = (most + blocks - 1) / blocks;
+    const double rounds = (double)((wgs * n + slots - 1) / slots);
+    const double cost = rounds * (blocks / unit + 6.0) + (n > 1 ? 8.0 + 0.1 * n : 0.0);
+    if (cost < best * 0.98) {
+      best = cost;
+      p.splits = n;
+      p.blocks = blocks;
+    }
+  }
   return p;
 }
 
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s) {
-  hipError_t e = a.dtype == DT_F32    ? launch_stream<DT_F32>(a, p, s)
+  hipError_t e = !p.stream ? launch_attend_tile(a, p, s)
+                 : a.dtype == DT_F32  ? launch_stream<DT_F32>(a, p, s)
                  : a.dtype == DT_BF16 ? launch_stream<DT_BF16>(a, p, s)
                                       : launch_stream<DT_F8>(a, p, s);
   if (e != hipSuccess || p.splits == 1) return e;

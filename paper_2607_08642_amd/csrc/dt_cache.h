@@ -68,6 +68,11 @@ inline ChunkView chunk_view(const dt_chunk &c) {
   return ChunkView{c.batch, c.rows, c.max_chunk, c.max_len, c.table_width, c.starts, c.lens, c.table};
 }
 
+// An index that is the same for the whole wave, read through the scalar cache.
+__device__ __forceinline__ int32_t scalar_at(const int32_t *p, int64_t i) {
+  return reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
 // A sequence's rows and tokens, kept within the tensors whatever starts and lens hold.
 struct Seq {
   int row0, n;  // rows [row0, row0 + n)
@@ -76,7 +81,7 @@ struct Seq {
 };
 __device__ inline Seq seq_of(const ChunkView &c, int page_shift, int b) {
   Seq s;
-  const int a = c.starts[b], e = c.starts[b + 1], len = c.lens[b];
+  const int a = scalar_at(c.starts, b), e = scalar_at(c.starts, b + 1), len = scalar_at(c.lens, b);
   s.row0 = min(max(a, 0), c.rows);
   s.n = min(max(e, s.row0), c.rows) - s.row0;
   s.base = min(max(len, 0), 1 << 30) - s.n;
@@ -118,10 +123,11 @@ struct AttendArgs {
   int splits, split_blocks;
 };
 
-// How a call is cut up: tiles of `rows` (query, head) rows of a kv head, the key blocks
-// of a tile dealt to `splits` workgroups of `blocks` blocks each.
+// How a call is cut up: tiles of tile_rows (query, head) rows of a kv head, the key blocks
+// of a tile dealt to `splits` workgroups of `waves` waves, `blocks` blocks each.
 struct AttendPlan {
-  int tile_rows, tiles, splits, blocks;
+  bool stream;  // each wave its own blocks (stream_kernel), not all of them the same (tile_kernel)
+  int waves, tile_rows, tiles, splits, blocks;
 };
 AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int heads, int window, int sinks, int nodes);
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s);

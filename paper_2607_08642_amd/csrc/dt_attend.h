@@ -101,6 +101,25 @@ __device__ __forceinline__ void tree_words(const AttendArgs &a, const Tile &t, i
   }
 }
 
+// Where a tile's blocks lie.
+struct Pages {
+  const char *base;  // of the kv head in page 0
+  const int32_t *table;
+  int64_t page_bytes;
+  int pages, shift;
+  __device__ __forceinline__ Pages(const AttendArgs &a, int b, int head)
+      : base(a.cache.base + head * a.cache.head_bytes), table(a.chunk.table + (int64_t)b * a.chunk.width),
+        page_bytes(a.cache.page_bytes), pages(a.cache.pages), shift(a.cache.page_shift) {}
+  // page of a block; out of range: -1
+  __device__ __forceinline__ int of(int block) const {
+    const int p = scalar_at(table, block * kBlk >> shift);
+    return (uint32_t)p < (uint32_t)pages ? p : -1;
+  }
+  // its head page (-1: page 0, whose tokens then count as unseen), and the block's first token in it
+  __device__ __forceinline__ const char *at(int page) const { return base + (int64_t)max(page, 0) * page_bytes; }
+  __device__ __forceinline__ int token(int block) const { return block * kBlk & ((1 << shift) - 1); }
+};
+
 // A lane's row and what it sees.
 struct Row {
   int r, i;            // (rows past the last repeat it)
@@ -146,11 +165,22 @@ __device__ __forceinline__ Row row_of(const AttendArgs &a, const Tile &t, int b,
   }
   return w;
 }
-__device__ __forceinline__ bool sees_all(const AttendArgs &a, const Row &w, int k0) {
-  return k0 + kBlk - 1 <= w.min_hi && (k0 > w.max_lo || (a.window > 0 && k0 + kBlk <= a.sinks));
-}
 __device__ __forceinline__ bool sees_none(const AttendArgs &a, const Row &w, int k0) {
   return k0 > w.reach || (k0 + kBlk - 1 <= w.min_lo && k0 >= a.sinks && k0 + kBlk <= w.tree_from);
+}
+// The end of the run of blocks from iteration `it` on that all rows see whole (`it`: none).
+__device__ __forceinline__ int full_end(const AttendArgs &a, const Tile &t, const Row &w, int it) {
+  const int blocks = max(w.min_hi + 1, 0) / kBlk;  // (those before it lie below every row's bound)
+  const int block = t.block(it);
+  int end;
+  if (block * kBlk > w.max_lo)
+    end = blocks;
+  else if (a.window > 0 && block * kBlk + kBlk <= a.sinks)
+    end = min(blocks, a.sinks / kBlk);
+  else
+    return it;
+  if (it < t.nsb) end = min(end, t.nsb);  // (then a gap follows)
+  return max(it, it + end - block);
 }
 // bit j: the lane's row sees token j of block k0
 __device__ __forceinline__ uint32_t seen_word(const AttendArgs &a, const Tile &t, const Row &w, int k0) {
@@ -215,12 +245,6 @@ __device__ __forceinline__ bf16x8 pack_p(const float (&p)[16], int s) {
   f32x8 v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = p[8 * s + i];
-  return __builtin_convertvector(v, bf16x8);
-}
-__device__ __forceinline__ bf16x8 pack_seen(uint32_t seen, int s) {  // 1 where a token is seen
-  f32x8 v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = seen >> reg_token(8 * s + i) & 1 ? 1.0f : 0.0f;
   return __builtin_convertvector(v, bf16x8);
 }
 // A word of values: all bits of its non-finite elements (`one` masked by them: 1 in their places).
@@ -343,102 +367,138 @@ __device__ __forceinline__ f32x16 scores(const char *keys, const char *exps, con
   return s;
 }
 
-// O^T += V^T P^T of a block: `vals` in LDS in the cache's order (DT_F8: `exps` their 32
-// exponents, which go to the probabilities: a product with a power of two, exact).
-// MASKED: non-finite values that not all rows see make NaN (of those components) of the rows
-// that do and are 0 for the others.
-template <int DT, int D, bool MASKED>
-__device__ __forceinline__ void add_values(const char *vals, const char *exps, float (&p)[16], uint32_t seen, int lane,
-                                           f32x16 (&o)[D / 32]) {
-  constexpr int T = D / 32, S = DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1;  // 16-byte pieces of a lane's tokens
-  const int h = lane >> 5, l32 = lane & 31;
-  const char *vp = vals + (h * D + l32) * 16;
-  auto piece = [&](int s, int t) { return lds16(vp + (2 * s * D + 32 * t) * 16); };
-  bf16x8 pf[2];
-  if constexpr (DT == DT_F8) {
+// A block's values in a lane's registers, in the cache's order: piece (s, t) holds element
+// 32 t + (lane & 31) of 4, 8 or 16 tokens.
+template <int DT, int D>
+struct VRegs {
+  static constexpr int S = DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1, T = D / 32;
+  u32x4 v[T][S];
+};
+template <int DT, int D>
+__device__ __forceinline__ const char *v_at(const char *vals, int s, int t, int lane) {
+  return vals + ((lane >> 5) * D + (lane & 31)) * 16 + (2 * s * D + 32 * t) * 16;
+}
+// The probabilities as the operand of those products (DT_F8: times the tokens' powers of two, `exps`
+// in LDS: exact).
+template <int DT, bool MASKED>
+struct POperand {
+  bf16x8 f[2];
+  __device__ __forceinline__ POperand(float (&p)[16], const char *exps, uint32_t seen, int h) {
+    if constexpr (DT == DT_F8) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const uint32_t w = *reinterpret_cast<const uint32_t *>(exps + 8 * t + 4 * h);
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(exps + 8 * t + 4 * h);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float e = __uint_as_float((j == 3 ? w >> 1 : w << (23 - 8 * j)) & 0x7f800000u);
-        p[4 * t + j] = MASKED && !(seen >> reg_token(4 * t + j) & 1) ? 0.0f : p[4 * t + j] * e;
-      }
-    }
-  }
-  if constexpr (DT != DT_F32) {
-    pf[0] = pack_p(p, 0);
-    pf[1] = pack_p(p, 1);
-  }
-  // the products of one d tile with pieces v
-  auto products = [&](const u32x4 (&v)[S], f32x16 acc) {
-    if constexpr (DT == DT_F32) {
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc = mfma(__uint_as_float(v[s][j]), p[4 * s + j], acc);
-    } else if constexpr (DT == DT_BF16) {
-      acc = mfma(as_bf16x8(v[0]), pf[0], acc);
-      acc = mfma(as_bf16x8(v[1]), pf[1], acc);
-    } else {
-      acc = mfma(widen8(v[0][0], v[0][1], 1.0f), pf[0], acc);
-      acc = mfma(widen8(v[0][2], v[0][3], 1.0f), pf[1], acc);
-    }
-    return acc;
-  };
-  if constexpr (MASKED) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int n = 0; n < S * T; ++n) {
-      const u32x4 v = piece(n / T, n % T);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= bad_bits<DT>(v[i]);
-      if (n % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight pieces at a time: registers)
-    }
-    const bool any = __ballot(bad != 0) != 0;
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      u32x4 v[S];
-#pragma unroll
-      for (int s = 0; s < S; ++s) v[s] = piece(s, t);
-      if (any) {
-        u32x4 one[S];
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t x = bad_bits<DT>(v[s][i]);
-            one[s][i] = x & kOnes<DT>;
-            v[s][i] &= ~x;
-          }
-        f32x16 hit = zero16();
-        if constexpr (DT == DT_F32) {
-#pragma unroll
-          for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              hit = mfma(__uint_as_float(one[s][j]), seen >> reg_token(4 * s + j) & 1 ? 1.0f : 0.0f, hit);
-        } else if constexpr (DT == DT_BF16) {
-          hit = mfma(as_bf16x8(one[0]), pack_seen(seen, 0), hit);
-          hit = mfma(as_bf16x8(one[1]), pack_seen(seen, 1), hit);
-        } else {
-          hit = mfma(widen8(one[0][0], one[0][1], 1.0f), pack_seen(seen, 0), hit);
-          hit = mfma(widen8(one[0][2], one[0][3], 1.0f), pack_seen(seen, 1), hit);
+        for (int j = 0; j < 4; ++j) {
+          const float e = __uint_as_float((j == 3 ? w >> 1 : w << (23 - 8 * j)) & 0x7f800000u);
+          p[4 * t + j] = MASKED && !(seen >> reg_token(4 * t + j) & 1) ? 0.0f : p[4 * t + j] * e;
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[t][i];
       }
-      o[t] = products(v, o[t]);
-      __builtin_amdgcn_sched_barrier(0);  // (one d tile at a time: registers)
     }
+    f[0] = pack_p(p, 0);
+    f[1] = pack_p(p, 1);
+  }
+};
+template <bool MASKED>
+struct POperand<DT_F32, MASKED> {
+  float f[16];
+  __device__ __forceinline__ POperand(float (&p)[16], const char *, uint32_t, int) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = p[i];
+  }
+};
+// one d tile's pieces times 32 probabilities
+template <int DT, int S, class P>
+__device__ __forceinline__ f32x16 products(const u32x4 (&v)[S], const P &p, f32x16 acc) {
+  if constexpr (DT == DT_F32) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc = mfma(__uint_as_float(v[s][j]), p.f[4 * s + j], acc);
+  } else if constexpr (DT == DT_BF16) {
+    acc = mfma(as_bf16x8(v[0]), p.f[0], acc);
+    acc = mfma(as_bf16x8(v[1]), p.f[1], acc);
   } else {
+    acc = mfma(widen8(v[0][0], v[0][1], 1.0f), p.f[0], acc);
+    acc = mfma(widen8(v[0][2], v[0][3], 1.0f), p.f[1], acc);
+  }
+  return acc;
+}
+
+// A block that all rows see whole: keys and values in LDS (DT_F8: with their exponents).
+// between(): after the scores, before the values are needed.
+template <int DT, int D, class F>
+__device__ __forceinline__ void full_block(const char *keys, const char *vals, const char *exps, const QRegs<DT, D> &q,
+                                           float c, int lane, float &m, float &l, f32x16 (&o)[D / 32],
+                                           const F &between) {
+  constexpr int T = D / 32, S = VRegs<DT, D>::S;
+  const f32x16 s = scores<DT, D>(keys, exps, q, lane);
+  between();
+  // the values are asked for before the softmax where registers allow
+  constexpr bool kEarly = S * T <= 8;
+  VRegs<DT, D> r;
+  if (kEarly)
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      u32x4 v[S];
+    for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int s = 0; s < S; ++s) v[s] = piece(s, t);
-      o[t] = products(v, o[t]);
+      for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(vals, x, t, lane));
+  float p[16];
+  softmax_block<false>(s, 0, c, m, l, o, p);
+  const POperand<DT, false> pf(p, exps + 32, 0, lane >> 5);
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    if (!kEarly)
+#pragma unroll
+      for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(vals, x, t, lane));
+    o[t] = products<DT>(r.v[t], pf, o[t]);
+  }
+}
+
+// Any other block.  Non-finite values that not all rows see make NaN (of those components)
+// of the rows that do and are 0 for the others.
+template <int DT, int D, class F>
+__device__ __forceinline__ void masked_block(const char *keys, const char *vals, const char *exps,
+                                             const QRegs<DT, D> &q, uint32_t seen, float c, int lane, float &m,
+                                             float &l, f32x16 (&o)[D / 32], const F &between) {
+  constexpr int T = D / 32, S = VRegs<DT, D>::S;
+  const f32x16 sc = scores<DT, D>(keys, exps, q, lane);
+  between();
+  float p[16];
+  softmax_block<true>(sc, seen, c, m, l, o, p);
+  const POperand<DT, true> pf(p, exps + 32, seen, lane >> 5);
+  uint32_t bad = 0;
+#pragma unroll
+  for (int n = 0; n < S * T; ++n) {
+    const u32x4 v = lds16(v_at<DT, D>(vals, n / T, n % T, lane));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= bad_bits<DT>(v[i]);
+    if (n % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight pieces at a time: registers)
+  }
+  const bool any = __ballot(bad != 0) != 0;
+  float sf[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sf[i] = seen >> reg_token(i) & 1 ? 1.0f : 0.0f;
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    u32x4 v[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) v[s] = lds16(v_at<DT, D>(vals, s, t, lane));
+    if (any) {
+      u32x4 one[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = bad_bits<DT>(v[s][i]);
+          one[s][i] = x & kOnes<DT>;
+          v[s][i] &= ~x;
+        }
+      const f32x16 hit = products<DT>(one, POperand<DT == DT_F8 ? DT_BF16 : DT, false>(sf, nullptr, 0, 0), zero16());
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[t][i];
     }
+    o[t] = products<DT>(v, pf, o[t]);
+    __builtin_amdgcn_sched_barrier(0);  // (one d tile at a time: registers)
   }
 }
 

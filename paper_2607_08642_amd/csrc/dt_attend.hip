@@ -52,103 +52,96 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   QRegs<DT, D> q;
   load_q<DT, D>(a, t, w, head, h, DT == DT_F8, q);
 
-  // ---- the wave's blocks: copies into its ring
-  const int32_t *table = a.chunk.table + (int64_t)b * a.chunk.width;
-  const int shift = a.cache.page_shift;
-  auto page_of = [&](int it) { return it < it1 ? scalar_at(table, t.block(it) * kBlk >> shift) : 0; };
-  // head page of a block (out of range: page 0, whose tokens then count as unseen), token in it
-  auto place = [&](int it, int page, int *n) {
-    const int p = __builtin_amdgcn_readfirstlane(page);
-    *n = t.block(it) * kBlk & ((1 << shift) - 1);
-    return a.cache.base + (int64_t)((uint32_t)p < (uint32_t)a.cache.pages ? p : 0) * a.cache.page_bytes +
-           head * a.cache.head_bytes;
-  };
-  char *mine = ring + wave * (St::kLds / W);
-  auto keys = [&](int s) { return mine + s * (2 * St::kPart + St::kExps); };
-  auto copy_keys = [&](int it, int page, int s) {
-    int n;
-    const char *hp = place(it, page, &n);
-    if (DT == DT_F8)  // lanes 0-7 (mod 16): the keys' 32 exponents, 8-15: the values'
-      copy4(hp + a.cache.s_off + n + (lane & 7) * 4 + (lane & 8 ? 1 << shift : 0), keys(s) + 2 * St::kPart);
-    hp += (int64_t)n * D * ES + lane * 16;
-#pragma unroll
-    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, keys(s) + x * 1024);
-  };
-  auto copy_vals = [&](int it, int page, int s) {
-    int n;
-    const char *hp = place(it, page, &n);
-    hp += a.cache.v_off + (int64_t)n * D * ES + lane * 16;
-#pragma unroll
-    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, keys(s) + St::kPart + x * 1024);
-  };
-  constexpr int kK = St::kOps + (DT == DT_F8 ? 1 : 0), kV = St::kOps;
-  int it = it0 + wave;
-  int pages[NS + 1];  // of blocks it, it + W, ..
-#pragma unroll
-  for (int x = 0; x <= NS; ++x) pages[x] = page_of(it + x * W);
-#pragma unroll
-  for (int x = 0; x < NS; ++x)
-    if (it + x * W < it1) {
-      copy_keys(it + x * W, pages[x], x);
-      copy_vals(it + x * W, pages[x], x);
-    }
-
-  if (a.nodes > 0) {
-    tree_words(a, t, b, words, 64 * W);
-    __syncthreads();
-  }
   f32x16 o[T];
 #pragma unroll
   for (int n = 0; n < T; ++n) o[n] = zero16();
   float m = kFloor, l = 0.0f;
 
-  int slot = 0;
-  for (; it < it1; it += W) {
-    const int after = page_of(it + (NS + 1) * W), k0 = t.block(it) * kBlk;
-    // (all slots asked for: the block's keys are there when this many copies are not; else wait for all)
-    const bool steady = it + (NS - 1) * W < it1, more = it + NS * W < it1;
-    const bool skip = sees_none(a, w, k0), there = (uint32_t)pages[0] < (uint32_t)a.cache.pages;
-    const bool all = there && sees_all(a, w, k0);
-    const char *kp = keys(slot), *ex = kp + 2 * St::kPart;
-    if (steady)
+  // ---- the wave's blocks: copies into its ring
+  const Pages pages(a, b, head);
+  char *mine = ring + wave * (St::kLds / W);
+  constexpr int kSlot = 2 * St::kPart + St::kExps;
+  auto copy_keys = [&](int block, int page, char *slot) {
+    const char *hp = pages.at(page);
+    const int n = pages.token(block);
+    if (DT == DT_F8)  // lanes 0-7 (mod 16): the keys' 32 exponents, 8-15: the values'
+      copy4(hp + a.cache.s_off + n + (lane & 7) * 4 + (lane & 8 ? 1 << pages.shift : 0), slot + 2 * St::kPart);
+    hp += (int64_t)n * D * ES + lane * 16;
+#pragma unroll
+    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, slot + x * 1024);
+  };
+  auto copy_vals = [&](int block, int page, char *slot) {
+    const char *hp = pages.at(page) + a.cache.v_off + (int64_t)pages.token(block) * D * ES + lane * 16;
+#pragma unroll
+    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, slot + St::kPart + x * 1024);
+  };
+  constexpr int kK = St::kOps + (DT == DT_F8 ? 1 : 0), kV = St::kOps;
+  uint32_t there = 0;  // bit x: block (the last one asked for) - x W has a page
+  auto page_of = [&](int it) { return it < it1 ? pages.of(t.block(it)) : -1; };
+  int it = it0 + wave;
+#pragma unroll
+  for (int x = 0; x < NS; ++x) {
+    const int page = page_of(it + x * W);
+    if (it + x * W < it1) {
+      copy_keys(t.block(it + x * W), page, mine + x * kSlot);
+      copy_vals(t.block(it + x * W), page, mine + x * kSlot);
+    }
+    there = there << 1 | (page >= 0 ? 1u : 0u);
+  }
+  int page = page_of(it + NS * W);
+  if (a.nodes > 0) {
+    tree_words(a, t, b, words, 64 * W);
+    __syncthreads();
+  }
+
+  // One turn: the block's keys are there (every slot asked for: when the later copies are all
+  // that is on its way; else when nothing is); as they are done with, their place takes the
+  // keys of block it + NS W; the same with the values.
+  char *slot = mine;
+  auto turn = [&](auto block_step) {
+    const bool more = it + NS * W < it1;
+    const int ahead = it + NS * W < it1 ? t.block(it + NS * W) : 0;
+    if (it + (NS - 1) * W < it1)
       wait_copies<kV + (NS - 1) * (kK + kV)>();
     else
       wait_copies<0>();
-    f32x16 s;
-    if (!skip) s = scores<DT, D>(kp, ex, q, lane);
-    wait_copies<63>();  // (LDS reads done: the keys' place is free)
-    // (DT_F8: the exponents' place is not, the values' are still to be read; they come with
-    // the next block's keys, so those are asked for after the values)
-    if (DT != DT_F8 && more) copy_keys(it + NS * W, pages[NS], slot);
-    float p[16];
-    uint32_t seen = 0;
-    if (!skip) {
-      if (all) {
-        softmax_block<false>(s, 0, c, m, l, o, p);
-      } else {
-        seen = there ? seen_word(a, t, w, k0) >> (4 * h) : 0;
-        softmax_block<true>(s, seen, c, m, l, o, p);
-      }
-    }
-    if (steady && more)
-      wait_copies<(NS - 1) * (kK + kV) + (DT != DT_F8 ? kK : 0)>();
-    else
-      wait_copies<0>();
-    if (!skip) {
-      if (all)
-        add_values<DT, D, false>(kp + St::kPart, ex + 32, p, 0, lane, o);
+    auto between = [&]() {
+      wait_copies<63>();  // (LDS reads done)
+      // (DT_F8: the values' exponents come with the keys, so those wait until the values are done with)
+      if (DT != DT_F8 && more) copy_keys(ahead, page, slot);
+      if (more)
+        wait_copies<(NS - 1) * (kK + kV) + (DT != DT_F8 ? kK : 0)>();
       else
-        add_values<DT, D, true>(kp + St::kPart, ex + 32, p, seen, lane, o);
-    }
+        wait_copies<0>();
+    };
+    block_step(between);
     wait_copies<63>();
     if (more) {
-      if (DT == DT_F8) copy_keys(it + NS * W, pages[NS], slot);
-      copy_vals(it + NS * W, pages[NS], slot);
+      if (DT == DT_F8) copy_keys(ahead, page, slot);
+      copy_vals(ahead, page, slot);
     }
-#pragma unroll
-    for (int x = 0; x < NS; ++x) pages[x] = pages[x + 1];
-    pages[NS] = after;
-    slot = slot == NS - 1 ? 0 : slot + 1;
+    there = there << 1 | (page >= 0 ? 1u : 0u);
+    it += W;
+    page = page_of(it + NS * W);
+    slot = slot == mine + (NS - 1) * kSlot ? mine : slot + kSlot;
+  };
+  while (it < it1) {
+    // (a loop of its own for the blocks that every row sees whole: with the masks in it, the
+    // sums would move between two sets of registers in every turn)
+    const int full = min(full_end(a, t, w, it), it1);
+    while (it < full && there >> (NS - 1) & 1)
+      turn([&](const auto &between) __attribute__((always_inline)) {
+        full_block<DT, D>(slot, slot + St::kPart, slot + 2 * St::kPart, q, c, lane, m, l, o, between);
+      });
+    if (it >= it1) break;
+    turn([&](const auto &between) __attribute__((always_inline)) {
+      const int k0 = t.block(it) * kBlk;
+      if (sees_none(a, w, k0))
+        between();
+      else
+        masked_block<DT, D>(slot, slot + St::kPart, slot + 2 * St::kPart, q,
+                            there >> (NS - 1) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, between);
+    });
   }
 
   // ---- the waves' results meet, each scaled to the common maximum: upper half to lower half

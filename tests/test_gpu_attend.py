@@ -94,6 +94,16 @@ def test_window(dtype, window, sinks, shape):
     a.check(a.run(window=window, sinks=sinks), window=window, sinks=sinks)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv", [(2, 2), (4, 2), (12, 2)])
+@pytest.mark.parametrize("window,sinks", [(100, 96), (64, 64), (40, 33), (1, 64), (300, 32)])
+def test_window_of_long_chunks(dtype, heads, kv, window, sinks):
+    """Tiles of many queries, whose windows start in different blocks, before and behind the first tokens' end."""
+    print(f"[attend] window chunk {dtype} {heads}/{kv} {window}/{sinks}", flush=True)
+    a = Attend(dtype, [(400, 400), (530, 290)], heads, 32, kv, 64, seed=window)
+    a.check(a.run(window=window, sinks=sinks), window=window, sinks=sinks)
+
+
 def trees(sizes, N, seed):
     """A tree for each sequence (every third one of fewer nodes, padded): masks and depths."""
     import random

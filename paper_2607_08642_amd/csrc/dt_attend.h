@@ -110,13 +110,13 @@ struct Pages {
   __device__ __forceinline__ Pages(const AttendArgs &a, int b, int head)
       : base(a.cache.base + head * a.cache.head_bytes), table(a.chunk.table + (int64_t)b * a.chunk.width),
         page_bytes(a.cache.page_bytes), pages(a.cache.pages), shift(a.cache.page_shift) {}
-  // page of a block; out of range: -1
-  __device__ __forceinline__ int of(int block) const {
-    const int p = scalar_at(table, block * kBlk >> shift);
-    return (uint32_t)p < (uint32_t)pages ? p : -1;
+  // page of a block, as the table has it (looked at a turn later: the load takes its time)
+  __device__ __forceinline__ int of(int block) const { return scalar_at(table, block * kBlk >> shift); }
+  __device__ __forceinline__ bool there(int page) const { return (uint32_t)page < (uint32_t)pages; }
+  // its head page (out of range: page 0, whose tokens then count as unseen), and the block's first token in it
+  __device__ __forceinline__ const char *at(int page) const {
+    return base + (int64_t)(there(page) ? page : 0) * page_bytes;
   }
-  // its head page (-1: page 0, whose tokens then count as unseen), and the block's first token in it
-  __device__ __forceinline__ const char *at(int page) const { return base + (int64_t)max(page, 0) * page_bytes; }
   __device__ __forceinline__ int token(int block) const { return block * kBlk & ((1 << shift) - 1); }
 };
 
@@ -452,6 +452,55 @@ __device__ __forceinline__ void full_block(const char *keys, const char *vals, c
       for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(vals, x, t, lane));
     o[t] = products<DT>(r.v[t], pf, o[t]);
   }
+}
+
+// Two blocks that all rows see whole, at slots `one` and `two`: one maximum for both, and the
+// second's exponentials beside the first's products.
+template <int DT, int D>
+__device__ __forceinline__ void full_pair(const char *one, const char *two, const QRegs<DT, D> &q, float c, int lane,
+                                          float &m, float &l, f32x16 (&o)[D / 32]) {
+  constexpr int T = D / 32, S = VRegs<DT, D>::S, kPart = kBlk * D * (DT == DT_F8 ? 1 : 2);
+  const f32x16 s[2] = {scores<DT, D>(one, one + 2 * kPart, q, lane), scores<DT, D>(two, two + 2 * kPart, q, lane)};
+  VRegs<DT, D> r;
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(one + kPart, x, t, lane));
+  float top[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    top[u] = max3(s[u][0], s[u][1], s[u][2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) top[u] = max3(top[u], s[u][i], s[u][i + 1]);
+  }
+  const float2 th = halves(max3(max2(top[0], top[1]), s[0][15], s[1][15]));
+  const float now = max2(th.x, th.y) * c;
+  if (__ballot(now > m + kSlack)) {
+    const float to = now > m ? now : m, f = __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    l *= f;
+    rescale(o, f);
+  }
+  float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], c, -m));
+      sum[i & 1] += p[i];
+    }
+    const char *at = u ? two : one;
+    const POperand<DT, false> pf(p, at + 2 * kPart + 32, 0, lane >> 5);
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      if (u)
+#pragma unroll
+        for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(at + kPart, x, t, lane));
+      o[t] = products<DT>(r.v[t], pf, o[t]);
+    }
+  }
+  l += sum[0] + sum[1];
 }
 
 // Any other block.  Non-finite values that not all rows see make NaN (of those components)

@@ -86,7 +86,7 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
       copy_keys(t.block(it + x * W), page, mine + x * kSlot);
       copy_vals(t.block(it + x * W), page, mine + x * kSlot);
     }
-    there = there << 1 | (page >= 0 ? 1u : 0u);
+    there = there << 1 | (pages.there(page) ? 1u : 0u);
   }
   int page = page_of(it + NS * W);
   if (a.nodes > 0) {
@@ -120,7 +120,7 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
       if (DT == DT_F8) copy_keys(ahead, page, slot);
       copy_vals(ahead, page, slot);
     }
-    there = there << 1 | (page >= 0 ? 1u : 0u);
+    there = there << 1 | (pages.there(page) ? 1u : 0u);
     it += W;
     page = page_of(it + NS * W);
     slot = slot == mine + (NS - 1) * kSlot ? mine : slot + kSlot;

@@ -10,8 +10,6 @@ namespace dt {
 namespace {
 using namespace att;
 
-constexpr int kCopies = 3;  // blocks on their way from memory
-
 // grid: kv head (fastest), tile (the last rows, which see most, first), split; sequence
 template <int DT, int D, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((
@@ -20,7 +18,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
                                                                                                      int tile_rows) {
   constexpr int T = D / 32, ES = DT == DT_F8 ? 1 : 2, kRows = 32 * NW, kPart = kBlk * D * ES;
   constexpr int kSlot = 2 * kPart + (DT == DT_F8 ? 256 : 0);  // keys, values, exponents
-  __shared__ __align__(16) char ring[(kCopies + 1) * kSlot];
+  // blocks of a turn, turns ahead that blocks are asked for
+  constexpr int B = NW == 8 && D <= 128 ? 2 : 1, kAhead = B == 2 ? 2 : 3, kSlots = (kAhead + 1) * B;
+  __shared__ __align__(16) char ring[kSlots * kSlot];
   __shared__ uint32_t words[kRows * kTreeWords];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
@@ -62,30 +62,35 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     }
   };
   uint32_t there = 0;  // bit x: block (the last one asked for) - x has a page
-  auto ask = [&](int it, int page, char *slot) {
-    if (it < it1) copy(t.block(it), page, slot);
-    there = there << 1 | (page >= 0 ? 1u : 0u);
+  int it = it0, last = it0 - 1;
+  auto ask = [&](int page, char *slot) {
+    ++last;
+    if (last < it1) copy(t.block(last), page, slot);
+    there = there << 1 | (pages.there(page) ? 1u : 0u);
   };
   auto page_of = [&](int it) { return it < it1 ? pages.of(t.block(it)) : -1; };
 #pragma unroll
-  for (int x = 0; x < kCopies; ++x) ask(it0 + x, page_of(it0 + x), ring + x * kSlot);
-  int page = page_of(it0 + kCopies), it = it0;
-  char *slot = ring, *before = ring + kCopies * kSlot;  // of the present block and of the last
-  // The present block is there (near the end: all that was asked for), for every wave, and every
-  // wave has done with the last one, whose slot takes the next.
+  for (int x = 0; x < kAhead * B; ++x) ask(page_of(it0 + x), ring + x * kSlot);
+  int page[B];
+#pragma unroll
+  for (int x = 0; x < B; ++x) page[x] = page_of(it0 + kAhead * B + x);
+  char *slot = ring, *before = ring + kAhead * B * kSlot;  // of the present block and of the last
   auto turn = [&]() {
-    if (it + kCopies <= it1)
-      wait_copies<(kCopies - 1) * kEach>();
+    if (B > 1 && (it - it0) % B) return;
+    if (it + kAhead * B <= it1)
+      wait_copies<(kAhead - 1) * B * kEach>();
     else
       wait_copies<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    ask(it + kCopies, page, before);
-    page = page_of(it + kCopies + 1);
+#pragma unroll
+    for (int x = 0; x < B; ++x) ask(page[x], before + x * kSlot);
+#pragma unroll
+    for (int x = 0; x < B; ++x) page[x] = page_of(last + 1 + x);
+    before = slot;
   };
   auto next = [&]() {
-    before = slot;
-    slot = slot == ring + kCopies * kSlot ? ring : slot + kSlot;
+    slot = slot == ring + (kSlots - 1) * kSlot ? ring : slot + kSlot;
     ++it;
   };
   auto nothing = [] {};
@@ -95,7 +100,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     // (a loop of its own for the blocks that every row sees whole: with the masks in it, the
     // sums would move between two sets of registers in every turn)
     const int full = min(full_end(a, t, w, it), it1);
-    for (; it < full && there >> (kCopies - 1) & 1; next()) {
+    if constexpr (B == 2)
+      while ((it - it0) % 2 == 0 && it + 1 < full && (there >> (last - it - 1) & 3) == 3) {
+        turn();
+        full_pair<DT, D>(slot, slot + kSlot, q, c, lane, m, l, o);
+        next();
+        next();
+      }
+    for (; it < full && there >> (last - it) & 1; next()) {
       turn();
       full_block<DT, D>(slot, slot + kPart, slot + 2 * kPart, q, c, lane, m, l, o, nothing);
     }
@@ -104,7 +116,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     const int k0 = t.block(it) * kBlk;
     if (!sees_none(a, w, k0))
       masked_block<DT, D>(slot, slot + kPart, slot + 2 * kPart, q,
-                          there >> kCopies & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
+                          there >> (last - it) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
     next();
   }
   if (idle) return;

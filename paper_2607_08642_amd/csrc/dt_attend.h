@@ -551,58 +551,60 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
   }
 }
 
-// A wave's 32 finished rows: the result, or one split's part of it.
+// Four elements of the result at element offset `at`.
+template <int DT>
+__device__ __forceinline__ void store4(const AttendArgs &a, int64_t at, float x, float y, float z, float w) {
+  if (DT == DT_F32) {
+    float *p = reinterpret_cast<float *>(a.out.p) + at;
+    if (a.out.vec)
+      *reinterpret_cast<f32x4 *>(p) = f32x4{x, y, z, w};
+    else
+      p[0] = x, p[1] = y, p[2] = z, p[3] = w;
+  } else {
+    __bf16 *p = reinterpret_cast<__bf16 *>(a.out.p) + at;
+    const bf16x2 u = {(__bf16)x, (__bf16)y}, v = {(__bf16)z, (__bf16)w};
+    if (a.out.vec) {
+      uint2 q;
+      __builtin_memcpy(&q.x, &u, 4);
+      __builtin_memcpy(&q.y, &v, 4);
+      *reinterpret_cast<uint2 *>(p) = q;
+    } else {
+      p[0] = u[0], p[1] = u[1], p[2] = v[0], p[3] = v[1];
+    }
+  }
+}
+
+// A wave's 32 finished rows: the result, or one split's part of it (the first split notes how many
+// there are; one alone writes the result).
 template <int DT, int D>
-__device__ __forceinline__ void write_rows(const AttendArgs &a, const Tile &t, const Row &w, int head, int split, bool direct,
-                                  bool valid, int h, const f32x16 (&o)[D / 32], float m, float l) {
+__device__ __forceinline__ void write_rows(const AttendArgs &a, const Tile &t, const Row &w, int head, int split,
+                                           int active, bool valid, int h, const f32x16 (&o)[D / 32], float m, float l) {
   if (!valid) return;
   const int hq = head * a.group + w.r % a.group;
-  const int64_t row = t.q.row0 + w.i;
-  if (!direct) {
-    const int64_t at = (row * a.heads + hq) * a.splits + split;
-    if (h == 0) a.part_ml[at] = make_float2(m, l);
-    float *p = a.part + at * D;
+  const int64_t row = t.q.row0 + w.i, x = row * a.heads + hq;
+  if (a.splits > 1) {
+    float2 *ml = a.part_ml + x * (a.splits + 1);
+    if (split == 0 && h == 0) ml[a.splits] = make_float2((float)active, 0.0f);
+    if (active > 1) {
+      if (h == 0) ml[split] = make_float2(m, l);
+      float *p = a.part + (x * a.splits + split) * D;
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n)
+      for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        *reinterpret_cast<f32x4 *>(p + 32 * n + 8 * x + 4 * h) =
-            f32x4{o[n][4 * x], o[n][4 * x + 1], o[n][4 * x + 2], o[n][4 * x + 3]};
-    return;
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4 *>(p + 32 * n + 8 * i + 4 * h) =
+              f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
+      return;
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (l = 0: the row saw nothing, o is 0)
   const int64_t at = row * a.out.row + (int64_t)hq * a.out.head;
 #pragma unroll
   for (int n = 0; n < D / 32; ++n)
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int d = 32 * n + 8 * x + 4 * h;
-      float y[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = o[n][4 * x + j] * inv;
-      if (DT == DT_F32) {
-        float *p = reinterpret_cast<float *>(a.out.p) + at + d;
-        if (a.out.vec)
-          *reinterpret_cast<f32x4 *>(p) = f32x4{y[0], y[1], y[2], y[3]};
-        else
-#pragma unroll
-          for (int j = 0; j < 4; ++j) p[j] = y[j];
-      } else {
-        __bf16 *p = reinterpret_cast<__bf16 *>(a.out.p) + at + d;
-        const bf16x2 u = {(__bf16)y[0], (__bf16)y[1]}, v = {(__bf16)y[2], (__bf16)y[3]};
-        if (a.out.vec) {
-          uint2 z;
-          __builtin_memcpy(&z.x, &u, 4);
-          __builtin_memcpy(&z.y, &v, 4);
-          *reinterpret_cast<uint2 *>(p) = z;
-        } else {
-          p[0] = u[0];
-          p[1] = u[1];
-          p[2] = v[0];
-          p[3] = v[1];
-        }
-      }
-    }
+    for (int i = 0; i < 4; ++i)
+      store4<DT>(a, at + 32 * n + 8 * i + 4 * h, o[n][4 * i] * inv, o[n][4 * i + 1] * inv, o[n][4 * i + 2] * inv,
+                 o[n][4 * i + 3] * inv);
 }
 
 }  // namespace att

@@ -6,6 +6,8 @@
 // which it fills by copies from memory that pass no registers: keys of block n + slots are
 // asked for when those of block n have been used, and the values after them.  No wave waits
 // for another until their partial results meet at the end.
+#include <math.h>
+
 #include "dt_attend.h"
 
 namespace dt {
@@ -183,41 +185,39 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
     __syncthreads();
   }
   if (wave > 0) return;
-  write_rows<DT, D>(a, t, w, head, split, active == 1, t.r0 + l32 < t.rows, h, o, top, l);
+  write_rows<DT, D>(a, t, w, head, split, active, t.r0 + l32 < t.rows, h, o, top, l);
 }
 
-// One wave per (query, head): the splits' parts scaled to their common maximum and summed
-// in order.  Rows of a tile with one split were written by it.
+// The splits' parts scaled to their common maximum and summed in order: D / 4 lanes (of a 16-, 32- or
+// 64-lane group) a (row, head), four elements each.  How many splits a row has stands with
+// its sums (1: the tile's one split has written the result), so nothing of the call's
+// geometry is worked out again.
 template <int DT>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int tile_rows) {
-  const int lane = threadIdx.x & 63, D = a.cache.D, b = blockIdx.y;
-  const int x = blockIdx.x * 4 + (threadIdx.x >> 6);  // query * heads + head
-  const int i = x / a.heads, hq = x - i * a.heads;
-  const int r = i * a.group + hq % a.group;
-  Tile t;
-  if (!tile_of(a, b, r / tile_rows * tile_rows, tile_rows, &t) || r >= t.rows) return;
-  const int active = active_splits(a, t);
-  if (active == 1) return;
-  const int64_t row = t.q.row0 + i, at = (row * a.heads + hq) * a.splits;
-  const float2 p = lane < active ? a.part_ml[at + lane] : make_float2(kFloor, 0.0f);
-  float top = p.x;
-  for (int o = 1; o < 64; o <<= 1) top = max2(top, __shfl_xor(top, o));
-  const float f = __builtin_amdgcn_exp2f(p.x - top);
-  float l = p.y * f;
-  for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const float *part = a.part + at * D;
-  for (int d = lane; d < D; d += 64) {
-    float y = 0.0f;
-#pragma unroll 8
-    for (int s = 0; s < active; ++s) y += part[(int64_t)s * D + d] * __shfl(f, s);
-    y *= inv;
-    const int64_t o = row * a.out.row + (int64_t)hq * a.out.head + d;
-    if (DT == DT_F32)
-      reinterpret_cast<float *>(a.out.p)[o] = y;
-    else
-      reinterpret_cast<__bf16 *>(a.out.p)[o] = (__bf16)y;
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int group_lanes) {
+  const int D = a.cache.D, first = scalar_at(a.chunk.starts, 0), end = scalar_at(a.chunk.starts, a.chunk.batch);
+  const int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) / group_lanes;  // row * heads + head
+  const int row = (int)(x / a.heads), d = threadIdx.x % group_lanes * 4;
+  if (row >= a.chunk.rows || row < first || row >= end || d >= D) return;
+  const float2 *ml = a.part_ml + x * (a.splits + 1);
+  const int n = min((int)ml[a.splits].x, a.splits);
+  if (n <= 1) return;
+  float top = ml[0].x;
+  for (int s = 1; s < n; ++s) top = max2(top, ml[s].x);
+  const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + x * a.splits * D + d);
+  f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const f32x4 v = part[(int64_t)s * D / 4];
+    const float2 p = ml[s];
+    const float f = __builtin_amdgcn_exp2f(p.x - top);
+    l += p.y * f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(v[j], f, y[j]);
   }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  store4<DT>(a, row * a.out.row + (x - (int64_t)row * a.heads) * a.out.head + d, y[0] * inv, y[1] * inv, y[2] * inv,
+             y[3] * inv);
 }
 
 template <int DT>
@@ -254,9 +254,12 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
     const int64_t near = (span + kBlk - 1) / kBlk + 1 + (sinks + kBlk - 1) / kBlk;
     most = near < all ? (int)near : all;
   }
-  // The number of splits whose estimate is least, in units of one block's time: rounds of
-  // the chip's slots x (a split's blocks + what starting and ending a workgroup costs), and the join.
-  const int64_t wgs = (int64_t)c.kv * p.tiles * k.batch, slots = p.waves == 8 ? 256 : 512;
+  // The number of splits whose estimate is least, in units of one block's time: what a
+  // workgroup takes (its blocks, and starting and ending), times the rounds that the chip needs for
+  // all, and the join.  Of a batch the lengths are known on the device only: its workgroups are
+  // taken to have half the blocks of the longest on average, and to fill gaps.
+  const int64_t wgs = (int64_t)c.kv * p.tiles * k.batch;
+  const double slots = !stream && p.waves == 4 && c.D <= 128 ? 512 : 256;
   const int unit = stream ? p.waves : 1;  // blocks that a workgroup takes at a time
   double best = 1e30;
   p.splits = 1;
@@ -264,8 +267,12 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
   for (int s = 1; s <= kMaxSplits && (s == 1 || (most + s - 1) / s >= 2 * unit); ++s) {
     const int blocks = ((most + s - 1) / s + unit - 1) / unit * unit;
     const int n = (most + blocks - 1) / blocks;
-    const double rounds = (double)((wgs * n + slots - 1) / slots);
-    const double cost = rounds * (blocks / unit + 6.0) + (n > 1 ? 8.0 + 0.1 * n : 0.0);
+    double rounds = wgs * n / slots;
+    if (k.batch == 1)
+      rounds = ceil(rounds);
+    else
+      rounds = rounds > 2.0 ? rounds / 2 : 1.0;
+    const double cost = rounds * (blocks / unit + 5.0) + (n > 1 ? 4.0 + 0.2 * n : 0.0);
     if (cost < best * 0.98) {
       best = cost;
       p.splits = n;
@@ -281,8 +288,9 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s
                  : a.dtype == DT_BF16 ? launch_stream<DT_BF16>(a, p, s)
                                       : launch_stream<DT_F8>(a, p, s);
   if (e != hipSuccess || p.splits == 1) return e;
-  const dim3 grid(((int64_t)a.chunk.max_chunk * a.heads + 3) / 4, a.chunk.batch);
-  (a.dtype == DT_F32 ? join_kernel<DT_F32> : join_kernel<DT_BF16>)<<<grid, 256, 0, s>>>(a, p.tile_rows);
+  const int lanes = a.cache.D <= 64 ? 16 : a.cache.D <= 128 ? 32 : 64;
+  const int64_t groups = ((int64_t)a.chunk.rows * a.heads * lanes + 255) / 256;
+  (a.dtype == DT_F32 ? join_kernel<DT_F32> : join_kernel<DT_BF16>)<<<(unsigned)groups, 256, 0, s>>>(a, lanes);
   return hipGetLastError();
 }
 

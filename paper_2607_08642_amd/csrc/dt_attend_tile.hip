@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
   }
   if (idle) return;
   const float2 lh = halves(l);
-  write_rows<DT, D>(a, t, w, head, split, active == 1, r < t.rows, h, o, m, lh.x + lh.y);
+  write_rows<DT, D>(a, t, w, head, split, active, r < t.rows, h, o, m, lh.x + lh.y);
 }
 
 template <int DT, int NW>

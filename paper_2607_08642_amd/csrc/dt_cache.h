@@ -119,7 +119,7 @@ struct AttendArgs {
   const uint8_t *mask;
   const int32_t *depth;
   float *part;     // [rows * heads][splits][D] partial sums
-  float2 *part_ml;  // [rows * heads][splits] maximum and sum
+  float2 *part_ml;  // [rows * heads][splits + 1] maximum and sum; how many splits there are
   int splits, split_blocks;
 };
 

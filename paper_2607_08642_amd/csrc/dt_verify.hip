@@ -106,10 +106,10 @@ struct AttendWs {
 AttendWs attend_ws(const AttendPlan &p, const dt_chunk *k, int heads, int D) {
   AttendWs w{};
   if (p.splits == 1) return w;
-  const size_t rows = (size_t)k->rows * heads * p.splits;
+  const size_t rows = (size_t)k->rows * heads;
   w.ml = 0;
-  w.part = align_up(rows * sizeof(float2), 256);
-  w.bytes = w.part + align_up(rows * D * sizeof(float), 256);
+  w.part = align_up(rows * (p.splits + 1) * sizeof(float2), 256);
+  w.bytes = w.part + align_up(rows * p.splits * D * sizeof(float), 256);
   return w;
 }
 

@@ -101,23 +101,48 @@ __device__ __forceinline__ void tree_words(const AttendArgs &a, const Tile &t, i
   }
 }
 
-// Where a tile's blocks lie.
-struct Pages {
+// A walk over a tile's blocks from iteration `it` on, in steps of STEP: where the present one lies.
+// Blocks of one page follow each other, so the table is looked at once a page, and a page ahead
+// (the scalar load takes its time).
+template <int STEP>
+struct Walk {
   const char *base;  // of the kv head in page 0
   const int32_t *table;
   int64_t page_bytes;
-  int pages, shift;
-  __device__ __forceinline__ Pages(const AttendArgs &a, int b, int head)
+  int pages, shift, it, end;
+  int left;         // blocks of the walk left in the page
+  int next_page;    // of the first block after those, as the table has it
+  bool there;       // the page is in range (else: page 0, whose tokens then count as unseen)
+  const char *keys;  // the block's keys (its values v_off behind them)
+  const char *exps;  // DT_F8: its keys' exponents
+  __device__ __forceinline__ Walk(const AttendArgs &a, const Tile &t, int b, int head, int from, int to)
       : base(a.cache.base + head * a.cache.head_bytes), table(a.chunk.table + (int64_t)b * a.chunk.width),
-        page_bytes(a.cache.page_bytes), pages(a.cache.pages), shift(a.cache.page_shift) {}
-  // page of a block, as the table has it (looked at a turn later: the load takes its time)
-  __device__ __forceinline__ int of(int block) const { return scalar_at(table, block * kBlk >> shift); }
-  __device__ __forceinline__ bool there(int page) const { return (uint32_t)page < (uint32_t)pages; }
-  // its head page (out of range: page 0, whose tokens then count as unseen), and the block's first token in it
-  __device__ __forceinline__ const char *at(int page) const {
-    return base + (int64_t)(there(page) ? page : 0) * page_bytes;
+        page_bytes(a.cache.page_bytes), pages(a.cache.pages), shift(a.cache.page_shift), it(from), end(to), left(0),
+        next_page(0), there(false), keys(base), exps(base) {
+    look(t, it);
   }
-  __device__ __forceinline__ int token(int block) const { return block * kBlk & ((1 << shift) - 1); }
+  __device__ __forceinline__ void look(const Tile &t, int at) {
+    if (at < end) next_page = scalar_at(table, t.block(at) * kBlk >> shift);
+  }
+  __device__ __forceinline__ bool done() const { return it >= end; }
+  // the present block (not done): keys, exps and there hold for it
+  __device__ __forceinline__ void open(const AttendArgs &a, const Tile &t, int block_bytes) {
+    if (left > 0) return;
+    const int block = t.block(it), n = block * kBlk & ((1 << shift) - 1);
+    there = (uint32_t)next_page < (uint32_t)pages;
+    const char *page = base + (int64_t)(there ? next_page : 0) * page_bytes;
+    keys = page + (int64_t)(n / kBlk) * block_bytes;
+    exps = page + a.cache.s_off + n;
+    const int in_page = ((1 << shift) - n) / kBlk, run = it < t.nsb ? min(in_page, t.nsb - it) : in_page;
+    left = (run + STEP - 1) / STEP;
+    look(t, it + left * STEP);
+  }
+  __device__ __forceinline__ void step(int block_bytes) {
+    keys += STEP * block_bytes;
+    exps += STEP * kBlk;
+    --left;
+    it += STEP;
+  }
 };
 
 // A lane's row and what it sees.
@@ -221,7 +246,7 @@ __device__ __forceinline__ void softmax_block(const f32x16 &s, uint32_t seen, fl
   for (int i = 3; i < 15; i += 2) top = max3(top, x[i], x[i + 1]);
   const float2 th = halves(max2(top, x[15]));
   const float now = max2(th.x, th.y) * c;
-  if (__ballot(now > m + kSlack)) {
+  if (__builtin_expect(__ballot(now > m + kSlack) != 0, 0)) {
     const float to = now > m ? now : m, f = __builtin_amdgcn_exp2f(m - to);
     m = to;
     l *= f;
@@ -321,12 +346,12 @@ __device__ __forceinline__ void wait_copies() {
   __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | (N >> 4) << 14);  // vmcnt(N) lgkmcnt(0)
   asm volatile("" ::: "memory");
 }
-// 64 lanes' 16 bytes (or 4) from their addresses to LDS, lane after lane
-__device__ __forceinline__ void copy16(const char *lane_src, char *dst) {
-  __builtin_amdgcn_global_load_lds(lane_src, (__attribute__((address_space(3))) char *)dst, 16, 0, 0);
+// 64 lanes' 16 bytes (or 4) at src + lane_off to LDS, lane after lane
+__device__ __forceinline__ void copy16(const char *src, uint32_t lane_off, char *dst) {
+  __builtin_amdgcn_global_load_lds(src + lane_off, (__attribute__((address_space(3))) char *)dst, 16, 0, 0);
 }
-__device__ __forceinline__ void copy4(const char *lane_src, char *dst) {
-  __builtin_amdgcn_global_load_lds(lane_src, (__attribute__((address_space(3))) char *)dst, 4, 0, 0);
+__device__ __forceinline__ void copy4(const char *src, uint32_t lane_off, char *dst) {
+  __builtin_amdgcn_global_load_lds(src + lane_off, (__attribute__((address_space(3))) char *)dst, 4, 0, 0);
 }
 
 // eight 8-bit elements (words a, b) times a power of two
@@ -452,55 +477,6 @@ __device__ __forceinline__ void full_block(const char *keys, const char *vals, c
       for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(vals, x, t, lane));
     o[t] = products<DT>(r.v[t], pf, o[t]);
   }
-}
-
-// Two blocks that all rows see whole, at slots `one` and `two`: one maximum for both, and the
-// second's exponentials beside the first's products.
-template <int DT, int D>
-__device__ __forceinline__ void full_pair(const char *one, const char *two, const QRegs<DT, D> &q, float c, int lane,
-                                          float &m, float &l, f32x16 (&o)[D / 32]) {
-  constexpr int T = D / 32, S = VRegs<DT, D>::S, kPart = kBlk * D * (DT == DT_F8 ? 1 : 2);
-  const f32x16 s[2] = {scores<DT, D>(one, one + 2 * kPart, q, lane), scores<DT, D>(two, two + 2 * kPart, q, lane)};
-  VRegs<DT, D> r;
-#pragma unroll
-  for (int t = 0; t < T; ++t)
-#pragma unroll
-    for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(one + kPart, x, t, lane));
-  float top[2];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    top[u] = max3(s[u][0], s[u][1], s[u][2]);
-#pragma unroll
-    for (int i = 3; i < 15; i += 2) top[u] = max3(top[u], s[u][i], s[u][i + 1]);
-  }
-  const float2 th = halves(max3(max2(top[0], top[1]), s[0][15], s[1][15]));
-  const float now = max2(th.x, th.y) * c;
-  if (__ballot(now > m + kSlack)) {
-    const float to = now > m ? now : m, f = __builtin_amdgcn_exp2f(m - to);
-    m = to;
-    l *= f;
-    rescale(o, f);
-  }
-  float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    float p[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], c, -m));
-      sum[i & 1] += p[i];
-    }
-    const char *at = u ? two : one;
-    const POperand<DT, false> pf(p, at + 2 * kPart + 32, 0, lane >> 5);
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      if (u)
-#pragma unroll
-        for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(at + kPart, x, t, lane));
-      o[t] = products<DT>(r.v[t], pf, o[t]);
-    }
-  }
-  l += sum[0] + sum[1];
 }
 
 // Any other block.  Non-finite values that not all rows see make NaN (of those components)

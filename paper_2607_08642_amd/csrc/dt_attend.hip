@@ -60,37 +60,37 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   float m = kFloor, l = 0.0f;
 
   // ---- the wave's blocks: copies into its ring
-  const Pages pages(a, b, head);
   char *mine = ring + wave * (St::kLds / W);
   constexpr int kSlot = 2 * St::kPart + St::kExps;
-  auto copy_keys = [&](int block, int page, char *slot) {
-    const char *hp = pages.at(page);
-    const int n = pages.token(block);
-    if (DT == DT_F8)  // lanes 0-7 (mod 16): the keys' 32 exponents, 8-15: the values'
-      copy4(hp + a.cache.s_off + n + (lane & 7) * 4 + (lane & 8 ? 1 << pages.shift : 0), slot + 2 * St::kPart);
-    hp += (int64_t)n * D * ES + lane * 16;
+  const uint32_t off16 = lane * 16;
+  // exponents: lanes 0-7 (mod 16) the keys' 32, lanes 8-15 the values'
+  const uint32_t off4 = (lane & 7) * 4 + (lane & 8 ? 1 << a.cache.page_shift : 0);
+  auto copy_keys = [&](const char *keys, const char *exps, char *slot) {
+    if (DT == DT_F8) copy4(exps, off4, slot + 2 * St::kPart);
 #pragma unroll
-    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, slot + x * 1024);
+    for (int x = 0; x < St::kOps; ++x) copy16(keys + x * 1024, off16, slot + x * 1024);
   };
-  auto copy_vals = [&](int block, int page, char *slot) {
-    const char *hp = pages.at(page) + a.cache.v_off + (int64_t)pages.token(block) * D * ES + lane * 16;
+  auto copy_vals = [&](const char *keys, char *slot) {
 #pragma unroll
-    for (int x = 0; x < St::kOps; ++x) copy16(hp + x * 1024, slot + St::kPart + x * 1024);
+    for (int x = 0; x < St::kOps; ++x) copy16(keys + a.cache.v_off + x * 1024, off16, slot + St::kPart + x * 1024);
   };
   constexpr int kK = St::kOps + (DT == DT_F8 ? 1 : 0), kV = St::kOps;
-  uint32_t there = 0;  // bit x: block (the last one asked for) - x W has a page
-  auto page_of = [&](int it) { return it < it1 ? pages.of(t.block(it)) : -1; };
   int it = it0 + wave;
+  Walk<W> walk(a, t, b, head, it, it1);
+  uint32_t there = 0;  // bit x: block (the last one asked for) - x W has a page
+  auto asked = [&]() {
+    there = there << 1 | (walk.there ? 1u : 0u);
+    walk.step(St::kPart);
+  };
 #pragma unroll
   for (int x = 0; x < NS; ++x) {
-    const int page = page_of(it + x * W);
-    if (it + x * W < it1) {
-      copy_keys(t.block(it + x * W), page, mine + x * kSlot);
-      copy_vals(t.block(it + x * W), page, mine + x * kSlot);
+    if (!walk.done()) {
+      walk.open(a, t, St::kPart);
+      copy_keys(walk.keys, walk.exps, mine + x * kSlot);
+      copy_vals(walk.keys, mine + x * kSlot);
     }
-    there = there << 1 | (pages.there(page) ? 1u : 0u);
+    asked();
   }
-  int page = page_of(it + NS * W);
   if (a.nodes > 0) {
     tree_words(a, t, b, words, 64 * W);
     __syncthreads();
@@ -101,30 +101,30 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   // keys of block it + NS W; the same with the values.
   char *slot = mine;
   auto turn = [&](auto block_step) {
-    const bool more = it + NS * W < it1;
-    const int ahead = it + NS * W < it1 ? t.block(it + NS * W) : 0;
+    const bool more = !walk.done();
     if (it + (NS - 1) * W < it1)
       wait_copies<kV + (NS - 1) * (kK + kV)>();
     else
       wait_copies<0>();
-    auto between = [&]() {
+    auto between = [&]() __attribute__((always_inline)) {
       wait_copies<63>();  // (LDS reads done)
       // (DT_F8: the values' exponents come with the keys, so those wait until the values are done with)
-      if (DT != DT_F8 && more) copy_keys(ahead, page, slot);
-      if (more)
+      if (more) {
+        walk.open(a, t, St::kPart);
+        if (DT != DT_F8) copy_keys(walk.keys, walk.exps, slot);
         wait_copies<(NS - 1) * (kK + kV) + (DT != DT_F8 ? kK : 0)>();
-      else
+      } else {
         wait_copies<0>();
+      }
     };
     block_step(between);
     wait_copies<63>();
     if (more) {
-      if (DT == DT_F8) copy_keys(ahead, page, slot);
-      copy_vals(ahead, page, slot);
+      if (DT == DT_F8) copy_keys(walk.keys, walk.exps, slot);
+      copy_vals(walk.keys, slot);
     }
-    there = there << 1 | (pages.there(page) ? 1u : 0u);
+    asked();
     it += W;
-    page = page_of(it + NS * W);
     slot = slot == mine + (NS - 1) * kSlot ? mine : slot + kSlot;
   };
   while (it < it1) {
@@ -239,11 +239,13 @@ static int stream_waves(int dtype, int D) { return kBlk * D * elem_bytes(dtype) 
 AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int heads, int window, int sinks, int nodes) {
   const int group = heads / c.kv, rows = k.max_chunk * group, sets = (rows + 31) / 32;
   AttendPlan p;
-  // few rows, or fp32: every wave its own blocks; more rows share them through LDS
-  const bool stream = dtype == DT_F32 || sets == 1;
-  p.waves = stream ? stream_waves(dtype, c.D) : sets <= 12 ? 4 : 8;
-  p.stream = stream;
-  const int full = stream ? 1 : p.waves;
+  // Few rows, or fp32: every wave its own blocks; more rows share them through LDS.  Eight waves
+  // a workgroup where that still fills the chip twice with equal work (one chunk of 4,096 over
+  // 16,384 tokens: 889 us against 925 with four); else four (eight ragged chunks of up to 509: 67
+  // against 86, a chunk of 2,047 under a window: 23 against 29).
+  p.stream = dtype == DT_F32 || sets == 1;
+  p.waves = p.stream ? stream_waves(dtype, c.D) : k.batch == 1 && (int64_t)c.kv * ((sets + 7) / 8) >= 512 ? 8 : 4;
+  const int full = p.stream ? 1 : p.waves;
   p.tiles = (sets + full - 1) / full;
   p.tile_rows = (sets + p.tiles - 1) / p.tiles * 32;  // (even tiles: 9 sets of 32 rows are 3 + 3 + 3, not 4 + 4 + 1)
   // blocks of a tile at most
@@ -254,25 +256,40 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
     const int64_t near = (span + kBlk - 1) / kBlk + 1 + (sinks + kBlk - 1) / kBlk;
     most = near < all ? (int)near : all;
   }
-  // The number of splits whose estimate is least, in units of one block's time: what a
-  // workgroup takes (its blocks, and starting and ending), times the rounds that the chip needs for
-  // all, and the join.  Of a batch the lengths are known on the device only: its workgroups are
-  // taken to have half the blocks of the longest on average, and to fill gaps.
+  // The number of splits whose estimate is least, in units of one block's time in a workgroup by
+  // itself (0.5 us with shared blocks; 1.1 us for one block of each wave):
+  //  - a workgroup takes its blocks and 5 to start and end; two on a CU take 1.5 times as long a
+  //    block, and where memory bounds the chip (5.2 TB/s) a block takes what its bytes do;
+  //  - one sequence: equal workgroups in whole rounds of the chip's slots.  A batch: its lengths
+  //    are known on the device only; 0.6 of the longest's blocks on average are assumed, and of the
+  //    chunks what the rows say; they fill gaps, with a tail of a third of a workgroup (powers of
+  //    two: three splits took longer than two and four: 120, 104, 113 us for 32 trees of 16);
+  //  - the join: its launch, and the parts written and read.
   const int64_t wgs = (int64_t)c.kv * p.tiles * k.batch;
-  const double slots = !stream && p.waves == 4 && c.D <= 128 ? 512 : 256;
-  const int unit = stream ? p.waves : 1;  // blocks that a workgroup takes at a time
+  const bool paired = !p.stream && p.waves == 4 && c.D <= 128;
+  const double unit_us = p.stream ? 1.1 : 0.5;
+  const int unit = p.stream ? p.waves : 1;  // blocks that a workgroup takes at a time
+  const double memory = unit * 2.0 * kBlk * c.D * elem_bytes(dtype) * 256 / 5.2e6 / unit_us;
+  const double share = k.batch == 1 ? 1.0 : 0.6 * k.rows / ((double)k.batch * k.max_chunk);
+  const double part = (double)k.rows * heads * c.D * 8 / 4.5e6 / unit_us;
   double best = 1e30;
   p.splits = 1;
   p.blocks = most;
-  for (int s = 1; s <= kMaxSplits && (s == 1 || (most + s - 1) / s >= 2 * unit); ++s) {
+  for (int s = 1; s <= kMaxSplits && (s == 1 || (most + s - 1) / s >= 2 * unit); s = k.batch == 1 ? s + 1 : 2 * s) {
     const int blocks = ((most + s - 1) / s + unit - 1) / unit * unit;
     const int n = (most + blocks - 1) / blocks;
-    double rounds = wgs * n / slots;
-    if (k.batch == 1)
-      rounds = ceil(rounds);
-    else
-      rounds = rounds > 2.0 ? rounds / 2 : 1.0;
-    const double cost = rounds * (blocks / unit + 5.0) + (n > 1 ? 4.0 + 0.2 * n : 0.0);
+    const double cus = wgs * n * share / 256, turns = (double)blocks / unit;
+    double slow = paired && cus > 1.0 ? 1.5 : 1.0;
+    if (p.stream && cus > 0.5 && memory > slow) slow = memory;
+    double cost = turns + 5.0;
+    const double rounds = paired ? cus / 2 : cus;
+    if (k.batch == 1) {
+      cost = ceil(rounds) * (turns * slow + 5.0);
+    } else {
+      const double filled = rounds * (turns * slow + 5.0) + 0.3 * cost;
+      cost = filled > cost ? filled : cost;
+    }
+    if (n > 1) cost += 4.0 + 0.1 * n + part * n * (k.batch == 1 ? 1.0 : 0.7);
     if (cost < best * 0.98) {
       best = cost;
       p.splits = n;

@@ -10,6 +10,8 @@ namespace dt {
 namespace {
 using namespace att;
 
+constexpr int kAhead = 3;  // blocks on their way from memory
+
 // grid: kv head (fastest), tile (the last rows, which see most, first), split; sequence
 template <int DT, int D, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((
@@ -18,9 +20,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
                                                                                                      int tile_rows) {
   constexpr int T = D / 32, ES = DT == DT_F8 ? 1 : 2, kRows = 32 * NW, kPart = kBlk * D * ES;
   constexpr int kSlot = 2 * kPart + (DT == DT_F8 ? 256 : 0);  // keys, values, exponents
-  // blocks of a turn, turns ahead that blocks are asked for
-  constexpr int B = NW == 8 && D <= 128 ? 2 : 1, kAhead = B == 2 ? 2 : 3, kSlots = (kAhead + 1) * B;
-  __shared__ __align__(16) char ring[kSlots * kSlot];
+  __shared__ __align__(16) char ring[(kAhead + 1) * kSlot];
   __shared__ uint32_t words[kRows * kTreeWords];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
@@ -46,51 +46,48 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
 
   // kilobytes of a block, each one wave's copy; every wave copies as many (past the last:
   // again one that another wave copies, the same bytes), so all count alike
-  constexpr int kPieces = 2 * kPart / 1024, kEach = (kPieces + NW - 1) / NW + (DT == DT_F8 ? 1 : 0);
-  const Pages pages(a, b, head);
-  auto copy = [&](int block, int page, char *slot) {
-    const char *hp = pages.at(page);
-    const int n = pages.token(block);
-    if (DT == DT_F8)  // lanes 0-7 (mod 16): the keys' 32 exponents, 8-15: the values'
-      copy4(hp + a.cache.s_off + n + (lane & 7) * 4 + (lane & 8 ? 1 << pages.shift : 0), slot + 2 * kPart);
-    hp += (int64_t)n * D * ES + lane * 16;
+  constexpr int kPieces = 2 * kPart / 1024, kMine = (kPieces + NW - 1) / NW, kEach = kMine + (DT == DT_F8 ? 1 : 0);
+  int64_t from[kMine];  // of the block's keys
+  int to[kMine];        // in its slot
 #pragma unroll
-    for (int x = 0; x < (kPieces + NW - 1) / NW; ++x) {
-      int i = wave + x * NW;
-      if (kPieces % NW) i = i < kPieces ? i : i - kPieces;
-      copy16(i < kPieces / 2 ? hp + i * 1024 : hp + a.cache.v_off + (i - kPieces / 2) * 1024, slot + i * 1024);
-    }
-  };
+  for (int x = 0; x < kMine; ++x) {
+    const int p = wave + x * NW, i = p < kPieces ? p : p - kPieces;
+    from[x] = i < kPieces / 2 ? i * 1024 : a.cache.v_off + (i - kPieces / 2) * 1024;
+    to[x] = i * 1024;
+  }
+  const uint32_t off16 = lane * 16;
+  // exponents: lanes 0-7 (mod 16) the keys' 32, lanes 8-15 the values'
+  const uint32_t off4 = (lane & 7) * 4 + (lane & 8 ? 1 << a.cache.page_shift : 0);
+  Walk<1> walk(a, t, b, head, it0, it1);
   uint32_t there = 0;  // bit x: block (the last one asked for) - x has a page
-  int it = it0, last = it0 - 1;
-  auto ask = [&](int page, char *slot) {
-    ++last;
-    if (last < it1) copy(t.block(last), page, slot);
-    there = there << 1 | (pages.there(page) ? 1u : 0u);
+  auto ask = [&](char *slot) {
+    if (!walk.done()) {
+      walk.open(a, t, kPart);
+      if (DT == DT_F8) copy4(walk.exps, off4, slot + 2 * kPart);
+#pragma unroll
+      for (int x = 0; x < kMine; ++x) copy16(walk.keys + from[x], off16, slot + to[x]);
+    }
+    there = there << 1 | (walk.there ? 1u : 0u);
+    walk.step(kPart);
   };
-  auto page_of = [&](int it) { return it < it1 ? pages.of(t.block(it)) : -1; };
 #pragma unroll
-  for (int x = 0; x < kAhead * B; ++x) ask(page_of(it0 + x), ring + x * kSlot);
-  int page[B];
-#pragma unroll
-  for (int x = 0; x < B; ++x) page[x] = page_of(it0 + kAhead * B + x);
-  char *slot = ring, *before = ring + kAhead * B * kSlot;  // of the present block and of the last
+  for (int x = 0; x < kAhead; ++x) ask(ring + x * kSlot);
+  int it = it0;
+  char *slot = ring, *before = ring + kAhead * kSlot;  // of the present block and of the last
+  // The present block is there (near the end: all that was asked for), for every wave, and every
+  // wave has done with the last one, whose slot takes the next.
   auto turn = [&]() {
-    if (B > 1 && (it - it0) % B) return;
-    if (it + kAhead * B <= it1)
-      wait_copies<(kAhead - 1) * B * kEach>();
+    if (it + kAhead <= it1)
+      wait_copies<(kAhead - 1) * kEach>();
     else
       wait_copies<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-#pragma unroll
-    for (int x = 0; x < B; ++x) ask(page[x], before + x * kSlot);
-#pragma unroll
-    for (int x = 0; x < B; ++x) page[x] = page_of(last + 1 + x);
-    before = slot;
+    ask(before);
   };
   auto next = [&]() {
-    slot = slot == ring + (kSlots - 1) * kSlot ? ring : slot + kSlot;
+    before = slot;
+    slot = slot == ring + kAhead * kSlot ? ring : slot + kSlot;
     ++it;
   };
   auto nothing = [] {};
@@ -100,14 +97,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     // (a loop of its own for the blocks that every row sees whole: with the masks in it, the
     // sums would move between two sets of registers in every turn)
     const int full = min(full_end(a, t, w, it), it1);
-    if constexpr (B == 2)
-      while ((it - it0) % 2 == 0 && it + 1 < full && (there >> (last - it - 1) & 3) == 3) {
-        turn();
-        full_pair<DT, D>(slot, slot + kSlot, q, c, lane, m, l, o);
-        next();
-        next();
-      }
-    for (; it < full && there >> (last - it) & 1; next()) {
+    for (; it < full && there >> (walk.it - 1 - it) & 1; next()) {
       turn();
       full_block<DT, D>(slot, slot + kPart, slot + 2 * kPart, q, c, lane, m, l, o, nothing);
     }
@@ -116,7 +106,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     const int k0 = t.block(it) * kBlk;
     if (!sees_none(a, w, k0))
       masked_block<DT, D>(slot, slot + kPart, slot + 2 * kPart, q,
-                          there >> (last - it) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
+                          there >> (walk.it - 1 - it) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
     next();
   }
   if (idle) return;

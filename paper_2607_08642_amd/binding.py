@@ -488,6 +488,8 @@ def scan_topm(logits, M: int, T: float, stream=None):
 
 
 # ---- verification: the paged cache, attention over it, the commit of a tree ----------------
+# Calls here are short (a kernel of a few us), so their own work is kept small: one lookup of the
+# raw stream, C structures that are filled anew rather than made, no checks that the C side makes.
 
 def _want(t, name, shape, dtype):
     """A contiguous device tensor of this shape and dtype, as the C ABI takes it."""
@@ -513,10 +515,12 @@ class Chunk:
         self.table = _want(table, "table", (batch, width), torch.int32)
         self.batch, self.max_chunk, self.max_len = batch, max_chunk, max_len
         self._c = dt_chunk(batch, 0, max_chunk, max_len, width, starts.data_ptr(), lens.data_ptr(), table.data_ptr())
+        self._ref = ctypes.byref(self._c)
 
-    def as_c(self, rows: int) -> dt_chunk:
+    def as_c(self, rows: int):
+        """The dt_chunk of a call with so many rows (by reference)."""
         self._c.rows = rows
-        return self._c
+        return self._ref
 
 
 @dataclasses.dataclass
@@ -531,8 +535,9 @@ class Cache:
     """dt_cache: keys and values of `layers` layers in pages, in the kernels' own order.
 
     dtype: torch.float32, torch.bfloat16 or torch.float8_e4m3fn (bf16 data with one power-of-two
-    scale for each token and head).  Calls run on torch's current stream unless one is given;
-    outputs made here are allocated on the current stream and recorded on the one that is given.
+    scale for each token and head).  Calls run on torch's current stream of the cache's device
+    unless one is given; outputs made here are allocated on the current stream and recorded on the
+    one that is given.  A Cache is used by one host thread at a time.
     """
 
     def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype, layers: int = 1,
@@ -541,7 +546,7 @@ class Cache:
         codes = {torch.float32: DT_F32, torch.bfloat16: DT_BF16, torch.float8_e4m3fn: DT_F8}
         if dtype not in codes:
             raise TypeError(f"unsupported dtype {dtype}")
-        self._lib = load()
+        self._lib, self._torch = load(), torch
         self.pages, self.page_size, self.kv_heads, self.head_dim, self.layers = (pages, page_size, kv_heads,
                                                                                 head_dim, layers)
         self.dtype = dtype
@@ -551,27 +556,42 @@ class Cache:
         _check(self._lib.dt_cache_size(ctypes.byref(c), ctypes.byref(n)))
         self.storage = torch.empty(n.value, dtype=torch.uint8, device=device)
         c.data = self.storage.data_ptr()
-        self._c = c
+        self._c, self._ref = c, ctypes.byref(c)
+        self._device = self.storage.device.index
+        self._a, self._b, self._o = dt_rows(), dt_rows(), dt_attend_options()   # a call's arguments
+        self._aref, self._bref, self._oref = (ctypes.byref(x) for x in (self._a, self._b, self._o))
         self._sizes = {}   # workspace bytes of a shape
         self._ws = {}      # a workspace of each stream
 
-    def _rows(self, t, name: str, heads: Optional[int] = None) -> dt_rows:
-        if t.dtype != self.data_dtype or t.dim() != 3 or t.shape[2] != self.head_dim or not t.is_cuda or \
-                (heads is not None and t.shape[1] != heads):
+    def _stream(self, stream):
+        if stream is None:
+            return self._torch._C._cuda_getCurrentRawStream(self._device) or None
+        return stream.cuda_stream or None
+
+    def _rows(self, c: dt_rows, t, name: str, heads: Optional[int] = None) -> int:
+        """Fill c from a tensor [rows, heads, head_dim]; its rows."""
+        shape, stride = t.shape, t.stride()
+        if t.dtype != self.data_dtype or len(shape) != 3 or shape[2] != self.head_dim or not t.is_cuda or \
+                (heads is not None and shape[1] != heads):
             raise ValueError(f"{name}: want a {self.data_dtype} device tensor [rows, {heads or 'heads'}, "
-                             f"{self.head_dim}], got {t.dtype} {tuple(t.shape)} on {t.device}")
-        s = t.stride()
-        if s[2] != 1:
-            raise ValueError(f"{name}: the last dimension must be contiguous (stride {s[2]})")
-        return dt_rows(t.data_ptr(), s[0], s[1])
+                             f"{self.head_dim}], got {t.dtype} {tuple(shape)} on {t.device}")
+        if stride[2] != 1:
+            raise ValueError(f"{name}: the last dimension must be contiguous (stride {stride[2]})")
+        c.data = t.data_ptr()
+        c.row_stride, c.head_stride = stride[0], stride[1]
+        return shape[0]
+
+    def _kv(self, k, v) -> int:
+        rows = self._rows(self._a, k, "k", self.kv_heads)
+        if self._rows(self._b, v, "v", self.kv_heads) != rows:
+            raise ValueError(f"k and v have {rows} and {v.shape[0]} rows")
+        return rows
 
     def append(self, chunk: Chunk, k, v, layer: int = 0, stream=None) -> None:
         """dt_cache_append: the chunk's keys and values [rows, kv_heads, head_dim] into a layer."""
-        kr, vr = self._rows(k, "k", self.kv_heads), self._rows(v, "v", self.kv_heads)
-        if k.shape[0] != v.shape[0]:
-            raise ValueError(f"k and v have {k.shape[0]} and {v.shape[0]} rows")
-        st = self._lib.dt_cache_append(ctypes.byref(self._c), layer, ctypes.byref(chunk.as_c(k.shape[0])),
-                                       ctypes.byref(kr), ctypes.byref(vr), _stream(stream))
+        rows = self._kv(k, v)
+        st = self._lib.dt_cache_append(self._ref, layer, chunk.as_c(rows), self._aref, self._bref,
+                                       self._stream(stream))
         if st != 0:
             _check(st)
 
@@ -581,42 +601,36 @@ class Cache:
         rows: rows of the tensors made (starts' last); out = (k, v) takes given ones instead.
         Rows that belong to no chunk are left as they are.
         """
-        import torch
         if out is None:
             if rows is None:
                 raise ValueError("read needs the number of rows, or out")
-            out = tuple(torch.empty(rows, self.kv_heads, self.head_dim, dtype=self.data_dtype,
-                                    device=self.storage.device) for _ in range(2))
+            both = self._torch.empty((2, rows, self.kv_heads, self.head_dim), dtype=self.data_dtype,
+                                     device=self.storage.device)
             if stream is not None:
-                for t in out:
-                    t.record_stream(stream)
-        k, v = out
-        kr, vr = self._rows(k, "k", self.kv_heads), self._rows(v, "v", self.kv_heads)
-        if k.shape[0] != v.shape[0]:
-            raise ValueError(f"k and v have {k.shape[0]} and {v.shape[0]} rows")
-        st = self._lib.dt_cache_read(ctypes.byref(self._c), layer, ctypes.byref(chunk.as_c(k.shape[0])),
-                                     ctypes.byref(kr), ctypes.byref(vr), _stream(stream))
+                both.record_stream(stream)
+            out = both.unbind(0)
+        n = self._kv(*out)
+        st = self._lib.dt_cache_read(self._ref, layer, chunk.as_c(n), self._aref, self._bref, self._stream(stream))
         if st != 0:
             _check(st)
         return out
 
     def workspace_size(self, chunk: Chunk, rows: int, heads: int, opts: dt_attend_options) -> int:
-        c = chunk.as_c(rows)
+        c = chunk._c
         key = (c.batch, rows, c.max_chunk, c.max_len, c.table_width, heads, opts.window, opts.sinks, opts.tree_nodes)
         n = self._sizes.get(key)
         if n is None:
             b = ctypes.c_size_t()
-            _check(self._lib.dt_attend_workspace_size(ctypes.byref(self._c), ctypes.byref(c), heads,
-                                                      ctypes.byref(opts), ctypes.byref(b)))
+            _check(self._lib.dt_attend_workspace_size(self._ref, chunk.as_c(rows), heads, ctypes.byref(opts),
+                                                      ctypes.byref(b)))
             n = self._sizes[key] = b.value
         return n
 
     def _workspace(self, n: int, stream):
         """The stream's workspace, grown to n bytes (calls on one stream follow one another)."""
-        import torch
         ws = self._ws.get(stream)
         if ws is None or ws.numel() < n:
-            ws = self._ws[stream] = torch.empty(n, dtype=torch.uint8, device=self.storage.device)
+            ws = self._ws[stream] = self._torch.empty(n, dtype=self._torch.uint8, device=self.storage.device)
         return ws
 
     def attend(self, chunk: Chunk, q, scale: Optional[float] = None, layer: int = 0, window: int = 0,
@@ -627,31 +641,30 @@ class Cache:
         mask [batch, N, N] uint8 (Tree.mask): the last N rows of every chunk are a tree's nodes, depth
         [batch, N] (Tree.depth) their depths, needed with a window.
         """
-        import torch
-        rows, heads = q.shape[0], q.shape[1]
-        qr = self._rows(q, "q")
+        rows, heads = self._rows(self._a, q, "q"), q.shape[1]
         if out is None:
-            out = torch.empty(rows, heads, self.head_dim, dtype=q.dtype, device=q.device)
+            out = self._torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=q.device)
             if stream is not None:
                 out.record_stream(stream)
-        elif out.shape[0] != rows:
+        if self._rows(self._b, out, "out", heads) != rows:
             raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
-        outr = self._rows(out, "out", heads)
-        nodes = 0
+        o = self._o
+        o.scale = self.head_dim ** -0.5 if scale is None else scale
+        o.window, o.sinks, o.tree_nodes = window, sinks, 0
+        o.mask = o.depth = None
         if mask is not None:
-            nodes = mask.shape[-1]
-            _want(mask, "mask", (chunk.batch, nodes, nodes), torch.uint8)
+            n = o.tree_nodes = mask.shape[-1]
+            o.mask = _want(mask, "mask", (chunk.batch, n, n), self._torch.uint8).data_ptr()
             if depth is not None:
-                _want(depth, "depth", (chunk.batch, nodes), torch.int32)
-        opts = dt_attend_options(self.head_dim ** -0.5 if scale is None else scale, window, sinks, nodes,
-                                 _ptr(mask), _ptr(depth))
-        s = _stream(stream)
+                o.depth = _want(depth, "depth", (chunk.batch, n), self._torch.int32).data_ptr()
+        s = self._stream(stream)
         if workspace is None:
-            n = self.workspace_size(chunk, rows, heads, opts)
-            workspace = self._workspace(n, s) if n else None
-        st = self._lib.dt_cache_attend(ctypes.byref(self._c), layer, ctypes.byref(chunk.as_c(rows)), heads,
-                                       ctypes.byref(qr), ctypes.byref(outr), ctypes.byref(opts), _ptr(workspace),
-                                       0 if workspace is None else workspace.numel(), s)
+            n = self.workspace_size(chunk, rows, heads, o)
+            if n:
+                workspace = self._workspace(n, s)
+        ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        st = self._lib.dt_cache_attend(self._ref, layer, chunk.as_c(rows), heads, self._aref, self._bref,
+                                       self._oref, ws, size, s)
         if st != 0:
             _check(st)
         return out
@@ -659,13 +672,13 @@ class Cache:
     def commit(self, chunk: Chunk, path, n_accepted, stream=None) -> None:
         """dt_cache_commit: the rows of the accepted nodes (Accepted.path, .n_accepted) moved together, in
         every layer; the nodes are the last path.shape[1] rows of each chunk."""
-        import torch
+        i32 = self._torch.int32
         n = path.shape[1]
+        _want(path, "path", (chunk.batch, n), i32)
+        _want(n_accepted, "n_accepted", (chunk.batch,), i32)
         every = min(chunk.batch * chunk.max_chunk, 2 ** 31 - 1)   # (no tensor of rows here: starts' bound)
-        _want(path, "path", (chunk.batch, n), torch.int32)
-        _want(n_accepted, "n_accepted", (chunk.batch,), torch.int32)
-        st = self._lib.dt_cache_commit(ctypes.byref(self._c), ctypes.byref(chunk.as_c(every)), n,
-                                       path.data_ptr(), n_accepted.data_ptr(), _stream(stream))
+        st = self._lib.dt_cache_commit(self._ref, chunk.as_c(every), n, path.data_ptr(), n_accepted.data_ptr(),
+                                       self._stream(stream))
         if st != 0:
             _check(st)
 
@@ -684,8 +697,9 @@ def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None)
         if stream is not None:
             for t in (out.path, out.n_accepted, out.next_token):
                 t.record_stream(stream)
+    s = torch._C._cuda_getCurrentRawStream(target.device.index) if stream is None else stream.cuda_stream
     st = load().dt_tree_accept(ctypes.byref(tree.as_c()), b, B, target.data_ptr(), out.path.data_ptr(),
-                               out.n_accepted.data_ptr(), out.next_token.data_ptr(), _stream(stream))
+                               out.n_accepted.data_ptr(), out.next_token.data_ptr(), s or None)
     if st != 0:
         _check(st)
     return out

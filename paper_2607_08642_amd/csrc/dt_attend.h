@@ -8,6 +8,8 @@
 // registers, and a row's 32 scores lie in two lanes (lane and lane ^ 32).
 #pragma once
 
+#include <type_traits>
+
 #include "dt_cache.h"
 
 namespace dt {
@@ -365,6 +367,14 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t a, uint32_t b, float scale) {
 
 __device__ __forceinline__ u32x4 lds16(const char *p) { return *reinterpret_cast<const u32x4 *>(p); }
 
+// Results of matrix products that are read behind a branch.  The products take cycles that the
+// hardware does not wait for and the compiler has to fill; it has been seen to leave out the
+// wait behind a branch (four of sixteen scores were read too early), so it stands here, in front of it.
+__device__ __forceinline__ void settle(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
+struct Nothing {  // (no branch)
+  __device__ __forceinline__ void operator()() const {}
+};
+
 // S^T of a block: `keys` in LDS in the cache's order (DT_F8: `exps` their 32 exponents).
 template <int DT, int D>
 __device__ __forceinline__ f32x16 scores(const char *keys, const char *exps, const QRegs<DT, D> &q, int lane) {
@@ -457,7 +467,8 @@ __device__ __forceinline__ void full_block(const char *keys, const char *vals, c
                                            float c, int lane, float &m, float &l, f32x16 (&o)[D / 32],
                                            const F &between) {
   constexpr int T = D / 32, S = VRegs<DT, D>::S;
-  const f32x16 s = scores<DT, D>(keys, exps, q, lane);
+  f32x16 s = scores<DT, D>(keys, exps, q, lane);
+  if (!std::is_same<F, Nothing>::value) settle(s);
   between();
   // the values are asked for before the softmax where registers allow
   constexpr bool kEarly = S * T <= 8;
@@ -486,7 +497,8 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
                                              const QRegs<DT, D> &q, uint32_t seen, float c, int lane, float &m,
                                              float &l, f32x16 (&o)[D / 32], const F &between) {
   constexpr int T = D / 32, S = VRegs<DT, D>::S;
-  const f32x16 sc = scores<DT, D>(keys, exps, q, lane);
+  f32x16 sc = scores<DT, D>(keys, exps, q, lane);
+  settle(sc);
   between();
   float p[16];
   softmax_block<true>(sc, seen, c, m, l, o, p);
@@ -550,37 +562,23 @@ __device__ __forceinline__ void store4(const AttendArgs &a, int64_t at, float x,
   }
 }
 
-// A wave's 32 finished rows: the result, or one split's part of it (the first split notes how many
-// there are; one alone writes the result).
-template <int DT, int D>
-__device__ __forceinline__ void write_rows(const AttendArgs &a, const Tile &t, const Row &w, int head, int split,
-                                           int active, bool valid, int h, const f32x16 (&o)[D / 32], float m, float l) {
-  if (!valid) return;
-  const int hq = head * a.group + w.r % a.group;
-  const int64_t row = t.q.row0 + w.i, x = row * a.heads + hq;
+// Four elements from d on of a finished row, maximum m and sum l: of the result, or of one split's part
+// of it (the first split notes how many there are; one alone writes the result).
+template <int DT>
+__device__ __forceinline__ void write4(const AttendArgs &a, int64_t row, int hq, int d, int split, int active, f32x4 y,
+                                       float m, float l) {
   if (a.splits > 1) {
+    const int64_t x = row * a.heads + hq;
     float2 *ml = a.part_ml + x * (a.splits + 1);
-    if (split == 0 && h == 0) ml[a.splits] = make_float2((float)active, 0.0f);
+    if (split == 0 && d == 0) ml[a.splits] = make_float2((float)active, 0.0f);
     if (active > 1) {
-      if (h == 0) ml[split] = make_float2(m, l);
-      float *p = a.part + (x * a.splits + split) * D;
-#pragma unroll
-      for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4 *>(p + 32 * n + 8 * i + 4 * h) =
-              f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
+      if (d == 0) ml[split] = make_float2(m, l);
+      *reinterpret_cast<f32x4 *>(a.part + (x * a.splits + split) * a.cache.D + d) = y;
       return;
     }
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (l = 0: the row saw nothing, o is 0)
-  const int64_t at = row * a.out.row + (int64_t)hq * a.out.head;
-#pragma unroll
-  for (int n = 0; n < D / 32; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      store4<DT>(a, at + 32 * n + 8 * i + 4 * h, o[n][4 * i] * inv, o[n][4 * i + 1] * inv, o[n][4 * i + 2] * inv,
-                 o[n][4 * i + 3] * inv);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // (l = 0: the row saw nothing, y is 0)
+  store4<DT>(a, row * a.out.row + (int64_t)hq * a.out.head + d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
 }  // namespace att

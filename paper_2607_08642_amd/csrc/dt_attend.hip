@@ -36,7 +36,7 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   using St = Stream<DT, D>;
   constexpr int T = D / 32, ES = St::ES, W = St::kWaves, NS = St::kSlots;
   __shared__ uint32_t words[kStreamRows * kTreeWords];
-  __shared__ float ml[W][2][32];
+  __shared__ float2 ml[W][32];  // maximum and sum
   __shared__ __align__(16) char ring[St::kLds];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, l32 = lane & 31;
@@ -146,46 +146,43 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
     });
   }
 
-  // ---- the waves' results meet, each scaled to the common maximum: upper half to lower half
+  // ---- the waves' results meet in LDS as rows; all threads scale them to the common maximum, sum
+  // and write (in loops that stay short: of a small call most of the time is code coming in)
+#pragma unroll
+  for (int n = 0; n < T; ++n) settle(o[n]);
   const float2 lh = halves(l);
-  l = lh.x + lh.y;
-  if (h == 0) {
-    ml[wave][0][l32] = m;
-    ml[wave][1][l32] = l;
-  }
+  if (h == 0) ml[wave][l32] = make_float2(m, lh.x + lh.y);
+  // (every wave is past its last block: the rings are free.  Rows of D floats, apart by one
+  // 16-byte column where that fits.)
+  constexpr int kRow = W * 32 * (D + 4) * 4 <= St::kLds ? D + 4 : D;
+  static_assert(W * 32 * kRow * 4 <= St::kLds, "");
+  float *meet = reinterpret_cast<float *>(ring);
   __syncthreads();
-  float top = ml[0][0][l32];
-#pragma unroll
-  for (int x = 1; x < W; ++x) top = max2(top, ml[x][0][l32]);
-  l = 0.0f;
-#pragma unroll
-  for (int x = 0; x < W; ++x) l += ml[x][1][l32] * __builtin_amdgcn_exp2f(ml[x][0][l32] - top);
-  const float f = __builtin_amdgcn_exp2f(m - top);
 #pragma unroll
   for (int n = 0; n < T; ++n)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[n][i] *= f;
-  // (every wave is past its last block: the rings are free.  [D][32 rows] fp32 of a wave.)
-  static_assert(W / 2 * D * 128 <= St::kLds, "");
-  float *meet = reinterpret_cast<float *>(ring);
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4 *>(meet + (wave * 32 + l32) * kRow + 32 * n + 8 * i + 4 * h) =
+          f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
+  __syncthreads();
+  const int rows = min(kStreamRows, t.rows - t.r0);
+#pragma unroll 1
+  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * W) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4, i = (t.r0 + r) / a.group, hq = head * a.group + t.r0 + r - i * a.group;
+    float top = ml[0][r].x, sum = 0.0f;
 #pragma unroll
-  for (int half = W / 2; half > 0; half >>= 1) {
-    float *at = meet + (wave & (half - 1)) * (D * 32) + 4 * h * 32 + l32;
-    if (wave >= half && wave < 2 * half)
+    for (int v = 1; v < W; ++v) top = max2(top, ml[v][r].x);
+    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int n = 0; n < T; ++n)
+    for (int v = 0; v < W; ++v) {
+      const float f = __builtin_amdgcn_exp2f(ml[v][r].x - top);
+      const f32x4 z = *reinterpret_cast<const f32x4 *>(meet + (v * 32 + r) * kRow + d);
+      sum += ml[v][r].y * f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) at[(32 * n + reg_token(i)) * 32] = o[n][i];
-    __syncthreads();
-    if (wave < half)
-#pragma unroll
-      for (int n = 0; n < T; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[n][i] += at[(32 * n + reg_token(i)) * 32];
-    __syncthreads();
+      for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(z[j], f, y[j]);
+    }
+    write4<DT>(a, (int64_t)(t.q.row0 + i), hq, d, split, active, y, top, sum);
   }
-  if (wave > 0) return;
-  write_rows<DT, D>(a, t, w, head, split, active, t.r0 + l32 < t.rows, h, o, top, l);
 }
 
 // The splits' parts scaled to their common maximum and summed in order: D / 4 lanes (of a 16-, 32- or

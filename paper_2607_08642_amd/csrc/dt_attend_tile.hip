@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     slot = slot == ring + kAhead * kSlot ? ring : slot + kSlot;
     ++it;
   };
-  auto nothing = [] {};
+  const Nothing nothing;
   if (idle)
     for (; it < it1; next()) turn();
   while (it < it1) {
@@ -109,9 +109,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
                           there >> (walk.it - 1 - it) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
     next();
   }
-  if (idle) return;
+#pragma unroll
+  for (int n = 0; n < T; ++n) settle(o[n]);
+  if (idle || r >= t.rows) return;
   const float2 lh = halves(l);
-  write_rows<DT, D>(a, t, w, head, split, active, r < t.rows, h, o, m, lh.x + lh.y);
+  const int hq = head * a.group + w.r % a.group;
+#pragma unroll
+  for (int n = 0; n < T; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      write4<DT_BF16>(a, t.q.row0 + w.i, hq, 32 * n + 8 * i + 4 * h, split, active,
+                      f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]}, m, lh.x + lh.y);
 }
 
 template <int DT, int NW>

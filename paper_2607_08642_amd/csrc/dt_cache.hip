@@ -3,9 +3,10 @@
 //
 // All are copies: bound by memory traffic for prompts, by latency for the few
 // rows of a decoding step.  A workgroup of append and read takes one block of 32
-// tokens of one kv head, keys or values (layout: dt_cache.h), through an LDS tile of
+// tokens of one kv head, keys and values (layout: dt_cache.h), through two LDS tiles of
 // 32 rows: rows of the caller's tensors are touched in runs of 128 bytes (eight lanes a
-// row), pieces of the cache in runs of 512 bytes and more.
+// row), pieces of the cache in runs of 512 bytes and more.  Values change sides in LDS two
+// elements at a time.
 #include "dt_cache.h"
 
 namespace dt {
@@ -83,199 +84,248 @@ __device__ inline bool block_of(const CacheView &c, const ChunkView &k, int b, i
   o->lo = max(first - o->pos0, 0);
   o->hi = min(min(o->q.base + o->q.n, k.width << c.page_shift) - o->pos0, kBlk);
   if (o->lo >= o->hi) return false;
-  const int page = k.table[(int64_t)b * k.width + (o->pos0 >> c.page_shift)];
+  const int page = scalar_at(k.table, (int64_t)b * k.width + (o->pos0 >> c.page_shift));
   o->page = page >= 0 && page < c.pages ? page : -1;
   o->in_page = o->pos0 & ((1 << c.page_shift) - 1);
   return true;
 }
 
-// grid: (kv head, keys or values, block of the chunk), sequence
-template <int DT>
+// Two rows' words side by side (bytes or halves of one token each): the low halves, the high halves.
+__device__ inline uint32_t low16(uint32_t a, uint32_t b) { return (a & 0xffffu) | b << 16; }
+__device__ inline uint32_t high16(uint32_t a, uint32_t b) { return a >> 16 | (b & 0xffff0000u); }
+
+// grid: (kv head, block of the chunk), sequence
+template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView k, RowsView kr, RowsView vr) {
   using El = Elem<DT>;
   using T = typename El::data;
   constexpr int E = El::E, kWords = sizeof(T) == 4 ? 8 : 4;  // words of eight elements
-  extern __shared__ __align__(16) char tile[];
-  const int head = blockIdx.x % c.kv, vals = blockIdx.x / c.kv & 1;
+  constexpr int kRow = D * El::bytes + kPad, kRuns = (D / 8 + 7) / 8;
+  __shared__ __align__(16) char tiles[2][kBlk * kRow];
+  const int head = blockIdx.x % c.kv;
   Block bl;
-  if (!block_of(c, k, blockIdx.y, blockIdx.x / (2 * c.kv), &bl) || bl.page < 0) return;
-  const int D = c.D, stride = D * El::bytes + kPad, tid = threadIdx.x;
+  if (!block_of(c, k, blockIdx.y, blockIdx.x / c.kv, &bl) || bl.page < 0) return;
+  const int tid = threadIdx.x;
   char *page = c.base + bl.page * c.page_bytes + head * c.head_bytes;
-  const RowsView &src = vals ? vr : kr;
   const int r = tid >> 3, sub = tid & 7;  // eight lanes a row
   const bool mine = r >= bl.lo && r < bl.hi;
-  uint32_t w[4][kWords];
+  uint32_t w[2][kRuns][kWords];
   if (mine) {
-    const T *p = reinterpret_cast<const T *>(src.p) + (int64_t)(bl.q.row0 + bl.pos0 + r - bl.q.base) * src.row +
-                 (int64_t)head * src.head;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (sub + 8 * i < D / 8) load8(p + 8 * (sub + 8 * i), src.vec, w[i]);
+    for (int v = 0; v < 2; ++v) {
+      const RowsView &src = v ? vr : kr;
+      const T *p = reinterpret_cast<const T *>(src.p) + (int64_t)(bl.q.row0 + bl.pos0 + r - bl.q.base) * src.row +
+                   (int64_t)head * src.head;
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i)
+        if (D % 64 == 0 || sub + 8 * i < D / 8) load8(p + 8 * (sub + 8 * i), src.vec, w[v][i]);
+    }
   }
-  char *row = tile + r * stride;
-  if constexpr (DT == DT_F8) {
-    // the row's largest finite magnitude (bf16 bits order like the values), over its eight lanes
-    uint32_t top = 0;
-    if (mine)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (sub + 8 * i < D / 8)
+  for (int v = 0; v < 2; ++v) {
+    char *row = tiles[v] + r * kRow;
+    if constexpr (DT == DT_F8) {
+      // the row's largest finite magnitude (bf16 bits order like the values), over its eight lanes
+      uint32_t top = 0;
+      if (mine)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t a = w[i][j] & 0x7fffu, b = w[i][j] >> 16 & 0x7fffu;
-            top = max(top, a < 0x7f80u ? a : 0u);
-            top = max(top, b < 0x7f80u ? b : 0u);
-          }
-    for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    // top = 1.m 2^(x - 127) <= 448 2^e = 1.75 2^(8 + e): e = x - 135, one more where 1.m > 1.75
-    const int byte = min(max((int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0), 7), 247);  // e + 127
-    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);                             // 2^-e
-    if (mine) {
-      if (sub == 0) page[c.s_off + (vals ? (1 << c.page_shift) : 0) + bl.in_page + r] = (char)byte;
+        for (int i = 0; i < kRuns; ++i)
+          if (D % 64 == 0 || sub + 8 * i < D / 8)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (sub + 8 * i < D / 8) {
-          uint32_t code[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            uint32_t v = 0, bad = 0;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t x = w[i][2 * u + j], lo = x << 16, hi = x & 0xffff0000u;
-              // (the products are exact; the conversion rounds to nearest even)
-              const int two = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(lo) * inv, __uint_as_float(hi) * inv,
-                                                              0, false);
-              v |= (two & 0xffff) << (16 * j);
-              bad |= ((finite_bits(lo) ? 0u : 0x7fu) | (finite_bits(hi) ? 0u : 0x7f00u)) << (16 * j);
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t a = w[v][i][j] & 0x7fffu, b = w[v][i][j] >> 16 & 0x7fffu;
+              top = max(top, a < 0x7f80u ? a : 0u);
+              top = max(top, b < 0x7f80u ? b : 0u);
             }
-            code[u] = v | bad;  // (0x7f and 0xff are the codes of NaN)
+      for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+      // top = 1.m 2^(x - 127) <= 448 2^e = 1.75 2^(8 + e): e = x - 135, one more where 1.m > 1.75
+      const int byte = min(max((int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0), 7), 247);  // e + 127
+      const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);                             // 2^-e
+      if (mine) {
+        if (sub == 0) page[c.s_off + (v ? (1 << c.page_shift) : 0) + bl.in_page + r] = (char)byte;
+#pragma unroll
+        for (int i = 0; i < kRuns; ++i)
+          if (D % 64 == 0 || sub + 8 * i < D / 8) {
+            uint32_t code[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              uint32_t x2 = 0, bad = 0;
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const uint32_t x = w[v][i][2 * u + j], lo = x << 16, hi = x & 0xffff0000u;
+                // (the products are exact; the conversion rounds to nearest even)
+                const int two = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(lo) * inv, __uint_as_float(hi) * inv,
+                                                                0, false);
+                x2 |= (two & 0xffff) << (16 * j);
+                bad |= ((finite_bits(lo) ? 0u : 0x7fu) | (finite_bits(hi) ? 0u : 0x7f00u)) << (16 * j);
+              }
+              code[u] = x2 | bad;  // (0x7f and 0xff are the codes of NaN)
+            }
+            *reinterpret_cast<uint2 *>(row + 8 * (sub + 8 * i)) = make_uint2(code[0], code[1]);
           }
-          *reinterpret_cast<uint2 *>(row + 8 * (sub + 8 * i)) = make_uint2(code[0], code[1]);
+      }
+    } else if (mine) {
+#pragma unroll
+      for (int i = 0; i < kRuns; ++i)
+        if (D % 64 == 0 || sub + 8 * i < D / 8) {
+          u32x4 *d = reinterpret_cast<u32x4 *>(row + 8 * El::bytes * (sub + 8 * i));
+#pragma unroll
+          for (int j = 0; j < kWords / 4; ++j)
+            d[j] = u32x4{w[v][i][4 * j], w[v][i][4 * j + 1], w[v][i][4 * j + 2], w[v][i][4 * j + 3]};
         }
     }
-  } else if (mine) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (sub + 8 * i < D / 8) {
-        u32x4 *d = reinterpret_cast<u32x4 *>(row + 8 * El::bytes * (sub + 8 * i));
-#pragma unroll
-        for (int j = 0; j < kWords / 4; ++j)
-          d[j] = u32x4{w[i][4 * j], w[i][4 * j + 1], w[i][4 * j + 2], w[i][4 * j + 3]};
-      }
   }
   __syncthreads();
-  if (!vals) {
-    char *out = page + (int64_t)bl.in_page * D * El::bytes;
-    for (int i = tid; i < kBlk * D / E; i += kThreads) {
-      const int rr = i & (kBlk - 1);
-      if (rr >= bl.lo && rr < bl.hi)
-        reinterpret_cast<u32x4 *>(out)[i] = *reinterpret_cast<const u32x4 *>(tile + rr * stride + (i / kBlk) * 16);
+  char *keys = page + (int64_t)bl.in_page * D * El::bytes, *vals = keys + c.v_off;
+#pragma unroll
+  for (int i = tid; i < kBlk * D / E; i += kThreads) {
+    const int rr = i % kBlk;
+    if (rr >= bl.lo && rr < bl.hi)
+      reinterpret_cast<u32x4 *>(keys)[i] = *reinterpret_cast<const u32x4 *>(tiles[0] + rr * kRow + (i / kBlk) * 16);
+  }
+  if (bl.lo == 0 && bl.hi == kBlk) {
+    // pieces (g, d) and (g, d + 1) from the rows of g's tokens
+    for (int i = tid; i < kBlk / E * D / 2; i += kThreads) {
+      const int g = i / (D / 2), d = i % (D / 2) * 2;
+      u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < E; j += El::bytes == 4 ? 1 : 2) {
+        const char *s = tiles[1] + v_token<E>(g, j) * kRow + d * El::bytes;  // (tokens j and j + 1 are neighbours)
+        if constexpr (El::bytes == 4) {
+          const uint2 a = *reinterpret_cast<const uint2 *>(s);
+          x[j] = a.x;
+          y[j] = a.y;
+        } else if constexpr (El::bytes == 2) {
+          const uint32_t a = *reinterpret_cast<const uint32_t *>(s), b = *reinterpret_cast<const uint32_t *>(s + kRow);
+          x[j / 2] = low16(a, b);
+          y[j / 2] = high16(a, b);
+        } else {
+          const uint32_t a = *reinterpret_cast<const uint16_t *>(s), b = *reinterpret_cast<const uint16_t *>(s + kRow);
+          x[j / 4] |= ((a & 0xffu) | (b & 0xffu) << 8) << (8 * (j & 3));
+          y[j / 4] |= (a >> 8 | (b & 0xff00u)) << (8 * (j & 3));
+        }
+      }
+      u32x4 *o = reinterpret_cast<u32x4 *>(vals) + g * D + d;
+      o[0] = x;
+      o[1] = y;
     }
     return;
   }
-  char *out = page + c.v_off + (int64_t)bl.in_page * D * El::bytes;
-  const bool whole = bl.lo == 0 && bl.hi == kBlk;
-  for (int i = tid; i < kBlk / E * D; i += kThreads) {
-    const int g = i / D, d = i - g * D;
-    if (whole) {
-      u32x4 v = {0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const char *s = tile + v_token<E>(g, j) * stride + d * El::bytes;
-        if constexpr (El::bytes == 4)
-          v[j] = *reinterpret_cast<const uint32_t *>(s);
-        else if constexpr (El::bytes == 2)
-          v[j >> 1] |= (uint32_t) * reinterpret_cast<const uint16_t *>(s) << (16 * (j & 1));
-        else
-          v[j >> 2] |= (uint32_t) * reinterpret_cast<const uint8_t *>(s) << (8 * (j & 3));
-      }
-      reinterpret_cast<u32x4 *>(out)[i] = v;
-    } else {
-      // (the piece's other tokens keep their elements)
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const int rr = v_token<E>(g, j);
-        if (rr < bl.lo || rr >= bl.hi) continue;
-        const char *s = tile + rr * stride + d * El::bytes;
-        char *o = out + (int64_t)i * 16 + j * El::bytes;
-        if constexpr (El::bytes == 4)
-          *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<const uint32_t *>(s);
-        else if constexpr (El::bytes == 2)
-          *reinterpret_cast<uint16_t *>(o) = *reinterpret_cast<const uint16_t *>(s);
-        else
-          *o = *s;
-      }
-    }
+  // (a part of a block: the pieces' other tokens keep their elements)
+  for (int i = tid; i < (bl.hi - bl.lo) * D; i += kThreads) {
+    const int rr = bl.lo + i / D, d = i % D;
+    const char *s = tiles[1] + rr * kRow + d * El::bytes;
+    char *o = vals + (v_group<E>(rr) * D + d) * 16 + v_elem<E>(rr) * El::bytes;
+    if constexpr (El::bytes == 4)
+      *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<const uint32_t *>(s);
+    else if constexpr (El::bytes == 2)
+      *reinterpret_cast<uint16_t *>(o) = *reinterpret_cast<const uint16_t *>(s);
+    else
+      *o = *s;
   }
 }
 
-// grid as append_kernel's; the tile holds the data type
-template <int DT>
+// grid as append_kernel's; the tiles hold the data type
+template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(CacheView c, ChunkView k, RowsView kr, RowsView vr) {
   using El = Elem<DT>;
   using T = typename El::data;
-  constexpr int E = El::E;
-  extern __shared__ __align__(16) char tile[];
-  const int head = blockIdx.x % c.kv, vals = blockIdx.x / c.kv & 1;
+  constexpr int E = El::E, kRow = D * (int)sizeof(T) + kPad, kPieces = kBlk * D / E;
+  __shared__ __align__(16) char tiles[2][kBlk * kRow];
+  const int head = blockIdx.x % c.kv;
   Block bl;
-  if (!block_of(c, k, blockIdx.y, blockIdx.x / (2 * c.kv), &bl)) return;
-  const int D = c.D, stride = D * (int)sizeof(T) + kPad, tid = threadIdx.x;
-  const char *page = c.base + (bl.page < 0 ? 0 : bl.page) * c.page_bytes + head * c.head_bytes;
-  const char *in = page + (vals ? c.v_off : 0) + (int64_t)bl.in_page * D * El::bytes;
-  const uint8_t *ex = reinterpret_cast<const uint8_t *>(page + c.s_off) + (vals ? (1 << c.page_shift) : 0) + bl.in_page;
-  for (int i = tid; i < kBlk * D / E; i += kThreads) {
-    u32x4 v = {0, 0, 0, 0};
-    if (bl.page >= 0) v = reinterpret_cast<const u32x4 *>(in)[i];
-    const int g = vals ? i / D : i / kBlk, d = vals ? i - g * D : g * E, rr = i & (kBlk - 1);
+  if (!block_of(c, k, blockIdx.y, blockIdx.x / c.kv, &bl)) return;
+  const int tid = threadIdx.x;
+  const bool there = bl.page >= 0;  // (else zeros)
+  const char *page = c.base + (there ? bl.page : 0) * c.page_bytes + head * c.head_bytes;
+  const char *keys = page + (int64_t)bl.in_page * D * El::bytes, *vals = keys + c.v_off;
+  const uint8_t *ke = reinterpret_cast<const uint8_t *>(page + c.s_off) + bl.in_page, *ve = ke + (1 << c.page_shift);
+  // all loads first
+  constexpr int kK = (kPieces + kThreads - 1) / kThreads, kV = (kPieces / 2 + kThreads - 1) / kThreads;
+  u32x4 kv[kK], vv[kV][2];
+#pragma unroll
+  for (int n = 0; n < kK; ++n) {
+    kv[n] = u32x4{0, 0, 0, 0};
+    if (there && (kPieces % kThreads == 0 || tid + n * kThreads < kPieces))
+      kv[n] = reinterpret_cast<const u32x4 *>(keys)[tid + n * kThreads];
+  }
+#pragma unroll
+  for (int n = 0; n < kV; ++n) {
+    vv[n][0] = vv[n][1] = u32x4{0, 0, 0, 0};
+    if (there && (kPieces / 2 % kThreads == 0 || tid + n * kThreads < kPieces / 2)) {
+      vv[n][0] = reinterpret_cast<const u32x4 *>(vals)[2 * (tid + n * kThreads)];
+      vv[n][1] = reinterpret_cast<const u32x4 *>(vals)[2 * (tid + n * kThreads) + 1];
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < kK; ++n) {
+    const int i = tid + n * kThreads, rr = i % kBlk, d = i / kBlk * E;
+    if (kPieces % kThreads && i >= kPieces) break;
+    char *o = tiles[0] + rr * kRow + d * (int)sizeof(T);
     if constexpr (DT == DT_F8) {
+      const float s = there ? exp_of(ke[rr]) : 0.0f;
+      u32x4 z[2];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(v[u], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(v[u], true);
-        const float f[4] = {a[0], a[1], b[0], b[1]};
-        if (vals) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int t = v_token<E>(g, 4 * u + j);
-            const uint32_t two = pack_bf16(bl.page < 0 ? 0.0f : f[j] * exp_of(ex[t]), 0.0f);
-            *reinterpret_cast<uint16_t *>(tile + t * stride + d * 2) = (uint16_t)two;
-          }
-        } else {
-          const float s = bl.page < 0 ? 0.0f : exp_of(ex[rr]);
-          *reinterpret_cast<uint2 *>(tile + rr * stride + (d + 4 * u) * 2) =
-              make_uint2(pack_bf16(f[0] * s, f[1] * s), pack_bf16(f[2] * s, f[3] * s));
-        }
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(kv[n][u], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(kv[n][u], true);
+        z[u >> 1][2 * (u & 1)] = pack_bf16(a[0] * s, a[1] * s);
+        z[u >> 1][2 * (u & 1) + 1] = pack_bf16(b[0] * s, b[1] * s);
       }
-    } else if (!vals) {
-      *reinterpret_cast<u32x4 *>(tile + rr * stride + d * El::bytes) = v;
+      reinterpret_cast<u32x4 *>(o)[0] = z[0];
+      reinterpret_cast<u32x4 *>(o)[1] = z[1];
     } else {
+      *reinterpret_cast<u32x4 *>(o) = kv[n];
+    }
+  }
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        char *o = tile + v_token<E>(g, j) * stride + d * El::bytes;
-        if constexpr (El::bytes == 4)
-          *reinterpret_cast<uint32_t *>(o) = v[j];
-        else
-          *reinterpret_cast<uint16_t *>(o) = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+  for (int n = 0; n < kV; ++n) {
+    // pieces (g, d) and (g, d + 1) into the rows of g's tokens
+    const int i = tid + n * kThreads, g = i / (D / 2), d = i % (D / 2) * 2;
+    if (kPieces / 2 % kThreads && i >= kPieces / 2) break;
+#pragma unroll
+    for (int j = 0; j < E; j += El::bytes == 4 ? 1 : 2) {
+      const int t = v_token<E>(g, j);  // (tokens j and j + 1 are neighbours)
+      char *o = tiles[1] + t * kRow + d * (int)sizeof(T);
+      if constexpr (DT == DT_F32) {
+        *reinterpret_cast<uint2 *>(o) = make_uint2(vv[n][0][j], vv[n][1][j]);
+      } else if constexpr (DT == DT_BF16) {
+        *reinterpret_cast<uint32_t *>(o) = low16(vv[n][0][j / 2], vv[n][1][j / 2]);
+        *reinterpret_cast<uint32_t *>(o + kRow) = high16(vv[n][0][j / 2], vv[n][1][j / 2]);
+      } else {
+        const bool hi = j & 2;
+        const f32x2 a = hi ? __builtin_amdgcn_cvt_pk_f32_fp8(vv[n][0][j / 4], true)
+                           : __builtin_amdgcn_cvt_pk_f32_fp8(vv[n][0][j / 4], false),
+                    b = hi ? __builtin_amdgcn_cvt_pk_f32_fp8(vv[n][1][j / 4], true)
+                           : __builtin_amdgcn_cvt_pk_f32_fp8(vv[n][1][j / 4], false);
+        const uint32_t e2 = there ? *reinterpret_cast<const uint16_t *>(ve + t) : 0u;  // (t is even)
+        const float s0 = exp_of(e2 & 0xffu), s1 = exp_of(e2 >> 8);
+        *reinterpret_cast<uint32_t *>(o) = pack_bf16(a[0] * s0, b[0] * s0);
+        *reinterpret_cast<uint32_t *>(o + kRow) = pack_bf16(a[1] * s1, b[1] * s1);
       }
     }
   }
   __syncthreads();
-  const RowsView &dst = vals ? vr : kr;
   const int r = tid >> 3, sub = tid & 7;
   if (r < bl.lo || r >= bl.hi) return;
-  T *p = reinterpret_cast<T *>(dst.p) + (int64_t)(bl.q.row0 + bl.pos0 + r - bl.q.base) * dst.row +
-         (int64_t)head * dst.head;
   constexpr int n = 16 / (int)sizeof(T);  // elements of a 16-byte store
-  for (int i = sub; i < D / n; i += 8) {
-    const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + r * stride + i * 16);
-    if (dst.vec) {
-      *reinterpret_cast<u32x4 *>(p + n * i) = v;
-    } else {
 #pragma unroll
-      for (int j = 0; j < n; ++j) {
-        if constexpr (sizeof(T) == 4)
-          p[n * i + j] = __uint_as_float(v[j]);
-        else
-          p[n * i + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+  for (int v = 0; v < 2; ++v) {
+    const RowsView &dst = v ? vr : kr;
+    T *p = reinterpret_cast<T *>(dst.p) + (int64_t)(bl.q.row0 + bl.pos0 + r - bl.q.base) * dst.row +
+           (int64_t)head * dst.head;
+#pragma unroll
+    for (int i = sub; i < D / n; i += 8) {
+      const u32x4 x = *reinterpret_cast<const u32x4 *>(tiles[v] + r * kRow + i * 16);
+      if (dst.vec) {
+        *reinterpret_cast<u32x4 *>(p + n * i) = x;
+      } else {
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+          if constexpr (sizeof(T) == 4)
+            p[n * i + j] = __uint_as_float(x[j]);
+          else
+            p[n * i + j] = (uint16_t)(x[j >> 1] >> (16 * (j & 1)));
+        }
       }
     }
   }
@@ -407,22 +457,30 @@ int chunk_blocks(const ChunkView &k) { return (k.max_chunk + 2 * kBlk - 2) / kBl
 
 }  // namespace
 
+template <int DT>
+static hipError_t launch_store(bool read, const CacheView &c, const ChunkView &k, const RowsView &kr, const RowsView &vr,
+                               hipStream_t s) {
+  const dim3 grid(c.kv * chunk_blocks(k), k.batch);
+  auto f = c.D == 64    ? read ? read_kernel<DT, 64> : append_kernel<DT, 64>
+           : c.D == 96  ? read ? read_kernel<DT, 96> : append_kernel<DT, 96>
+           : c.D == 128 ? read ? read_kernel<DT, 128> : append_kernel<DT, 128>
+                        : read ? read_kernel<DT, 256> : append_kernel<DT, 256>;
+  f<<<grid, kThreads, 0, s>>>(c, k, kr, vr);
+  return hipGetLastError();
+}
+
 hipError_t launch_append(const CacheView &c, int dtype, const ChunkView &k, const RowsView &kr, const RowsView &vr,
                          hipStream_t s) {
-  const dim3 grid(c.kv * 2 * chunk_blocks(k), k.batch);
-  const size_t lds = (size_t)kBlk * (c.D * elem_bytes(dtype) + kPad);
-  auto f = dtype == DT_F32 ? append_kernel<DT_F32> : dtype == DT_BF16 ? append_kernel<DT_BF16> : append_kernel<DT_F8>;
-  f<<<grid, kThreads, lds, s>>>(c, k, kr, vr);
-  return hipGetLastError();
+  return dtype == DT_F32    ? launch_store<DT_F32>(false, c, k, kr, vr, s)
+         : dtype == DT_BF16 ? launch_store<DT_BF16>(false, c, k, kr, vr, s)
+                            : launch_store<DT_F8>(false, c, k, kr, vr, s);
 }
 
 hipError_t launch_read(const CacheView &c, int dtype, const ChunkView &k, const RowsView &kr, const RowsView &vr,
                        hipStream_t s) {
-  const dim3 grid(c.kv * 2 * chunk_blocks(k), k.batch);
-  const size_t lds = (size_t)kBlk * (c.D * (dtype == DT_F32 ? 4 : 2) + kPad);
-  auto f = dtype == DT_F32 ? read_kernel<DT_F32> : dtype == DT_BF16 ? read_kernel<DT_BF16> : read_kernel<DT_F8>;
-  f<<<grid, kThreads, lds, s>>>(c, k, kr, vr);
-  return hipGetLastError();
+  return dtype == DT_F32    ? launch_store<DT_F32>(true, c, k, kr, vr, s)
+         : dtype == DT_BF16 ? launch_store<DT_BF16>(true, c, k, kr, vr, s)
+                            : launch_store<DT_F8>(true, c, k, kr, vr, s);
 }
 
 hipError_t launch_accept(const dt_tree &t, int batch, int B, const int32_t *target, int32_t *path, int32_t *n,

@@ -15,6 +15,8 @@ namespace {
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kPad = 16;  // bytes after each row of the LDS tile: an odd number of 16-byte columns
@@ -65,8 +67,6 @@ __device__ inline void load8(const uint16_t *p, bool vec, uint32_t (&w)[4]) {
     for (int i = 0; i < 4; ++i) w[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
   }
 }
-
-__device__ inline bool finite_bits(uint32_t f32) { return (f32 & 0x7f800000u) != 0x7f800000u; }
 
 // The block of this workgroup: blocks of a chunk follow the cache's, so the first and the
 // last may be partial.  False where it has no token.
@@ -125,22 +125,33 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
   for (int v = 0; v < 2; ++v) {
     char *row = tiles[v] + r * kRow;
     if constexpr (DT == DT_F8) {
-      // the row's largest finite magnitude (bf16 bits order like the values), over its eight lanes
-      uint32_t top = 0;
-      if (mine)
+      // the row's largest magnitude (bf16 bits order like the values), two at a time, over its
+      // eight lanes; only where one is not finite, again without those
+      u16x2 top2 = {0, 0};
+      auto halves_of = [&](auto f) __attribute__((always_inline)) {
+        if (mine)
 #pragma unroll
-        for (int i = 0; i < kRuns; ++i)
-          if (D % 64 == 0 || sub + 8 * i < D / 8)
+          for (int i = 0; i < kRuns; ++i)
+            if (D % 64 == 0 || sub + 8 * i < D / 8)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t a = w[v][i][j] & 0x7fffu, b = w[v][i][j] >> 16 & 0x7fffu;
-              top = max(top, a < 0x7f80u ? a : 0u);
-              top = max(top, b < 0x7f80u ? b : 0u);
-            }
+              for (int j = 0; j < 4; ++j) {
+                u16x2 x;
+                const uint32_t m = w[v][i][j] & 0x7fff7fffu;
+                __builtin_memcpy(&x, &m, 4);
+                top2 = __builtin_elementwise_max(top2, f(x));
+              }
+      };
+      halves_of([](u16x2 x) { return x; });
+      const bool bad = top2[0] >= 0x7f80 || top2[1] >= 0x7f80;
+      if (__ballot(bad)) {
+        top2 = u16x2{0, 0};
+        halves_of([](u16x2 x) { return u16x2{(uint16_t)(x[0] < 0x7f80 ? x[0] : 0), (uint16_t)(x[1] < 0x7f80 ? x[1] : 0)}; });
+      }
+      uint32_t top = max((uint32_t)top2[0], (uint32_t)top2[1]);
       for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
       // top = 1.m 2^(x - 127) <= 448 2^e = 1.75 2^(8 + e): e = x - 135, one more where 1.m > 1.75
       const int byte = min(max((int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0), 7), 247);  // e + 127
-      const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);                             // 2^-e
+      const float scale = exp_of((uint32_t)byte);
       if (mine) {
         if (sub == 0) page[c.s_off + (v ? (1 << c.page_shift) : 0) + bl.in_page + r] = (char)byte;
 #pragma unroll
@@ -149,17 +160,21 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
             uint32_t code[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              uint32_t x2 = 0, bad = 0;
+              // (x 2^-e, exact, rounded to nearest even)
+              bf16x2 a, b;
+              __builtin_memcpy(&a, &w[v][i][2 * u], 4);
+              __builtin_memcpy(&b, &w[v][i][2 * u + 1], 4);
+              i16x2 x = {0, 0};
+              x = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(x, a, scale, false);
+              x = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(x, b, scale, true);
+              __builtin_memcpy(&code[u], &x, 4);
+            }
+            if (bad) {  // (0x7f and 0xff are the codes of NaN)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const uint32_t x = w[v][i][2 * u + j], lo = x << 16, hi = x & 0xffff0000u;
-                // (the products are exact; the conversion rounds to nearest even)
-                const int two = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(lo) * inv, __uint_as_float(hi) * inv,
-                                                                0, false);
-                x2 |= (two & 0xffff) << (16 * j);
-                bad |= ((finite_bits(lo) ? 0u : 0x7fu) | (finite_bits(hi) ? 0u : 0x7f00u)) << (16 * j);
+              for (int u = 0; u < 8; ++u) {
+                const uint32_t x = w[v][i][u / 2] >> (16 * (u & 1)) & 0x7fffu;
+                if (x >= 0x7f80u) code[u / 4] |= 0x7fu << (8 * (u & 3));
               }
-              code[u] = x2 | bad;  // (0x7f and 0xff are the codes of NaN)
             }
             *reinterpret_cast<uint2 *>(row + 8 * (sub + 8 * i)) = make_uint2(code[0], code[1]);
           }

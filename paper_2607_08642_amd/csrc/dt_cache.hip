@@ -7,6 +7,8 @@
 // 32 rows: rows of the caller's tensors are touched in runs of 128 bytes (eight lanes a
 // row), pieces of the cache in runs of 512 bytes and more.  Values change sides in LDS two
 // elements at a time.
+#include <type_traits>
+
 #include "dt_cache.h"
 
 namespace dt {
@@ -47,7 +49,8 @@ __device__ inline uint32_t pack_bf16(float a, float b) {
 }
 
 // eight elements of a row of the caller's tensor, as 32-bit words (bf16: two a word)
-__device__ inline void load8(const float *p, bool vec, uint32_t (&w)[8]) {
+template <bool vec>
+__device__ __forceinline__ void load8(const float *p, uint32_t (&w)[8]) {
   if (vec) {
     const u32x4 a = reinterpret_cast<const u32x4 *>(p)[0], b = reinterpret_cast<const u32x4 *>(p)[1];
 #pragma unroll
@@ -57,7 +60,8 @@ __device__ inline void load8(const float *p, bool vec, uint32_t (&w)[8]) {
     for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(p[i]);
   }
 }
-__device__ inline void load8(const uint16_t *p, bool vec, uint32_t (&w)[4]) {
+template <bool vec>
+__device__ __forceinline__ void load8(const uint16_t *p, uint32_t (&w)[4]) {
   if (vec) {
     const u32x4 a = reinterpret_cast<const u32x4 *>(p)[0];
 #pragma unroll
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
   const int r = tid >> 3, sub = tid & 7;  // eight lanes a row
   const bool mine = r >= bl.lo && r < bl.hi;
   uint32_t w[2][kRuns][kWords];
-  if (mine) {
+  auto load = [&](auto vec) __attribute__((always_inline)) {
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
       const RowsView &src = v ? vr : kr;
@@ -118,8 +122,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
                    (int64_t)head * src.head;
 #pragma unroll
       for (int i = 0; i < kRuns; ++i)
-        if (D % 64 == 0 || sub + 8 * i < D / 8) load8(p + 8 * (sub + 8 * i), src.vec, w[v][i]);
+        if (D % 64 == 0 || sub + 8 * i < D / 8) load8<decltype(vec)::value>(p + 8 * (sub + 8 * i), w[v][i]);
     }
+  };
+  if (mine) {
+    if (kr.vec && vr.vec)
+      load(std::true_type());
+    else
+      load(std::false_type());
   }
 #pragma unroll
   for (int v = 0; v < 2; ++v) {

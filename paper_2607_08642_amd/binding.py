@@ -499,6 +499,25 @@ def _want(t, name, shape, dtype):
     return t
 
 
+def _empty(shape, dtype, device, stream):
+    """A tensor written on `stream` (None: torch's current one) and read on torch's current stream: allocated on
+    the first, so that what its memory held before is not still in use, and kept until the second has passed."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _keep(stream, *tensors):
+    """Tensors of other streams stay allocated until a call on `stream` has used them."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 class Chunk:
     """dt_chunk: the new tokens of a batch of sequences and where they lie in a cache.
 
@@ -513,6 +532,7 @@ class Chunk:
         self.starts = _want(starts, "starts", (batch + 1,), torch.int32)
         self.lens = _want(lens, "lens", (batch,), torch.int32)
         self.table = _want(table, "table", (batch, width), torch.int32)
+        self.tensors = starts, lens, table
         self.batch, self.max_chunk, self.max_len = batch, max_chunk, max_len
         self._c = dt_chunk(batch, 0, max_chunk, max_len, width, starts.data_ptr(), lens.data_ptr(), table.data_ptr())
         self._ref = ctypes.byref(self._c)
@@ -536,8 +556,10 @@ class Cache:
 
     dtype: torch.float32, torch.bfloat16 or torch.float8_e4m3fn (bf16 data with one power-of-two
     scale for each token and head).  Calls run on torch's current stream of the cache's device
-    unless one is given; outputs made here are allocated on the current stream and recorded on the
-    one that is given.  A Cache is used by one host thread at a time.
+    unless one is given (which has to wait for what made its inputs, and be waited for, as any);
+    workspaces are kept for each stream.  A captured call keeps its workspace too: a graph that is
+    replayed beside other calls on this cache is captured with a workspace of its own (`workspace`).
+    A Cache is used by one host thread at a time, with its device as the current one.
     """
 
     def __init__(self, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype, layers: int = 1,
@@ -564,6 +586,8 @@ class Cache:
         self._ws = {}      # a workspace of each stream
 
     def _stream(self, stream):
+        if self._torch._C._cuda_getDevice() != self._device:
+            raise ValueError(f"the cache is on device {self._device}, which is not the current one")
         if stream is None:
             return self._torch._C._cuda_getCurrentRawStream(self._device) or None
         return stream.cuda_stream or None
@@ -571,10 +595,10 @@ class Cache:
     def _rows(self, c: dt_rows, t, name: str, heads: Optional[int] = None) -> int:
         """Fill c from a tensor [rows, heads, head_dim]; its rows."""
         shape, stride = t.shape, t.stride()
-        if t.dtype != self.data_dtype or len(shape) != 3 or shape[2] != self.head_dim or not t.is_cuda or \
-                (heads is not None and shape[1] != heads):
-            raise ValueError(f"{name}: want a {self.data_dtype} device tensor [rows, {heads or 'heads'}, "
-                             f"{self.head_dim}], got {t.dtype} {tuple(shape)} on {t.device}")
+        if t.dtype != self.data_dtype or len(shape) != 3 or shape[2] != self.head_dim or \
+                t.get_device() != self._device or (heads is not None and shape[1] != heads):
+            raise ValueError(f"{name}: want a {self.data_dtype} tensor [rows, {heads or 'heads'}, {self.head_dim}] "
+                             f"on {self.storage.device}, got {t.dtype} {tuple(shape)} on {t.device}")
         if stride[2] != 1:
             raise ValueError(f"{name}: the last dimension must be contiguous (stride {stride[2]})")
         c.data = t.data_ptr()
@@ -594,6 +618,8 @@ class Cache:
                                        self._stream(stream))
         if st != 0:
             _check(st)
+        if stream is not None:
+            _keep(stream, k, v, *chunk.tensors)
 
     def read(self, chunk: Chunk, rows: Optional[int] = None, layer: int = 0, out=None, stream=None):
         """dt_cache_read: the chunk's keys and values as (k, v) [rows, kv_heads, head_dim].
@@ -604,15 +630,14 @@ class Cache:
         if out is None:
             if rows is None:
                 raise ValueError("read needs the number of rows, or out")
-            both = self._torch.empty((2, rows, self.kv_heads, self.head_dim), dtype=self.data_dtype,
-                                     device=self.storage.device)
-            if stream is not None:
-                both.record_stream(stream)
-            out = both.unbind(0)
+            out = _empty((2, rows, self.kv_heads, self.head_dim), self.data_dtype, self.storage.device,
+                         stream).unbind(0)
         n = self._kv(*out)
         st = self._lib.dt_cache_read(self._ref, layer, chunk.as_c(n), self._aref, self._bref, self._stream(stream))
         if st != 0:
             _check(st)
+        if stream is not None:
+            _keep(stream, *out, *chunk.tensors)
         return out
 
     def workspace_size(self, chunk: Chunk, rows: int, heads: int, opts: dt_attend_options) -> int:
@@ -626,11 +651,11 @@ class Cache:
             n = self._sizes[key] = b.value
         return n
 
-    def _workspace(self, n: int, stream):
-        """The stream's workspace, grown to n bytes (calls on one stream follow one another)."""
-        ws = self._ws.get(stream)
+    def _workspace(self, n: int, raw, stream):
+        """The stream's workspace, grown to n bytes: allocated on that stream, where calls follow one another."""
+        ws = self._ws.get(raw)
         if ws is None or ws.numel() < n:
-            ws = self._ws[stream] = self._torch.empty(n, dtype=self._torch.uint8, device=self.storage.device)
+            ws = self._ws[raw] = _empty((n,), self._torch.uint8, self.storage.device, stream)
         return ws
 
     def attend(self, chunk: Chunk, q, scale: Optional[float] = None, layer: int = 0, window: int = 0,
@@ -643,9 +668,7 @@ class Cache:
         """
         rows, heads = self._rows(self._a, q, "q"), q.shape[1]
         if out is None:
-            out = self._torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=q.device)
-            if stream is not None:
-                out.record_stream(stream)
+            out = _empty((rows, heads, self.head_dim), self.data_dtype, self.storage.device, stream)
         if self._rows(self._b, out, "out", heads) != rows:
             raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
         o = self._o
@@ -661,12 +684,14 @@ class Cache:
         if workspace is None:
             n = self.workspace_size(chunk, rows, heads, o)
             if n:
-                workspace = self._workspace(n, s)
+                workspace = self._workspace(n, s, stream)
         ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
         st = self._lib.dt_cache_attend(self._ref, layer, chunk.as_c(rows), heads, self._aref, self._bref,
                                        self._oref, ws, size, s)
         if st != 0:
             _check(st)
+        if stream is not None:
+            _keep(stream, q, out, mask, depth, workspace, *chunk.tensors)
         return out
 
     def commit(self, chunk: Chunk, path, n_accepted, stream=None) -> None:
@@ -681,6 +706,8 @@ class Cache:
                                        self._stream(stream))
         if st != 0:
             _check(st)
+        if stream is not None:
+            _keep(stream, path, n_accepted, *chunk.tensors)
 
 
 def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None) -> Accepted:
@@ -692,14 +719,12 @@ def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None)
     b, B = tree.tokens.shape
     _want(target, "target", (b, B + 1), torch.int32)
     if out is None:
-        i32 = dict(dtype=torch.int32, device=target.device)
-        out = Accepted(torch.empty(b, B, **i32), torch.empty(b, **i32), torch.empty(b, **i32))
-        if stream is not None:
-            for t in (out.path, out.n_accepted, out.next_token):
-                t.record_stream(stream)
+        out = Accepted(*(_empty(shape, torch.int32, target.device, stream) for shape in ((b, B), (b,), (b,))))
     s = torch._C._cuda_getCurrentRawStream(target.device.index) if stream is None else stream.cuda_stream
     st = load().dt_tree_accept(ctypes.byref(tree.as_c()), b, B, target.data_ptr(), out.path.data_ptr(),
                                out.n_accepted.data_ptr(), out.next_token.data_ptr(), s or None)
     if st != 0:
         _check(st)
+    if stream is not None:
+        _keep(stream, tree.tokens, tree.parents, tree.n_nodes, target, out.path, out.n_accepted, out.next_token)
     return out

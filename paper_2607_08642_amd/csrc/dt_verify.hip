@@ -5,6 +5,9 @@
 namespace dt {
 namespace {
 
+// Workgroups along a grid's axis: a launch counts its threads (256 or fewer a group here) in 32 bits.
+constexpr int kMaxGroups = 1 << 24;
+
 bool positive_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 dt_status check_cache(const dt_cache *c, bool data) {
@@ -73,7 +76,7 @@ dt_status check_store(const dt_cache *cache, int layer, const dt_chunk *chunk, c
   if (st == DT_OK) st = check_chunk(cache, chunk, true);
   if (st == DT_OK) st = check_rows(k, data_dtype(cache->dtype), "k", kr);
   if (st == DT_OK) st = check_rows(v, data_dtype(cache->dtype), "v", vr);
-  if (st == DT_OK && ((int64_t)chunk->max_chunk / kBlk + 3) * 2 * cache->kv_heads > 0x7fffffff)
+  if (st == DT_OK && ((int64_t)chunk->max_chunk / kBlk + 3) * cache->kv_heads >= kMaxGroups)
     st = fail(DT_ERR_UNSUPPORTED, "max_chunk and kv_heads are too large together");
   return st;
 }
@@ -83,8 +86,8 @@ dt_status check_attend(const dt_cache *c, const dt_chunk *k, int heads, const dt
   if (heads < 1 || heads % c->kv_heads)
     return fail(DT_ERR_SHAPE, "heads (%d) must be a positive multiple of kv_heads (%d)", heads, c->kv_heads);
   if (heads / c->kv_heads > 1024) return fail(DT_ERR_UNSUPPORTED, "at most 1024 heads per kv head");
-  if ((int64_t)k->max_chunk * heads > (int64_t)1 << 30)
-    return fail(DT_ERR_UNSUPPORTED, "max_chunk * heads must be <= 2^30");
+  if ((int64_t)k->max_chunk * heads > (int64_t)1 << 28)
+    return fail(DT_ERR_UNSUPPORTED, "max_chunk * heads must be <= 2^28");
   if (!(o->scale - o->scale == 0.0f)) return fail(DT_ERR_SHAPE, "scale must be finite");
   if (o->window < 0 || o->sinks < 0 || o->tree_nodes < 0)
     return fail(DT_ERR_SHAPE, "window, sinks and tree_nodes must be >= 0");
@@ -212,6 +215,7 @@ dt_status dt_tree_accept(const dt_tree *tree, int batch, int B, const int32_t *t
     return fail(DT_ERR_NULL, "tree (tokens, parents, n_nodes), target and every output are required");
   if (batch < 1 || B < 1) return fail(DT_ERR_SHAPE, "sizes must be positive (batch=%d B=%d)", batch, B);
   if (B > kMaxB) return fail(DT_ERR_UNSUPPORTED, "B must be <= %d (%d)", kMaxB, B);
+  if (batch >= kMaxGroups) return fail(DT_ERR_UNSUPPORTED, "batch must be < %d (%d)", kMaxGroups, batch);
   for (const void *p : {(const void *)tree->tokens, (const void *)tree->parents, (const void *)tree->n_nodes,
                         (const void *)target, (const void *)path, (const void *)n_accepted, (const void *)next_token})
     if (reinterpret_cast<uintptr_t>(p) % 4) return fail(DT_ERR_ALIGN, "tensors must be naturally aligned");
@@ -231,7 +235,7 @@ dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int node
   if (nodes < 1 || nodes > chunk->max_chunk)
     return fail(DT_ERR_SHAPE, "nodes %d outside [1, max_chunk=%d]", nodes, chunk->max_chunk);
   if (nodes > kMaxB) return fail(DT_ERR_UNSUPPORTED, "nodes must be <= %d (%d)", kMaxB, nodes);
-  if ((int64_t)cache->layers * cache->kv_heads > 0x7fffffff)
+  if ((int64_t)cache->layers * cache->kv_heads >= kMaxGroups)
     return fail(DT_ERR_UNSUPPORTED, "layers * kv_heads is too large");
   const hipError_t e = launch_commit(cache_view(*cache, 0), cache->dtype, cache->layers, chunk_view(*chunk), nodes,
                                      path, n_accepted, static_cast<hipStream_t>(stream));

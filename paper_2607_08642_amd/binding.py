@@ -499,10 +499,9 @@ def _want(t, name, shape, dtype):
     return t
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(torch, shape, dtype, device, stream):
     """A tensor written on `stream` (None: torch's current one) and read on torch's current stream: allocated on
     the first, so that what its memory held before is not still in use, and kept until the second has passed."""
-    import torch
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
@@ -572,14 +571,15 @@ class Cache:
         self.pages, self.page_size, self.kv_heads, self.head_dim, self.layers = (pages, page_size, kv_heads,
                                                                                 head_dim, layers)
         self.dtype = dtype
-        self.data_dtype = torch.float32 if dtype == torch.float32 else torch.bfloat16
+        self.data_dtype, self._data_bytes = (torch.float32, 4) if dtype == torch.float32 else (torch.bfloat16, 2)
         c = dt_cache(None, layers, pages, page_size, kv_heads, head_dim, codes[dtype])
         n = ctypes.c_size_t()
         _check(self._lib.dt_cache_size(ctypes.byref(c), ctypes.byref(n)))
         self.storage = torch.empty(n.value, dtype=torch.uint8, device=device)
         c.data = self.storage.data_ptr()
         self._c, self._ref = c, ctypes.byref(c)
-        self._device = self.storage.device.index
+        self._at = self.storage.device
+        self._device = self._at.index
         self._a, self._b, self._o = dt_rows(), dt_rows(), dt_attend_options()   # a call's arguments
         self._aref, self._bref, self._oref = (ctypes.byref(x) for x in (self._a, self._b, self._o))
         self._sizes = {}   # workspace bytes of a shape
@@ -598,7 +598,7 @@ class Cache:
         if t.dtype != self.data_dtype or len(shape) != 3 or shape[2] != self.head_dim or \
                 t.get_device() != self._device or (heads is not None and shape[1] != heads):
             raise ValueError(f"{name}: want a {self.data_dtype} tensor [rows, {heads or 'heads'}, {self.head_dim}] "
-                             f"on {self.storage.device}, got {t.dtype} {tuple(shape)} on {t.device}")
+                             f"on {self._at}, got {t.dtype} {tuple(shape)} on {t.device}")
         if stride[2] != 1:
             raise ValueError(f"{name}: the last dimension must be contiguous (stride {stride[2]})")
         c.data = t.data_ptr()
@@ -630,12 +630,19 @@ class Cache:
         if out is None:
             if rows is None:
                 raise ValueError("read needs the number of rows, or out")
-            out = _empty((2, rows, self.kv_heads, self.head_dim), self.data_dtype, self.storage.device,
-                         stream).unbind(0)
-        n = self._kv(*out)
-        st = self._lib.dt_cache_read(self._ref, layer, chunk.as_c(n), self._aref, self._bref, self._stream(stream))
+            both = _empty(self._torch, (2, rows, self.kv_heads, self.head_dim), self.data_dtype, self._at, stream)
+            a, b = self._a, self._b
+            a.data = at = both.data_ptr()
+            a.head_stride = b.head_stride = self.head_dim
+            a.row_stride = b.row_stride = row = self.kv_heads * self.head_dim
+            b.data = at + rows * row * self._data_bytes
+        else:
+            rows = self._kv(*out)
+        st = self._lib.dt_cache_read(self._ref, layer, chunk.as_c(rows), self._aref, self._bref, self._stream(stream))
         if st != 0:
             _check(st)
+        if out is None:
+            out = both.unbind(0)
         if stream is not None:
             _keep(stream, *out, *chunk.tensors)
         return out
@@ -655,7 +662,7 @@ class Cache:
         """The stream's workspace, grown to n bytes: allocated on that stream, where calls follow one another."""
         ws = self._ws.get(raw)
         if ws is None or ws.numel() < n:
-            ws = self._ws[raw] = _empty((n,), self._torch.uint8, self.storage.device, stream)
+            ws = self._ws[raw] = _empty(self._torch, (n,), self._torch.uint8, self._at, stream)
         return ws
 
     def attend(self, chunk: Chunk, q, scale: Optional[float] = None, layer: int = 0, window: int = 0,
@@ -668,7 +675,7 @@ class Cache:
         """
         rows, heads = self._rows(self._a, q, "q"), q.shape[1]
         if out is None:
-            out = _empty((rows, heads, self.head_dim), self.data_dtype, self.storage.device, stream)
+            out = _empty(self._torch, (rows, heads, self.head_dim), self.data_dtype, self._at, stream)
         if self._rows(self._b, out, "out", heads) != rows:
             raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
         o = self._o
@@ -719,7 +726,9 @@ def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None)
     b, B = tree.tokens.shape
     _want(target, "target", (b, B + 1), torch.int32)
     if out is None:
-        out = Accepted(*(_empty(shape, torch.int32, target.device, stream) for shape in ((b, B), (b,), (b,))))
+        at, i32 = target.device, torch.int32
+        out = Accepted(_empty(torch, (b, B), i32, at, stream), _empty(torch, (b,), i32, at, stream),
+                       _empty(torch, (b,), i32, at, stream))
     s = torch._C._cuda_getCurrentRawStream(target.device.index) if stream is None else stream.cuda_stream
     st = load().dt_tree_accept(ctypes.byref(tree.as_c()), b, B, target.data_ptr(), out.path.data_ptr(),
                                out.n_accepted.data_ptr(), out.next_token.data_ptr(), s or None)

@@ -185,33 +185,49 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   }
 }
 
-// The splits' parts scaled to their common maximum and summed in order: D / 4 lanes (of a 16-, 32- or
-// 64-lane group) a (row, head), four elements each.  How many splits a row has stands with
-// its sums (1: the tile's one split has written the result), so nothing of the call's
-// geometry is worked out again.
-template <int DT>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int group_lanes) {
+// The splits' parts scaled to their common maximum and summed in order: LANES (16, 32 or 64) lanes a
+// (row, head), four elements each.  The lanes look at the splits' maxima and sums side by side, so a
+// row waits for memory three times, not once a split.  How many splits a row has stands with its sums (1: the tile's
+// one split has written the result), so nothing of the call's geometry is worked out again.
+template <int DT, int LANES>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
+  constexpr int kEach = kMaxSplits / LANES, kDeep = 8;  // splits a lane looks at; parts on their way at once
   const int D = a.cache.D, first = scalar_at(a.chunk.starts, 0), end = scalar_at(a.chunk.starts, a.chunk.batch);
-  const int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) / group_lanes;  // row * heads + head
-  const int row = (int)(x / a.heads), d = threadIdx.x % group_lanes * 4;
-  if (row >= a.chunk.rows || row < first || row >= end || d >= D) return;
+  const int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;  // row * heads + head
+  const int row = (int)(x / a.heads), lane = threadIdx.x % LANES, d = lane * 4;
+  if (row >= a.chunk.rows || row < first || row >= end) return;  // (LANES lanes as one)
   const float2 *ml = a.part_ml + x * (a.splits + 1);
   const int n = min((int)ml[a.splits].x, a.splits);
   if (n <= 1) return;
-  float top = ml[0].x;
-  for (int s = 1; s < n; ++s) top = max2(top, ml[s].x);
-  const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + x * a.splits * D + d);
+  float2 mine[kEach];
+  float top = kFloor;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) mine[e] = ml[min(lane + e * LANES, n - 1)];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) top = max2(top, mine[e].x);
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) top = max2(top, __shfl_xor(top, o));
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) mine[e].x = __builtin_amdgcn_exp2f(mine[e].x - top);
+  const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + x * a.splits * D + min(d, D - 4));
   f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
   float l = 0.0f;
-#pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const f32x4 v = part[(int64_t)s * D / 4];
-    const float2 p = ml[s];
-    const float f = __builtin_amdgcn_exp2f(p.x - top);
-    l += p.y * f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(v[j], f, y[j]);
-  }
+  for (int e = 0; e < kEach; ++e)
+    for (int s0 = e * LANES; s0 < min(n, (e + 1) * LANES); s0 += kDeep) {
+      f32x4 v[kDeep];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) v[j] = part[(int64_t)min(s0 + j, n - 1) * D / 4];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        const float f = s0 + j < n ? __shfl(mine[e].x, (s0 + j) % LANES, LANES) : 0.0f;
+        const float sum = __shfl(mine[e].y, (s0 + j) % LANES, LANES);
+        l = __builtin_fmaf(sum, f, l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __builtin_fmaf(v[j][i], f, y[i]);
+      }
+    }
+  if (d >= D) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   store4<DT>(a, row * a.out.row + (x - (int64_t)row * a.heads) * a.out.head + d, y[0] * inv, y[1] * inv, y[2] * inv,
              y[3] * inv);
@@ -304,7 +320,13 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s
   if (e != hipSuccess || p.splits == 1) return e;
   const int lanes = a.cache.D <= 64 ? 16 : a.cache.D <= 128 ? 32 : 64;
   const int64_t groups = ((int64_t)a.chunk.rows * a.heads * lanes + 255) / 256;
-  (a.dtype == DT_F32 ? join_kernel<DT_F32> : join_kernel<DT_BF16>)<<<(unsigned)groups, 256, 0, s>>>(a, lanes);
+  auto f = a.dtype == DT_F32 ? lanes == 16   ? join_kernel<DT_F32, 16>
+                               : lanes == 32 ? join_kernel<DT_F32, 32>
+                                             : join_kernel<DT_F32, 64>
+           : lanes == 16 ? join_kernel<DT_BF16, 16>
+           : lanes == 32 ? join_kernel<DT_BF16, 32>
+                         : join_kernel<DT_BF16, 64>;
+  f<<<(unsigned)groups, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

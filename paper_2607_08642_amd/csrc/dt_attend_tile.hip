@@ -31,8 +31,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
   const int active = active_splits(a, t);
   if (split >= active) return;
   const int it0 = split * a.split_blocks, it1 = split == active - 1 ? t.n_iter : it0 + a.split_blocks;
-  if (a.nodes > 0) tree_words(a, t, b, words, 64 * NW);
-  __syncthreads();
   const int r = t.r0 + 32 * wave + l32;
   const bool idle = 32 * wave >= tile_rows || t.r0 + 32 * wave >= t.rows;  // (no rows: it copies only)
   const Row w = row_of(a, t, b, idle ? t.r0 : r, words);
@@ -47,15 +45,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
   // kilobytes of a block, each one wave's copy; every wave copies as many (past the last:
   // again one that another wave copies, the same bytes), so all count alike
   constexpr int kPieces = 2 * kPart / 1024, kMine = (kPieces + NW - 1) / NW, kEach = kMine + (DT == DT_F8 ? 1 : 0);
-  int64_t from[kMine];  // of the block's keys
-  int to[kMine];        // in its slot
+  uint32_t from[kMine];  // of the block's keys, this lane's
+  int to[kMine];         // in its slot
 #pragma unroll
   for (int x = 0; x < kMine; ++x) {
     const int p = wave + x * NW, i = p < kPieces ? p : p - kPieces;
-    from[x] = i < kPieces / 2 ? i * 1024 : a.cache.v_off + (i - kPieces / 2) * 1024;
+    from[x] = (i < kPieces / 2 ? i * 1024 : (int)a.cache.v_off + (i - kPieces / 2) * 1024) + lane * 16;
     to[x] = i * 1024;
   }
-  const uint32_t off16 = lane * 16;
   // exponents: lanes 0-7 (mod 16) the keys' 32, lanes 8-15 the values'
   const uint32_t off4 = (lane & 7) * 4 + (lane & 8 ? 1 << a.cache.page_shift : 0);
   Walk<1> walk(a, t, b, head, it0, it1);
@@ -65,19 +62,24 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
       walk.open(a, t, kPart);
       if (DT == DT_F8) copy4(walk.exps, off4, slot + 2 * kPart);
 #pragma unroll
-      for (int x = 0; x < kMine; ++x) copy16(walk.keys + from[x], off16, slot + to[x]);
+      for (int x = 0; x < kMine; ++x) copy16(walk.keys, from[x], slot + to[x]);
     }
     there = there << 1 | (walk.there ? 1u : 0u);
     walk.step(kPart);
   };
 #pragma unroll
   for (int x = 0; x < kAhead; ++x) ask(ring + x * kSlot);
+  if (a.nodes > 0) {
+    tree_words(a, t, b, words, 64 * NW);
+    __syncthreads();
+  }
   int it = it0;
   char *slot = ring, *before = ring + kAhead * kSlot;  // of the present block and of the last
-  // The present block is there (near the end: all that was asked for), for every wave, and every
+  const int steady = it1 - kAhead;  // up to there every turn asks for a block
+  // (bit kAhead - 1 of `there` is the present block before its turn, bit kAhead after it.)  The present block is there (near the end: all that was asked for), for every wave, and every
   // wave has done with the last one, whose slot takes the next.
   auto turn = [&]() {
-    if (it + kAhead <= it1)
+    if (__builtin_expect(it <= steady, 1))
       wait_copies<(kAhead - 1) * kEach>();
     else
       wait_copies<0>();
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     // (a loop of its own for the blocks that every row sees whole: with the masks in it, the
     // sums would move between two sets of registers in every turn)
     const int full = min(full_end(a, t, w, it), it1);
-    for (; it < full && there >> (walk.it - 1 - it) & 1; next()) {
+    for (; it < full && there >> (kAhead - 1) & 1; next()) {
       turn();
       full_block<DT, D>(slot, slot + kPart, slot + 2 * kPart, q, c, lane, m, l, o, nothing);
     }
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
     const int k0 = t.block(it) * kBlk;
     if (!sees_none(a, w, k0))
       masked_block<DT, D>(slot, slot + kPart, slot + 2 * kPart, q,
-                          there >> (walk.it - 1 - it) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
+                          there >> kAhead & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, nothing);
     next();
   }
 #pragma unroll

@@ -676,7 +676,9 @@ class Cache:
         rows, heads = self._rows(self._a, q, "q"), q.shape[1]
         if out is None:
             out = _empty(self._torch, (rows, heads, self.head_dim), self.data_dtype, self._at, stream)
-        if self._rows(self._b, out, "out", heads) != rows:
+            b = self._b
+            b.data, b.row_stride, b.head_stride = out.data_ptr(), heads * self.head_dim, self.head_dim
+        elif self._rows(self._b, out, "out", heads) != rows:
             raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
         o = self._o
         o.scale = self.head_dim ** -0.5 if scale is None else scale
@@ -726,9 +728,8 @@ def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None)
     b, B = tree.tokens.shape
     _want(target, "target", (b, B + 1), torch.int32)
     if out is None:
-        at, i32 = target.device, torch.int32
-        out = Accepted(_empty(torch, (b, B), i32, at, stream), _empty(torch, (b,), i32, at, stream),
-                       _empty(torch, (b,), i32, at, stream))
+        path, n, token = _empty(torch, (b * (B + 2),), torch.int32, target.device, stream).split_with_sizes((b * B, b, b))
+        out = Accepted(path.view(b, B), n, token)
     s = torch._C._cuda_getCurrentRawStream(target.device.index) if stream is None else stream.cuda_stream
     st = load().dt_tree_accept(ctypes.byref(tree.as_c()), b, B, target.data_ptr(), out.path.data_ptr(),
                                out.n_accepted.data_ptr(), out.next_token.data_ptr(), s or None)

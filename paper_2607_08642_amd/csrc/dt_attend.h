@@ -306,15 +306,15 @@ struct QRegs {
   static constexpr int N = DT == DT_F32 ? D / 8 : D / 16;  // 16-byte registers
   u32x4 v[N];
 };
-// (scale < 0: the sign goes into q)
+// (scale < 0: the sign goes into q; elements d0 on)
 template <int DT, int D>
-__device__ __forceinline__ void load_q(const AttendArgs &a, const Tile &t, const Row &w, int head, int h, bool interleave8,
+__device__ __forceinline__ void load_q(const AttendArgs &a, const Tile &t, const Row &w, int head, int h, int d0,
                               QRegs<DT, D> &q) {
-  const int64_t at = (int64_t)(t.q.row0 + w.i) * a.q.row + (int64_t)(head * a.group + w.r % a.group) * a.q.head;
+  const int64_t at = (int64_t)(t.q.row0 + w.i) * a.q.row + (int64_t)(head * a.group + w.r % a.group) * a.q.head + d0;
   // first element of piece n: f32 pieces of 4, bf16 of 8; an 8-bit cache's pieces of 16
   // elements are two operands
   auto first = [&](int n) {
-    return DT == DT_F32 ? (2 * n + h) * 4 : interleave8 ? (2 * (n >> 1) + h) * 16 + 8 * (n & 1) : (2 * n + h) * 8;
+    return DT == DT_F32 ? (2 * n + h) * 4 : DT == DT_F8 ? (2 * (n >> 1) + h) * 16 + 8 * (n & 1) : (2 * n + h) * 8;
   };
   if (a.q.vec) {
 #pragma unroll
@@ -372,7 +372,7 @@ __device__ __forceinline__ u32x4 lds16(const char *p) { return *reinterpret_cast
 // wait behind a branch (four of sixteen scores were read too early), so it stands here, in front of it.
 __device__ __forceinline__ void settle(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
 struct Nothing {  // (no branch)
-  __device__ __forceinline__ void operator()() const {}
+  __device__ __forceinline__ void operator()(f32x16 &) const {}
 };
 
 // S^T of a block: `keys` in LDS in the cache's order (DT_F8: `exps` their 32 exponents).
@@ -461,7 +461,7 @@ __device__ __forceinline__ f32x16 products(const u32x4 (&v)[S], const P &p, f32x
 }
 
 // A block that all rows see whole: keys and values in LDS (DT_F8: with their exponents).
-// between(): after the scores, before the values are needed.
+// between(scores): before the values are needed.
 template <int DT, int D, class F>
 __device__ __forceinline__ void full_block(const char *keys, const char *vals, const char *exps, const QRegs<DT, D> &q,
                                            float c, int lane, float &m, float &l, f32x16 (&o)[D / 32],
@@ -469,7 +469,7 @@ __device__ __forceinline__ void full_block(const char *keys, const char *vals, c
   constexpr int T = D / 32, S = VRegs<DT, D>::S;
   f32x16 s = scores<DT, D>(keys, exps, q, lane);
   if (!std::is_same<F, Nothing>::value) settle(s);
-  between();
+  between(s);
   // the values are asked for before the softmax where registers allow
   constexpr bool kEarly = S * T <= 8;
   VRegs<DT, D> r;
@@ -499,7 +499,7 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
   constexpr int T = D / 32, S = VRegs<DT, D>::S;
   f32x16 sc = scores<DT, D>(keys, exps, q, lane);
   settle(sc);
-  between();
+  between(sc);
   float p[16];
   softmax_block<true>(sc, seen, c, m, l, o, p);
   const POperand<DT, true> pf(p, exps + 32, seen, lane >> 5);

@@ -16,17 +16,25 @@ using namespace att;
 
 constexpr int kStreamRows = 32;
 
+// Waves that walk a block together, each with its share of the head's elements: two where there are
+// 256 (by itself a wave's queries and sums leave too few registers; two kv heads of four, one token,
+// single waves and pairs: 32 sequences of 4,096 in fp32 384 and 193 us, bf16 66 and 72, 8 bits 40 and 38; one of
+// 300 in bf16 19.5 and 14.6).
+constexpr int stream_share(int D) { return D == 256 ? 2 : 1; }
+// Blocks that a workgroup works on at a time.
+constexpr int stream_blocks(int D) { return D <= 128 ? 4 : 2; }
+
 // Shape of a workgroup: waves, and blocks in a wave's ring, for at most 144 KB of LDS.
 template <int DT, int D>
 struct Stream {
-  static constexpr int ES = DT == DT_F32 ? 4 : DT == DT_BF16 ? 2 : 1;
-  static constexpr int kPart = kBlk * D * ES;                       // a block's keys, or values
+  static constexpr int P = stream_share(D), DH = D / P, W = stream_blocks(D), kWaves = W * P;
+  static constexpr int kPart = kBlk * DH * elem_bytes(DT);          // a wave's keys of a block, or values
   static constexpr int kExps = DT == DT_F8 ? 256 : 0;               // its exponents, as copied
-  static constexpr int kWaves = kPart <= 16384 ? 4 : 2;
   static constexpr int kFit = 147456 / (kWaves * (2 * kPart + kExps));
   static constexpr int kSlots = kFit > 4 ? 4 : kFit;
   static constexpr int kLds = kWaves * kSlots * (2 * kPart + kExps);
   static constexpr int kOps = kPart / 1024;                         // copies of a part
+  static constexpr int kSwap = P > 1 ? kWaves * 4096 : 16;          // scores on their way between two waves
 };
 
 // grid: kv head (fastest: the workgroups of a head share an XCD's cache where there are
@@ -34,12 +42,13 @@ struct Stream {
 template <int DT, int D>
 __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(AttendArgs a, int tiles) {
   using St = Stream<DT, D>;
-  constexpr int T = D / 32, ES = St::ES, W = St::kWaves, NS = St::kSlots;
+  constexpr int P = St::P, DH = St::DH, T = DH / 32, W = St::W, WT = St::kWaves, NS = St::kSlots;
   __shared__ uint32_t words[kStreamRows * kTreeWords];
   __shared__ float2 ml[W][32];  // maximum and sum
   __shared__ __align__(16) char ring[St::kLds];
+  __shared__ __align__(16) char swap[St::kSwap];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane >> 5, l32 = lane & 31;
+  const int h = lane >> 5, l32 = lane & 31, which = wave / P, share = wave % P;  // block of the turn, part of it
   const int head = blockIdx.x % a.cache.kv, tile = blockIdx.x / a.cache.kv % tiles,
             split = blockIdx.x / (a.cache.kv * tiles), b = blockIdx.y;
   Tile t;
@@ -51,8 +60,8 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   // ---- its rows (q asked for before the blocks: it comes first)
   const Row w = row_of(a, t, b, t.r0 + l32, words);
   const float c = __builtin_fabsf(a.scale_log2e);
-  QRegs<DT, D> q;
-  load_q<DT, D>(a, t, w, head, h, DT == DT_F8, q);
+  QRegs<DT, DH> q;
+  load_q<DT, DH>(a, t, w, head, h, share * DH, q);
 
   f32x16 o[T];
 #pragma unroll
@@ -60,7 +69,7 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   float m = kFloor, l = 0.0f;
 
   // ---- the wave's blocks: copies into its ring
-  char *mine = ring + wave * (St::kLds / W);
+  char *mine = ring + wave * (St::kLds / WT);
   constexpr int kSlot = 2 * St::kPart + St::kExps;
   const uint32_t off16 = lane * 16;
   // exponents: lanes 0-7 (mod 16) the keys' 32, lanes 8-15 the values'
@@ -68,31 +77,36 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   auto copy_keys = [&](const char *keys, const char *exps, char *slot) {
     if (DT == DT_F8) copy4(exps, off4, slot + 2 * St::kPart);
 #pragma unroll
-    for (int x = 0; x < St::kOps; ++x) copy16(keys + x * 1024, off16, slot + x * 1024);
+    for (int x = 0; x < St::kOps; ++x) copy16(keys + share * St::kPart + x * 1024, off16, slot + x * 1024);
   };
   auto copy_vals = [&](const char *keys, char *slot) {
 #pragma unroll
-    for (int x = 0; x < St::kOps; ++x) copy16(keys + a.cache.v_off + x * 1024, off16, slot + St::kPart + x * 1024);
+    for (int x = 0; x < St::kOps; ++x) {
+      const int group = x * 1024 / (DH * 16), in = x * 1024 % (DH * 16);  // (the tokens of 16 bytes: one run of D)
+      static_assert(P == 1 || DH * 16 % 1024 == 0, "");
+      copy16(keys + a.cache.v_off + (P == 1 ? x * 1024 : group * D * 16 + share * DH * 16 + in), off16,
+             slot + St::kPart + x * 1024);
+    }
   };
   constexpr int kK = St::kOps + (DT == DT_F8 ? 1 : 0), kV = St::kOps;
-  int it = it0 + wave;
+  int it = it0 + which;
   Walk<W> walk(a, t, b, head, it, it1);
   uint32_t there = 0;  // bit x: block (the last one asked for) - x W has a page
   auto asked = [&]() {
     there = there << 1 | (walk.there ? 1u : 0u);
-    walk.step(St::kPart);
+    walk.step(P * St::kPart);
   };
 #pragma unroll
   for (int x = 0; x < NS; ++x) {
     if (!walk.done()) {
-      walk.open(a, t, St::kPart);
+      walk.open(a, t, P * St::kPart);
       copy_keys(walk.keys, walk.exps, mine + x * kSlot);
       copy_vals(walk.keys, mine + x * kSlot);
     }
     asked();
   }
   if (a.nodes > 0) {
-    tree_words(a, t, b, words, 64 * W);
+    tree_words(a, t, b, words, 64 * WT);
     __syncthreads();
   }
 
@@ -100,17 +114,39 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   // that is on its way; else when nothing is); as they are done with, their place takes the
   // keys of block it + NS W; the same with the values.
   char *slot = mine;
+  // A pair's scores are the sums of its waves' (each takes the same sum).  Every wave comes by once a turn.
+  auto meet_scores = [&](f32x16 &s) __attribute__((always_inline)) {
+    if constexpr (P > 1) {
+      wait_copies<63>();
+      __builtin_amdgcn_s_barrier();  // (the last turn's are read)
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4 *>(swap + wave * 4096 + i * 1024 + lane * 16) =
+            f32x4{s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]};
+      wait_copies<63>();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 z = *reinterpret_cast<const f32x4 *>(swap + (wave ^ 1) * 4096 + i * 1024 + lane * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * i + j] += z[j];
+      }
+    }
+  };
   auto turn = [&](auto block_step) {
     const bool more = !walk.done();
     if (it + (NS - 1) * W < it1)
       wait_copies<kV + (NS - 1) * (kK + kV)>();
     else
       wait_copies<0>();
-    auto between = [&]() __attribute__((always_inline)) {
+    auto between = [&](f32x16 &s) __attribute__((always_inline)) {
+      meet_scores(s);
       wait_copies<63>();  // (LDS reads done)
       // (DT_F8: the values' exponents come with the keys, so those wait until the values are done with)
       if (more) {
-        walk.open(a, t, St::kPart);
+        walk.open(a, t, P * St::kPart);
         if (DT != DT_F8) copy_keys(walk.keys, walk.exps, slot);
         wait_copies<(NS - 1) * (kK + kV) + (DT != DT_F8 ? kK : 0)>();
       } else {
@@ -133,17 +169,23 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
     const int full = min(full_end(a, t, w, it), it1);
     while (it < full && there >> (NS - 1) & 1)
       turn([&](const auto &between) __attribute__((always_inline)) {
-        full_block<DT, D>(slot, slot + St::kPart, slot + 2 * St::kPart, q, c, lane, m, l, o, between);
+        full_block<DT, DH>(slot, slot + St::kPart, slot + 2 * St::kPart, q, c, lane, m, l, o, between);
       });
     if (it >= it1) break;
     turn([&](const auto &between) __attribute__((always_inline)) {
       const int k0 = t.block(it) * kBlk;
+      f32x16 none = zero16();
       if (sees_none(a, w, k0))
-        between();
+        between(none);
       else
-        masked_block<DT, D>(slot, slot + St::kPart, slot + 2 * St::kPart, q,
-                            there >> (NS - 1) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, between);
+        masked_block<DT, DH>(slot, slot + St::kPart, slot + 2 * St::kPart, q,
+                             there >> (NS - 1) & 1 ? seen_word(a, t, w, k0) >> (4 * h) : 0, c, lane, m, l, o, between);
     });
+  }
+
+  if (P > 1 && (it1 - it0 - 1) % W < which) {  // (one block fewer than the others)
+    f32x16 none = zero16();
+    meet_scores(none);
   }
 
   // ---- the waves' results meet in LDS as rows; all threads scale them to the common maximum, sum
@@ -151,7 +193,7 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
 #pragma unroll
   for (int n = 0; n < T; ++n) settle(o[n]);
   const float2 lh = halves(l);
-  if (h == 0) ml[wave][l32] = make_float2(m, lh.x + lh.y);
+  if (h == 0 && share == 0) ml[which][l32] = make_float2(m, lh.x + lh.y);
   // (every wave is past its last block: the rings are free.  Rows of D floats, apart by one
   // 16-byte column where that fits.)
   constexpr int kRow = W * 32 * (D + 4) * 4 <= St::kLds ? D + 4 : D;
@@ -162,12 +204,12 @@ __global__ __launch_bounds__((64 * Stream<DT, D>::kWaves)) void stream_kernel(At
   for (int n = 0; n < T; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4 *>(meet + (wave * 32 + l32) * kRow + 32 * n + 8 * i + 4 * h) =
+      *reinterpret_cast<f32x4 *>(meet + (which * 32 + l32) * kRow + share * DH + 32 * n + 8 * i + 4 * h) =
           f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
   __syncthreads();
   const int rows = min(kStreamRows, t.rows - t.r0);
 #pragma unroll 1
-  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * W) {
+  for (int x = threadIdx.x; x < rows * (D / 4); x += 64 * WT) {
     const int r = x / (D / 4), d = x % (D / 4) * 4, i = (t.r0 + r) / a.group, hq = head * a.group + t.r0 + r - i * a.group;
     float top = ml[0][r].x, sum = 0.0f;
 #pragma unroll
@@ -240,14 +282,12 @@ hipError_t launch_stream(const AttendArgs &a, const AttendPlan &p, hipStream_t s
            : a.cache.D == 96  ? stream_kernel<DT, 96>
            : a.cache.D == 128 ? stream_kernel<DT, 128>
                               : stream_kernel<DT, 256>;
-  f<<<grid, 64 * p.waves, 0, s>>>(a, p.tiles);
+  f<<<grid, 64 * p.waves * stream_share(a.cache.D), 0, s>>>(a, p.tiles);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// (as Stream::kWaves)
-static int stream_waves(int dtype, int D) { return kBlk * D * elem_bytes(dtype) <= 16384 ? 4 : 2; }
 
 AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int heads, int window, int sinks, int nodes) {
   const int group = heads / c.kv, rows = k.max_chunk * group, sets = (rows + 31) / 32;
@@ -257,7 +297,7 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
   // 16,384 tokens: 889 us against 925 with four); else four (eight ragged chunks of up to 509: 67
   // against 86, a chunk of 2,047 under a window: 23 against 29).
   p.stream = dtype == DT_F32 || sets == 1;
-  p.waves = p.stream ? stream_waves(dtype, c.D) : k.batch == 1 && (int64_t)c.kv * ((sets + 7) / 8) >= 512 ? 8 : 4;
+  p.waves = p.stream ? stream_blocks(c.D) : k.batch == 1 && (int64_t)c.kv * ((sets + 7) / 8) >= 512 ? 8 : 4;
   const int full = p.stream ? 1 : p.waves;
   p.tiles = (sets + full - 1) / full;
   p.tile_rows = (sets + p.tiles - 1) / p.tiles * 32;  // (even tiles: 9 sets of 32 rows are 3 + 3 + 3, not 4 + 4 + 1)

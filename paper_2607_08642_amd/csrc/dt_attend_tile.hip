@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
   const Row w = row_of(a, t, b, idle ? t.r0 : r, words);
   const float c = __builtin_fabsf(a.scale_log2e);
   QRegs<DT, D> q;
-  load_q<DT, D>(a, t, w, head, h, DT == DT_F8, q);
+  load_q<DT, D>(a, t, w, head, h, 0, q);
   f32x16 o[T];
 #pragma unroll
   for (int n = 0; n < T; ++n) o[n] = zero16();

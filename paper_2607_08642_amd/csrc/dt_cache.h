@@ -42,7 +42,7 @@ struct RowsView {
   int vec;            // 16-byte aligned throughout
 };
 
-inline int elem_bytes(int dtype) { return dtype == DT_F32 ? 4 : dtype == DT_BF16 ? 2 : 1; }
+constexpr int elem_bytes(int dtype) { return dtype == DT_F32 ? 4 : dtype == DT_BF16 ? 2 : 1; }
 inline int data_dtype(int cache_dtype) { return cache_dtype == DT_F32 ? DT_F32 : DT_BF16; }
 
 // bytes of a head page

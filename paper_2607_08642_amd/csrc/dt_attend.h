@@ -286,6 +286,31 @@ __device__ __forceinline__ uint32_t bad_bits(uint32_t v) {
   const uint32_t t = ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
   return (t >> 7) * 0xffu;
 }
+// Whether any of many words has a non-finite element: two or three instructions a word.
+template <int DT>
+struct AnyBad {
+  uint32_t acc = 0;
+  __device__ __forceinline__ void look(uint32_t v) {
+    if constexpr (DT == DT_F32) {
+      acc = max(acc, v & 0x7f800000u);
+    } else if constexpr (DT == DT_BF16) {  // (the largest exponent of either half)
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      u16x2 x, y;
+      const uint32_t e = v & 0x7f807f80u;
+      __builtin_memcpy(&x, &acc, 4);
+      __builtin_memcpy(&y, &e, 4);
+      x = __builtin_elementwise_max(x, y);
+      __builtin_memcpy(&acc, &x, 4);
+    } else {
+      acc |= (v & 0x7f7f7f7fu) + 0x01010101u;
+    }
+  }
+  __device__ __forceinline__ bool any() const {
+    if (DT == DT_F32) return acc == 0x7f800000u;
+    if (DT == DT_BF16) return (acc & 0xffffu) == 0x7f80u || acc >> 16 == 0x7f80u;
+    return (acc & 0x80808080u) != 0;
+  }
+};
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -413,6 +438,19 @@ template <int DT, int D>
 __device__ __forceinline__ const char *v_at(const char *vals, int s, int t, int lane) {
   return vals + ((lane >> 5) * D + (lane & 31)) * 16 + (2 * s * D + 32 * t) * 16;
 }
+// 2^(byte j of w - 127): byte j to the exponent's place (one instruction, where a shift and a mask would do)
+__device__ __forceinline__ float power_of(uint32_t w, int j) {
+  float e;
+  if (j == 0)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(e) : "v"(23), "v"(w));
+  else if (j == 1)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(e) : "v"(23), "v"(w));
+  else if (j == 2)
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(e) : "v"(23), "v"(w));
+  else
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(e) : "v"(23), "v"(w));
+  return e;
+}
 // The probabilities as the operand of those products (DT_F8: times the tokens' powers of two, `exps`
 // in LDS: exact).
 template <int DT, bool MASKED>
@@ -425,7 +463,7 @@ struct POperand {
         const uint32_t w = *reinterpret_cast<const uint32_t *>(exps + 8 * t + 4 * h);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float e = __uint_as_float((j == 3 ? w >> 1 : w << (23 - 8 * j)) & 0x7f800000u);
+          const float e = power_of(w, j);
           p[4 * t + j] = MASKED && !(seen >> reg_token(4 * t + j) & 1) ? 0.0f : p[4 * t + j] * e;
         }
       }
@@ -503,24 +541,24 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
   float p[16];
   softmax_block<true>(sc, seen, c, m, l, o, p);
   const POperand<DT, true> pf(p, exps + 32, seen, lane >> 5);
-  uint32_t bad = 0;
+  AnyBad<DT> bad;
 #pragma unroll
   for (int n = 0; n < S * T; ++n) {
     const u32x4 v = lds16(v_at<DT, D>(vals, n / T, n % T, lane));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad |= bad_bits<DT>(v[i]);
+    for (int i = 0; i < 4; ++i) bad.look(v[i]);
     if (n % 8 == 7) __builtin_amdgcn_sched_barrier(0);  // (eight pieces at a time: registers)
   }
-  const bool any = __ballot(bad != 0) != 0;
-  float sf[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) sf[i] = seen >> reg_token(i) & 1 ? 1.0f : 0.0f;
+  const bool any = __ballot(bad.any()) != 0;
 #pragma unroll
   for (int t = 0; t < T; ++t) {
     u32x4 v[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) v[s] = lds16(v_at<DT, D>(vals, s, t, lane));
-    if (any) {
+    if (__builtin_expect(any, 0)) {
+      float sf[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sf[i] = seen >> reg_token(i) & 1 ? 1.0f : 0.0f;
       u32x4 one[S];
 #pragma unroll
       for (int s = 0; s < S; ++s)

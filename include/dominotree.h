@@ -394,7 +394,7 @@ typedef struct {
   int layers;    /* >= 1 */
   int pages;     /* >= 1, in each layer */
   int page_size; /* tokens: 32, 64, 128 or 256 */
-  int kv_heads;  /* >= 1 */
+  int kv_heads;  /* 1 .. 4096 */
   int head_dim;  /* D: 64, 96, 128 or 256 */
   int dtype;     /* DT_F32, DT_BF16 or DT_F8; the data type of k, v, q and out is DT_F32
                     for DT_F32 and DT_BF16 for the others */
@@ -431,7 +431,8 @@ typedef struct {
 /* Bytes of a cache (data is not looked at). */
 dt_status dt_cache_size(const dt_cache *cache, size_t *bytes);
 
-/* Write the chunk's keys and values ([rows, kv_heads, D], the data type) into a layer. */
+/* Write the chunk's keys and values ([rows, kv_heads, D], the data type) into a layer.
+ * ((max_chunk / 32 + 3) * kv_heads < 2^24, here and in dt_cache_read.) */
 dt_status dt_cache_append(const dt_cache *cache, int layer, const dt_chunk *chunk, const dt_rows *k,
                           const dt_rows *v, void *stream);
 
@@ -465,12 +466,13 @@ dt_status dt_attend_workspace_size(const dt_cache *cache, const dt_chunk *chunk,
 /* Attention of the chunk's queries q [rows, heads, D] over a layer of the cache:
  *   out[i, h] = sum_j p_j v_j,  p = softmax over the visible j of scale q[i, h] . k_j,
  * head h reading kv head h / (heads / kv_heads).  heads is a multiple of kv_heads, at most
- * 1024 heads per kv head.  The chunk's own keys and values have to be in the cache.
+ * 1024 heads per kv head, max_chunk * heads <= 2^28.  The chunk's own keys and values have to be in the cache.
  * A row that sees nothing gives zeros; NaN and infinities of keys and values that a
  * row does not see leave it untouched, those it sees make its result (or those
  * components of it) non-finite.  Scores, softmax and sums are fp32; with bf16
  * data the probabilities are rounded to bf16 before their product with the
- * values.  q and out may have different strides and must not overlap.
+ * values.  scale q . k has to stay below 2^30 in magnitude (an fp32 score beyond that is
+ * rounded by whole powers of two of its probability).  q and out may have different strides and must not overlap.
  *   workspace: >= dt_attend_workspace_size bytes, 256-byte aligned (NULL where 0);
  *   not to be shared by calls that can overlap. */
 dt_status dt_cache_attend(const dt_cache *cache, int layer, const dt_chunk *chunk, int heads,
@@ -484,14 +486,15 @@ dt_status dt_cache_attend(const dt_cache *cache, int layer, const dt_chunk *chun
  *           (column i + 1), its argmax or a sample;
  *   path: [batch, B] the accepted nodes in order, then -1;
  *   n_accepted: [batch]; next_token: [batch] the target's token at the last of them.
- * 1 <= B <= 256. */
+ * 1 <= B <= 256, batch < 2^24. */
 dt_status dt_tree_accept(const dt_tree *tree, int batch, int B, const int32_t *target, int32_t *path,
                          int32_t *n_accepted, int32_t *next_token, void *stream);
 
 /* Move the rows of the accepted nodes together, in every layer: with N nodes as the last
  * rows of each chunk, node path[b][i] to the place of node i for i < n_accepted[b].
  * Rows past those keep what they hold.  path ([batch, N]) rises along each row, as
- * dt_tree_accept writes it; entries below their index or out of range are left out. */
+ * dt_tree_accept writes it; entries below their index or out of range are left out.
+ * 1 <= N <= 256, N <= max_chunk, layers * kv_heads < 2^24. */
 dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int nodes, const int32_t *path,
                           const int32_t *n_accepted, void *stream);
 

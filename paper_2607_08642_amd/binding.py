@@ -652,6 +652,8 @@ class Cache:
         key = (c.batch, rows, c.max_chunk, c.max_len, c.table_width, heads, opts.window, opts.sinks, opts.tree_nodes)
         n = self._sizes.get(key)
         if n is None:
+            if len(self._sizes) >= 4096:   # (shapes of a long-running program)
+                self._sizes.clear()
             b = ctypes.c_size_t()
             _check(self._lib.dt_attend_workspace_size(self._ref, chunk.as_c(rows), heads, ctypes.byref(opts),
                                                       ctypes.byref(b)))

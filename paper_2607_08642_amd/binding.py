@@ -533,6 +533,7 @@ class Chunk:
         self.table = _want(table, "table", (batch, width), torch.int32)
         self.tensors = starts, lens, table
         self.batch, self.max_chunk, self.max_len = batch, max_chunk, max_len
+        self.sizes = (batch, max_chunk, max_len, width)
         self._c = dt_chunk(batch, 0, max_chunk, max_len, width, starts.data_ptr(), lens.data_ptr(), table.data_ptr())
         self._ref = ctypes.byref(self._c)
 
@@ -582,6 +583,7 @@ class Cache:
         self._device = self._at.index
         self._a, self._b, self._o = dt_rows(), dt_rows(), dt_attend_options()   # a call's arguments
         self._aref, self._bref, self._oref = (ctypes.byref(x) for x in (self._a, self._b, self._o))
+        self._scale = head_dim ** -0.5
         self._sizes = {}   # workspace bytes of a shape
         self._ws = {}      # a workspace of each stream
 
@@ -648,8 +650,10 @@ class Cache:
         return out
 
     def workspace_size(self, chunk: Chunk, rows: int, heads: int, opts: dt_attend_options) -> int:
-        c = chunk._c
-        key = (c.batch, rows, c.max_chunk, c.max_len, c.table_width, heads, opts.window, opts.sinks, opts.tree_nodes)
+        return self._workspace_size(chunk, rows, heads, opts, opts.window, opts.sinks, opts.tree_nodes)
+
+    def _workspace_size(self, chunk: Chunk, rows: int, heads: int, opts: dt_attend_options, window, sinks, nodes) -> int:
+        key = (chunk.sizes, rows, heads, window, sinks, nodes)
         n = self._sizes.get(key)
         if n is None:
             if len(self._sizes) >= 4096:   # (shapes of a long-running program)
@@ -675,25 +679,29 @@ class Cache:
         mask [batch, N, N] uint8 (Tree.mask): the last N rows of every chunk are a tree's nodes, depth
         [batch, N] (Tree.depth) their depths, needed with a window.
         """
-        rows, heads = self._rows(self._a, q, "q"), q.shape[1]
+        rows, heads, d = self._rows(self._a, q, "q"), q.shape[1], self.head_dim
         if out is None:
-            out = _empty(self._torch, (rows, heads, self.head_dim), self.data_dtype, self._at, stream)
+            if stream is None and q.is_contiguous():
+                out = self._torch.empty_like(q)
+            else:
+                out = _empty(self._torch, (rows, heads, d), self.data_dtype, self._at, stream)
             b = self._b
-            b.data, b.row_stride, b.head_stride = out.data_ptr(), heads * self.head_dim, self.head_dim
+            b.data, b.row_stride, b.head_stride = out.data_ptr(), heads * d, d
         elif self._rows(self._b, out, "out", heads) != rows:
             raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
         o = self._o
-        o.scale = self.head_dim ** -0.5 if scale is None else scale
-        o.window, o.sinks, o.tree_nodes = window, sinks, 0
+        o.scale = self._scale if scale is None else scale
+        o.window, o.sinks, nodes = window, sinks, 0
         o.mask = o.depth = None
         if mask is not None:
-            n = o.tree_nodes = mask.shape[-1]
-            o.mask = _want(mask, "mask", (chunk.batch, n, n), self._torch.uint8).data_ptr()
+            nodes = mask.shape[-1]
+            o.mask = _want(mask, "mask", (chunk.batch, nodes, nodes), self._torch.uint8).data_ptr()
             if depth is not None:
-                o.depth = _want(depth, "depth", (chunk.batch, n), self._torch.int32).data_ptr()
+                o.depth = _want(depth, "depth", (chunk.batch, nodes), self._torch.int32).data_ptr()
+        o.tree_nodes = nodes
         s = self._stream(stream)
         if workspace is None:
-            n = self.workspace_size(chunk, rows, heads, o)
+            n = self._workspace_size(chunk, rows, heads, o, window, sinks, nodes)
             if n:
                 workspace = self._workspace(n, s, stream)
         ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())

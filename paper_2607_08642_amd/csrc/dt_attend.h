@@ -441,14 +441,19 @@ __device__ __forceinline__ const char *v_at(const char *vals, int s, int t, int 
 // 2^(byte j of w - 127): byte j to the exponent's place (one instruction, where a shift and a mask would do)
 __device__ __forceinline__ float power_of(uint32_t w, int j) {
   float e;
+#define DT_SHIFT(n)                                                                                               \
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_" #n \
+      : "=v"(e)                                                                                                   \
+      : "v"(23), "v"(w))
   if (j == 0)
-    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(e) : "v"(23), "v"(w));
+    DT_SHIFT(0);
   else if (j == 1)
-    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(e) : "v"(23), "v"(w));
+    DT_SHIFT(1);
   else if (j == 2)
-    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(e) : "v"(23), "v"(w));
+    DT_SHIFT(2);
   else
-    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(e) : "v"(23), "v"(w));
+    DT_SHIFT(3);
+#undef DT_SHIFT
   return e;
 }
 // The probabilities as the operand of those products (DT_F8: times the tokens' powers of two, `exps`

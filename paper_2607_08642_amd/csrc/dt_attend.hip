@@ -15,8 +15,9 @@
 // What bounds it: memory, from some thousand tokens a sequence on.  One token of 32 sequences of
 // 2,580 to 8,192 (8 kv heads of 128, bf16): 709 MB in 133 us, 5.3 TB/s (a copy of 2 GiB: 4.7, a sum: 4.0).  Below that the
 // time of a chain: arguments, lengths, page, keys, the meeting of the waves (37 tokens of two heads
-// of 64 in fp32: 7.6 us).  In fp32 the products of 32 rows are taken whatever the rows that are there: one
-// token of 32 sequences of 4,096, 4 kv heads of 128: 3.5 TB/s.
+// of 64 in fp32: 7.4 us).  In fp32 the products of 32 rows are taken whatever the rows that are there: one
+// token of 32 sequences of 4,096, 4 kv heads of 128: 110 us, 4.9 TB/s; 1,024 rows of 32 heads of 128 over 4,096: 539 us, 112
+// TFLOP/s of the 153 of a large product (one wave a SIMD: its waits are not filled).
 #include <math.h>
 
 #include "dt_attend.h"
@@ -29,8 +30,8 @@ constexpr int kStreamRows = 32;
 
 // Waves that walk a block together, each with its share of the head's elements: two where there are
 // 256 (by itself a wave's queries and sums leave too few registers; two kv heads of four, one token,
-// single waves and pairs: 32 sequences of 4,096 in fp32 384 and 193 us, bf16 66 and 72, 8 bits 40 and 38; one of
-// 300 in bf16 19.5 and 14.6).
+// single waves and pairs in the same splits: 32 sequences of 4,096 in fp32 384 and 193 us, bf16 66 and 72, 8 bits
+// 40 and 38; one of 300 in bf16 19.5 and 14.6; with splits for pairs fp32 119, bf16 56).
 constexpr int stream_share(int D) { return D == 256 ? 2 : 1; }
 // Blocks that a workgroup works on at a time.
 constexpr int stream_blocks(int D) { return D <= 128 ? 4 : 2; }
@@ -323,9 +324,10 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
     most = near < all ? (int)near : all;
   }
   // The number of splits whose estimate is least, in units of one block's time in a workgroup by
-  // itself (0.5 us with shared blocks; 1.1 us for one block of each wave):
-  //  - a workgroup takes its blocks and 5 to start and end; two on a CU take 1.5 times as long a
-  //    block, and where memory bounds the chip (5.2 TB/s) a block takes what its bytes do;
+  // itself (0.5 us with shared blocks; 1.1 us for one block of each wave, 1.6 where pairs share them, in fp32 2.5 to 4.5 with 64 to
+  // 128 elements a wave; with 1.1 there too, the choice took 1.3 times as long as the best of eight shapes):
+  //  - a workgroup takes its blocks and 2.5 or 5.5 us to start and end; two on a CU take 1.5 times as long a
+  //    block, and from half the CUs on a block takes at least what its bytes do (5.2 TB/s for all of them);
   //  - one sequence: equal workgroups in whole rounds of the chip's slots.  A batch: its lengths
   //    are known on the device only; 0.6 of the longest's blocks on average are assumed, and of the
   //    chunks what the rows say; they fill gaps, with a tail of a third of a workgroup (powers of
@@ -333,7 +335,11 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
   //  - the join: its launch, and the parts written and read.
   const int64_t wgs = (int64_t)c.kv * p.tiles * k.batch;
   const bool paired = !p.stream && p.waves == 4 && c.D <= 128;
-  const double unit_us = p.stream ? 1.1 : 0.5;
+  const double base_us = p.stream ? 1.1 : 0.5;
+  const double unit_us = dtype == DT_F32                       ? 0.5 + 0.031 * c.D / stream_share(c.D)
+                         : p.stream && stream_share(c.D) > 1 ? 1.6
+                                                             : base_us;
+  const double start = 5.0 * base_us / unit_us;
   const int unit = p.stream ? p.waves : 1;  // blocks that a workgroup takes at a time
   const double memory = unit * 2.0 * kBlk * c.D * elem_bytes(dtype) * 256 / 5.2e6 / unit_us;
   const double share = k.batch == 1 ? 1.0 : 0.6 * k.rows / ((double)k.batch * k.max_chunk);
@@ -346,16 +352,16 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
     const int n = (most + blocks - 1) / blocks;
     const double cus = wgs * n * share / 256, turns = (double)blocks / unit;
     double slow = paired && cus > 1.0 ? 1.5 : 1.0;
-    if (p.stream && cus > 0.5 && memory > slow) slow = memory;
-    double cost = turns + 5.0;
+    if (p.stream && cus > 0.5) slow = fmax(slow, memory * fmin(cus, 1.0));
+    double cost = turns + start;
     const double rounds = paired ? cus / 2 : cus;
     if (k.batch == 1) {
-      cost = ceil(rounds) * (turns * slow + 5.0);
+      cost = ceil(rounds) * (turns * slow + start);
     } else {
-      const double filled = rounds * (turns * slow + 5.0) + 0.3 * cost;
+      const double filled = rounds * (turns * slow + start) + 0.3 * cost;
       cost = filled > cost ? filled : cost;
     }
-    if (n > 1) cost += 4.0 + 0.1 * n + part * n * (k.batch == 1 ? 1.0 : 0.7);
+    if (n > 1) cost += (4.0 + 0.1 * n) * base_us / unit_us + part * n * (k.batch == 1 ? 1.0 : 0.7);
     if (cost < best * 0.98) {
       best = cost;
       p.splits = n;

@@ -1,9 +1,9 @@
 // Attention over the paged cache for many rows (chunks of prompts, trees): bf16 data.
 //
-// The mathematics is the one-pass softmax of dt_attend.hip; a workgroup of NW waves holds 32 rows a wave of one kv head; all its waves walk the same
-// key blocks, which every wave copies its share of from memory into a ring of LDS slots,
-// three blocks ahead and past the registers.  The slots hold the blocks in the cache's
-// order, so a wave's operand is 1,024 contiguous bytes and no bank is hit twice.
+// The mathematics is the one-pass softmax of dt_attend.hip; a workgroup of NW waves holds 32 rows
+// a wave of one kv head; all its waves walk the same key blocks, which every wave copies its share
+// of from memory into a ring of LDS slots, three blocks ahead and past the registers.  The slots hold
+// the blocks in the cache's order, so a wave's operand is 1,024 contiguous bytes and no bank is hit twice.
 //
 // What bounds it: the issue of instructions.  A wave by itself takes about five cycles an instruction,
 // and a block of 32 tokens of 128 is 16 matrix products (512 cycles of the matrix unit) among
@@ -89,7 +89,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((
   int it = it0;
   char *slot = ring, *before = ring + kAhead * kSlot;  // of the present block and of the last
   const int steady = it1 - kAhead;  // up to there every turn asks for a block
-  // (bit kAhead - 1 of `there` is the present block before its turn, bit kAhead after it.)  The present block is there (near the end: all that was asked for), for every wave, and every
+  // (bit kAhead - 1 of `there` is the present block before its turn, bit kAhead after it.)
+  // A turn: the present block is there (near the end: all that was asked for), for every wave, and every
   // wave has done with the last one, whose slot takes the next.
   auto turn = [&]() {
     if (__builtin_expect(it <= steady, 1))

@@ -3,7 +3,8 @@
 //
 // All are copies: bound by memory traffic for prompts (append and read of four prompts of 11,437 to 16,384,
 // 8 kv heads of 128: 85 and 58 us for 342 MB each in 8 bits, 4.0 and 5.9 TB/s; bf16 and fp32 together
-// 5.0 to 5.2 TB/s; a copy: 4.7), by latency for the few rows of a decoding step (3.5 to 5 us a launch).  A workgroup of append and read takes one block of 32
+// 5.0 to 5.2 TB/s; a copy: 4.7), by latency for the few rows of a decoding step (3.5 to 5 us a launch).
+// A workgroup of append and read takes one block of 32
 // tokens of one kv head, keys and values (layout: dt_cache.h), through two LDS tiles of
 // 32 rows: rows of the caller's tensors are touched in runs of 128 bytes (eight lanes a
 // row), pieces of the cache in runs of 512 bytes and more.  Values change sides in LDS two
@@ -357,8 +358,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(CacheView c, ChunkView k
   }
 }
 
-// Bound by latency (2.3 us at one tree of 64 nodes, 3.8 at 32 trees of 16).  One wave per tree: at every step the lanes look for the child among their nodes (four
-// each at most); the lowest index counts.
+// Bound by latency (2.3 us at one tree of 64 nodes, 3.8 at 32 trees of 16).  One wave per tree: at every
+// step the lanes look for the child among their nodes (four each at most); the lowest index counts.
 __global__ __launch_bounds__(64) void accept_kernel(const int32_t *tokens, const int32_t *parents,
                                                     const int32_t *n_nodes, int B, const int32_t *target,
                                                     int32_t *path, int32_t *n_accepted, int32_t *next_token) {

@@ -9,7 +9,7 @@
 // and a block of 32 tokens of 128 is 16 matrix products (512 cycles of the matrix unit) among
 // some 190 others in bf16, 280 in 8 bits (64 of them widen codes, 36 bring in the values' scales): a
 // block takes 0.5 us of a workgroup by itself, 0.65 in 8 bits, and two workgroups a CU fill each other's
-// gaps.  4,096 rows of 32 heads over 16,384 tokens: 870 to 890 us, 1,090 TFLOP/s of the 1,245 of a large
+// gaps.  4,096 rows of 32 heads over 16,384 tokens: 870 to 900 us, 1,070 to 1,100 TFLOP/s of the 1,245 of a large
 // product; in 8 bits 1,029 us.  Eight ragged chunks of 16 heads of 64 in 8 bits: 68 us, 260
 // TFLOP/s (the longest tile's blocks, one after another); 65 rows of 32 heads over 30,011 tokens in 8 bits: 70 us, of which
 // about 20 do not depend on the length (start, masked blocks, parts, join).

@@ -232,7 +232,8 @@ __device__ __forceinline__ void rescale(f32x16 (&o)[T], float f) {
 }
 
 // One block's scores into probabilities (masked: bits of `seen`, already shifted by 4 h).
-// m: the reference that exponents are taken against, l: this lane's part of the sum.  m
+// m: the reference that exponents are taken against, l: this lane's part of the sum (which the
+// probabilities join as they become an operand: POperand).  m
 // is raised, and what was summed scaled, only once a row's maximum lies more than kSlack
 // above it: probabilities up to 2^kSlack do no harm in fp32, nor rounded to bf16, and after a
 // tile's first blocks the scaling (as many products as there are sums) hardly ever runs.
@@ -254,17 +255,11 @@ __device__ __forceinline__ void softmax_block(const f32x16 &s, uint32_t seen, fl
     l *= f;
     rescale(o, f);
   }
-  float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -m));
     if (MASKED) p[i] = seen >> reg_token(i) & 1 ? p[i] : 0.0f;
-    if (i & 1)
-      sum1 += p[i];
-    else
-      sum0 += p[i];
   }
-  l += sum0 + sum1;
 }
 
 // eight probabilities (registers 8 s .. 8 s + 7) as the second operand of step s
@@ -456,13 +451,35 @@ __device__ __forceinline__ float power_of(uint32_t w, int j) {
 #undef DT_SHIFT
   return e;
 }
+// The sum of an operand's elements, two an instruction (products with 1 are exact).
+__device__ __forceinline__ float sum_p(bf16x8 v) {
+  const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[i], v[i + 1]}, one, sum, false);
+  return sum;
+}
+__device__ __forceinline__ float sum_p(const float (&p)[16]) {
+  float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; i += 2) sum0 += p[i], sum1 += p[i + 1];
+  return sum0 + sum1;
+}
 // The probabilities as the operand of those products (DT_F8: times the tokens' powers of two, `exps`
-// in LDS: exact).
+// in LDS: exact), and in the row's sum l.  bf16 and 8-bit values are multiplied by probabilities rounded to
+// bf16: a second product with what the rounding leaves would be half as many matrix instructions again, where the
+// result has no more bits than these.  With bf16 values the sum takes them as rounded, so that a row's weights
+// add up to one as they are used (equal values give that value; the error against 64 bits with a sum of the
+// unrounded and of the rounded: a chunk of 4,096 rows 2.27e-3 and 2.24e-3, one of 2,047 under a window 2.27e-3 and
+// 2.16e-3; the result's rounding alone is 1.66e-3).  In 8 bits the product wants them times a power of two, and
+// rounding them once more for the sum took 5% longer (1,024 rows over 8,192 tokens: 177 and 185 us) for values
+// that are themselves off by up to 2^-4: there the sum takes them unrounded.
 template <int DT, bool MASKED>
 struct POperand {
   bf16x8 f[2];
-  __device__ __forceinline__ POperand(float (&p)[16], const char *exps, uint32_t seen, int h) {
+  __device__ __forceinline__ POperand(float (&p)[16], const char *exps, uint32_t seen, int h, float &l) {
     if constexpr (DT == DT_F8) {
+      l += sum_p(p);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const uint32_t w = *reinterpret_cast<const uint32_t *>(exps + 8 * t + 4 * h);
@@ -475,12 +492,14 @@ struct POperand {
     }
     f[0] = pack_p(p, 0);
     f[1] = pack_p(p, 1);
+    if constexpr (DT != DT_F8) l += sum_p(f[0]) + sum_p(f[1]);
   }
 };
 template <bool MASKED>
 struct POperand<DT_F32, MASKED> {
   float f[16];
-  __device__ __forceinline__ POperand(float (&p)[16], const char *, uint32_t, int) {
+  __device__ __forceinline__ POperand(float (&p)[16], const char *, uint32_t, int, float &l) {
+    l += sum_p(p);
 #pragma unroll
     for (int i = 0; i < 16; ++i) f[i] = p[i];
   }
@@ -523,7 +542,7 @@ __device__ __forceinline__ void full_block(const char *keys, const char *vals, c
       for (int x = 0; x < S; ++x) r.v[t][x] = lds16(v_at<DT, D>(vals, x, t, lane));
   float p[16];
   softmax_block<false>(s, 0, c, m, l, o, p);
-  const POperand<DT, false> pf(p, exps + 32, 0, lane >> 5);
+  const POperand<DT, false> pf(p, exps + 32, 0, lane >> 5, l);
 #pragma unroll
   for (int t = 0; t < T; ++t) {
     if (!kEarly)
@@ -545,7 +564,7 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
   between(sc);
   float p[16];
   softmax_block<true>(sc, seen, c, m, l, o, p);
-  const POperand<DT, true> pf(p, exps + 32, seen, lane >> 5);
+  const POperand<DT, true> pf(p, exps + 32, seen, lane >> 5, l);
   AnyBad<DT> bad;
 #pragma unroll
   for (int n = 0; n < S * T; ++n) {
@@ -561,7 +580,7 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
 #pragma unroll
     for (int s = 0; s < S; ++s) v[s] = lds16(v_at<DT, D>(vals, s, t, lane));
     if (__builtin_expect(any, 0)) {
-      float sf[16];
+      float sf[16], none = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sf[i] = seen >> reg_token(i) & 1 ? 1.0f : 0.0f;
       u32x4 one[S];
@@ -573,7 +592,8 @@ __device__ __forceinline__ void masked_block(const char *keys, const char *vals,
           one[s][i] = x & kOnes<DT>;
           v[s][i] &= ~x;
         }
-      const f32x16 hit = products<DT>(one, POperand<DT == DT_F8 ? DT_BF16 : DT, false>(sf, nullptr, 0, 0), zero16());
+      const POperand<DT == DT_F8 ? DT_BF16 : DT, false> seen_op(sf, nullptr, 0, 0, none);
+      const f32x16 hit = products<DT>(one, seen_op, zero16());
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[t][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[t][i];
     }

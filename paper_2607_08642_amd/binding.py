@@ -510,6 +510,14 @@ def _empty(torch, shape, dtype, device, stream):
     return t
 
 
+def _capturing(torch, stream) -> bool:
+    """Whether calls on `stream` (None: torch's current one) go into a graph."""
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _keep(stream, *tensors):
     """Tensors of other streams stay allocated until a call on `stream` has used them."""
     for t in tensors:
@@ -557,8 +565,9 @@ class Cache:
     dtype: torch.float32, torch.bfloat16 or torch.float8_e4m3fn (bf16 data with one power-of-two
     scale for each token and head).  Calls run on torch's current stream of the cache's device
     unless one is given (which has to wait for what made its inputs, and be waited for, as any);
-    workspaces are kept for each stream.  A captured call keeps its workspace too: a graph that is
-    replayed beside other calls on this cache is captured with a workspace of its own (`workspace`).
+    workspaces are kept for each stream.  A captured call has a workspace from its graph's memory
+    (torch.cuda.graph's), which no other call is given while the graph lives: replays and other calls
+    may overlap.  A stream that is captured by other means needs `workspace`.
     A Cache is used by one host thread at a time, with its device as the current one.
     """
 
@@ -665,7 +674,10 @@ class Cache:
         return n
 
     def _workspace(self, n: int, raw, stream):
-        """The stream's workspace, grown to n bytes: allocated on that stream, where calls follow one another."""
+        """The stream's workspace, grown to n bytes: allocated on that stream, where calls follow one another, so an
+        outgrown one may go.  A graph's calls come again after that: what they use is the graph's, not the stream's."""
+        if _capturing(self._torch, stream):
+            return _empty(self._torch, (n,), self._torch.uint8, self._at, stream)
         ws = self._ws.get(raw)
         if ws is None or ws.numel() < n:
             ws = self._ws[raw] = _empty(self._torch, (n,), self._torch.uint8, self._at, stream)

@@ -472,7 +472,8 @@ dt_status dt_attend_workspace_size(const dt_cache *cache, const dt_chunk *chunk,
  * components of it) non-finite.  Scores, softmax and sums are fp32; with bf16
  * data the probabilities are rounded to bf16 before their product with the
  * values.  scale q . k has to stay below 2^30 in magnitude (an fp32 score beyond that is
- * rounded by whole powers of two of its probability).  q and out may have different strides and must not overlap.
+ * rounded by whole powers of two of its probability), and sum_j |v_j| over the keys that a row
+ * sees within fp32's range: the sum of p_j v_j, p_j <= 1, is divided at the end.  q and out may have different strides and must not overlap.
  *   workspace: >= dt_attend_workspace_size bytes, 256-byte aligned (NULL where 0);
  *   not to be shared by calls that can overlap. */
 dt_status dt_cache_attend(const dt_cache *cache, int layer, const dt_chunk *chunk, int heads,

@@ -233,10 +233,11 @@ __device__ __forceinline__ void rescale(f32x16 (&o)[T], float f) {
 
 // One block's scores into probabilities (masked: bits of `seen`, already shifted by 4 h).
 // m: the reference that exponents are taken against, l: this lane's part of the sum (which the
-// probabilities join as they become an operand: POperand).  m
-// is raised, and what was summed scaled, only once a row's maximum lies more than kSlack
-// above it: probabilities up to 2^kSlack do no harm in fp32, nor rounded to bf16, and after a
-// tile's first blocks the scaling (as many products as there are sums) hardly ever runs.
+// probabilities join as they become an operand: POperand).  m is never below a maximum, so no
+// probability is above one and sums of p v stay within what the values themselves sum to.  It is raised, and
+// what was summed scaled, to kSlack above the maximum that passed it: the lesser probabilities do no harm in
+// fp32, nor rounded to bf16 (both have their bits down to 2^-126), and after a tile's first blocks the
+// scaling (as many products as there are sums) hardly ever runs.
 constexpr float kSlack = 8.0f;
 template <bool MASKED, int T>
 __device__ __forceinline__ void softmax_block(const f32x16 &s, uint32_t seen, float c, float &m, float &l,
@@ -249,8 +250,8 @@ __device__ __forceinline__ void softmax_block(const f32x16 &s, uint32_t seen, fl
   for (int i = 3; i < 15; i += 2) top = max3(top, x[i], x[i + 1]);
   const float2 th = halves(max2(top, x[15]));
   const float now = max2(th.x, th.y) * c;
-  if (__builtin_expect(__ballot(now > m + kSlack) != 0, 0)) {
-    const float to = now > m ? now : m, f = __builtin_amdgcn_exp2f(m - to);
+  if (__builtin_expect(__ballot(now > m) != 0, 0)) {
+    const float to = now > m ? now + kSlack : m, f = __builtin_amdgcn_exp2f(m - to);
     m = to;
     l *= f;
     rescale(o, f);

@@ -2,7 +2,7 @@
 // size), the join of split calls, and the choice of kernel and split.
 //
 // A row's result is sum_j p_j v_j / sum_j p_j with p_j = 2^(c s_j - m), s_j = q k_j, c = scale log2 e, in one
-// pass over the keys: m is a running reference near the maximum of c s, and what was summed under an
+// pass over the keys: m is a running reference at or above the maximum of c s, and what was summed under an
 // older one is scaled by 2^(old - new).  Two parts (m1, l1, o1), (m2, l2, o2) of the keys join the same way, which
 // is what the waves, and the splits of a long sequence, do.
 //

@@ -2,6 +2,7 @@
 
 Where a tolerance is needed it is the one of the attention tests (test_gpu_attend.allowed)."""
 import pytest
+import torch
 
 from test_gpu_attend import Attend
 
@@ -31,3 +32,21 @@ def test_equal_values_give_that_value(D, shape):
     store(a)
     got = a.run()
     assert bool((got == 1.875).all()), f"{int((got != 1.875).sum())} of {got.numel()} differ"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f8"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("chunk", [1, 64])
+def test_values_whose_sum_is_just_finite(dtype, D, chunk):
+    """256 values of about 1e36, the later half's scores 7.5 (in powers of two) above the first's: no sum passes
+    what the values themselves sum to, 2.6e38."""
+    print(f"[values] large {dtype} D={D} chunk={chunk}", flush=True)
+    a = Attend(dtype, [(256, chunk)], 8, 64, 2, D, seed=D)
+    a.q.fill_(1.0)
+    a.k.zero_()
+    a.k[128:] = 7.5 / 1.4426950408889634 / D ** 0.5
+    a.v.copy_((0.75 + 0.25 * a.v.float().abs().clamp(max=1.0)) * 1e36)
+    store(a)
+    got = a.run()
+    assert bool(torch.isfinite(got).all())
+    a.check(got)

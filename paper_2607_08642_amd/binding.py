@@ -491,12 +491,23 @@ def scan_topm(logits, M: int, T: float, stream=None):
 # Calls here are short (a kernel of a few us), so their own work is kept small: one lookup of the
 # raw stream, C structures that are filled anew rather than made, no checks that the C side makes.
 
-def _want(t, name, shape, dtype):
-    """A contiguous device tensor of this shape and dtype, as the C ABI takes it."""
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name}: want a contiguous {dtype} device tensor of shape {shape}, "
+def _want(t, name, shape, dtype, device):
+    """A contiguous tensor of this shape and dtype on a device (its index), as the C ABI takes it."""
+    if t.dtype != dtype or tuple(t.shape) != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: want a contiguous {dtype} tensor of shape {shape} on cuda:{device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
+
+
+def _raw_stream(torch, device: int, stream, what: str):
+    """The handle of `stream` (None: torch's current one) for a call on a device, which has to be the current one."""
+    if torch._C._cuda_getDevice() != device:
+        raise ValueError(f"{what} on device {device}, which is not the current one")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device) or None
+    if stream.device_index != device:
+        raise ValueError(f"{what} on device {device}, the stream on device {stream.device_index}")
+    return stream.cuda_stream or None
 
 
 def _empty(torch, shape, dtype, device, stream):
@@ -528,17 +539,20 @@ def _keep(stream, *tensors):
 class Chunk:
     """dt_chunk: the new tokens of a batch of sequences and where they lie in a cache.
 
-    starts [batch + 1], lens [batch] and table [batch, width]: int32 device tensors, read when the
-    kernels run, so a program may go on changing their contents in place; max_chunk and max_len
+    starts [batch + 1], lens [batch] and table [batch, width]: int32 tensors on the cache's device, read when
+    the kernels run, so a program may go on changing their contents in place; max_chunk and max_len
     bound the chunks and the lengths they will hold.
     """
 
     def __init__(self, starts, lens, table, max_chunk: int, max_len: int):
         import torch
         batch, width = table.shape
-        self.starts = _want(starts, "starts", (batch + 1,), torch.int32)
-        self.lens = _want(lens, "lens", (batch,), torch.int32)
-        self.table = _want(table, "table", (batch, width), torch.int32)
+        self.device = table.get_device()
+        if self.device < 0:
+            raise ValueError(f"table: want a tensor on a GPU, got one on {table.device}")
+        self.starts = _want(starts, "starts", (batch + 1,), torch.int32, self.device)
+        self.lens = _want(lens, "lens", (batch,), torch.int32, self.device)
+        self.table = _want(table, "table", (batch, width), torch.int32, self.device)
         self.tensors = starts, lens, table
         self.batch, self.max_chunk, self.max_len = batch, max_chunk, max_len
         self.sizes = (batch, max_chunk, max_len, width)
@@ -597,11 +611,13 @@ class Cache:
         self._ws = {}      # a workspace of each stream
 
     def _stream(self, stream):
-        if self._torch._C._cuda_getDevice() != self._device:
-            raise ValueError(f"the cache is on device {self._device}, which is not the current one")
-        if stream is None:
-            return self._torch._C._cuda_getCurrentRawStream(self._device) or None
-        return stream.cuda_stream or None
+        return _raw_stream(self._torch, self._device, stream, "the cache is")
+
+    def _chunk(self, chunk: Chunk, rows: int):
+        """The dt_chunk of a call with so many rows (by reference)."""
+        if chunk.device != self._device:
+            raise ValueError(f"the chunk's tensors are on device {chunk.device}, the cache is on {self._device}")
+        return chunk.as_c(rows)
 
     def _rows(self, c: dt_rows, t, name: str, heads: Optional[int] = None) -> int:
         """Fill c from a tensor [rows, heads, head_dim]; its rows."""
@@ -625,7 +641,7 @@ class Cache:
     def append(self, chunk: Chunk, k, v, layer: int = 0, stream=None) -> None:
         """dt_cache_append: the chunk's keys and values [rows, kv_heads, head_dim] into a layer."""
         rows = self._kv(k, v)
-        st = self._lib.dt_cache_append(self._ref, layer, chunk.as_c(rows), self._aref, self._bref,
+        st = self._lib.dt_cache_append(self._ref, layer, self._chunk(chunk, rows), self._aref, self._bref,
                                        self._stream(stream))
         if st != 0:
             _check(st)
@@ -649,7 +665,8 @@ class Cache:
             b.data = at + rows * row * self._data_bytes
         else:
             rows = self._kv(*out)
-        st = self._lib.dt_cache_read(self._ref, layer, chunk.as_c(rows), self._aref, self._bref, self._stream(stream))
+        st = self._lib.dt_cache_read(self._ref, layer, self._chunk(chunk, rows), self._aref, self._bref,
+                                     self._stream(stream))
         if st != 0:
             _check(st)
         if out is None:
@@ -707,17 +724,21 @@ class Cache:
         o.mask = o.depth = None
         if mask is not None:
             nodes = mask.shape[-1]
-            o.mask = _want(mask, "mask", (chunk.batch, nodes, nodes), self._torch.uint8).data_ptr()
+            o.mask = _want(mask, "mask", (chunk.batch, nodes, nodes), self._torch.uint8,
+                           self._device).data_ptr()
             if depth is not None:
-                o.depth = _want(depth, "depth", (chunk.batch, nodes), self._torch.int32).data_ptr()
+                o.depth = _want(depth, "depth", (chunk.batch, nodes), self._torch.int32,
+                                self._device).data_ptr()
         o.tree_nodes = nodes
         s = self._stream(stream)
         if workspace is None:
             n = self._workspace_size(chunk, rows, heads, o, window, sinks, nodes)
             if n:
                 workspace = self._workspace(n, s, stream)
+        elif workspace.get_device() != self._device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: want a contiguous tensor on {self._at}, got one on {workspace.device}")
         ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-        st = self._lib.dt_cache_attend(self._ref, layer, chunk.as_c(rows), heads, self._aref, self._bref,
+        st = self._lib.dt_cache_attend(self._ref, layer, self._chunk(chunk, rows), heads, self._aref, self._bref,
                                        self._oref, ws, size, s)
         if st != 0:
             _check(st)
@@ -730,10 +751,10 @@ class Cache:
         every layer; the nodes are the last path.shape[1] rows of each chunk."""
         i32 = self._torch.int32
         n = path.shape[1]
-        _want(path, "path", (chunk.batch, n), i32)
-        _want(n_accepted, "n_accepted", (chunk.batch,), i32)
+        _want(path, "path", (chunk.batch, n), i32, self._device)
+        _want(n_accepted, "n_accepted", (chunk.batch,), i32, self._device)
         every = min(chunk.batch * chunk.max_chunk, 2 ** 31 - 1)   # (no tensor of rows here: starts' bound)
-        st = self._lib.dt_cache_commit(self._ref, chunk.as_c(every), n, path.data_ptr(), n_accepted.data_ptr(),
+        st = self._lib.dt_cache_commit(self._ref, self._chunk(chunk, every), n, path.data_ptr(), n_accepted.data_ptr(),
                                        self._stream(stream))
         if st != 0:
             _check(st)
@@ -744,17 +765,26 @@ class Cache:
 def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None) -> Accepted:
     """dt_tree_accept: the longest path of each tree that the target agrees with.
 
-    target [b, B + 1] int32: the target's token at the root and at every node.
+    target [b, B + 1] int32: the target's token at the root and at every node.  Runs on torch's current stream
+    of the tensors' device (the current one) unless one is given; out: results to write instead of new ones.
     """
     import torch
     b, B = tree.tokens.shape
-    _want(target, "target", (b, B + 1), torch.int32)
+    i32, device = torch.int32, target.get_device()
+    s = _raw_stream(torch, device, stream, "target is")
+    _want(target, "target", (b, B + 1), i32, device)
+    if tree.__dict__.get("_device") != device:   # (looked at once, as its C view is made once)
+        for name, shape in (("tokens", (b, B)), ("parents", (b, B)), ("n_nodes", (b,))):
+            _want(getattr(tree, name), name, shape, i32, device)
+        tree.__dict__["_device"] = device
     if out is None:
-        path, n, token = _empty(torch, (b * (B + 2),), torch.int32, target.device, stream).split_with_sizes((b * B, b, b))
+        path, n, token = _empty(torch, (b * (B + 2),), i32, target.device, stream).split_with_sizes((b * B, b, b))
         out = Accepted(path.view(b, B), n, token)
-    s = torch._C._cuda_getCurrentRawStream(target.device.index) if stream is None else stream.cuda_stream
+    else:
+        for name, shape in (("path", (b, B)), ("n_accepted", (b,)), ("next_token", (b,))):
+            _want(getattr(out, name), name, shape, i32, device)
     st = load().dt_tree_accept(ctypes.byref(tree.as_c()), b, B, target.data_ptr(), out.path.data_ptr(),
-                               out.n_accepted.data_ptr(), out.next_token.data_ptr(), s or None)
+                               out.n_accepted.data_ptr(), out.next_token.data_ptr(), s)
     if st != 0:
         _check(st)
     if stream is not None:

@@ -8,6 +8,128 @@ import torch
 from paper_2607_08642_amd import binding
 
 
+class On:
+    """As much of a device tensor as the binding looks at."""
+
+    def __init__(self, shape, dtype=torch.int32, device=0):
+        self.shape, self.dtype, self.index = torch.Size(shape), dtype, device
+        self.device, self.is_cuda = torch.device("cuda", device), True
+
+    def get_device(self):
+        return self.index
+
+    def stride(self):
+        return tuple(torch.empty(self.shape, device="meta").stride())
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def numel(self):
+        return self.shape.numel()
+
+
+class Calls:
+    """A library that notes the names of its calls and does nothing."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.made.append(name) or 0
+
+
+@pytest.fixture
+def on_device(cache, monkeypatch):
+    """(cache, library): a cache on device 0, the current one, over a library that does nothing."""
+    lib = Calls()
+    cache._lib, cache._device = lib, 0
+    monkeypatch.setattr(binding, "load", lambda: lib)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0, raising=False)
+    return cache, lib
+
+
+def chunk(device=0):
+    return binding.Chunk(On([3], device=device), On([2], device=device), On([2, 4], device=device), 5, 128)
+
+
+BF16 = torch.bfloat16
+
+
+def attend(c, k, **kw):
+    return c.attend(k, On([8, 2, 64], BF16), out=On([8, 2, 64], BF16), **kw)
+
+
+def test_calls_on_one_device_are_made(on_device):
+    c, lib = on_device
+    x = On([8, 1, 64], BF16)
+    c.append(chunk(), x, x)
+    c.read(chunk(), out=(x, x))
+    attend(c, chunk(), mask=On([2, 4, 4], torch.uint8), depth=On([2, 4]), workspace=On([1 << 20], torch.uint8))
+    c.commit(chunk(), On([2, 4]), On([2]))
+    assert lib.made == ["dt_cache_append", "dt_cache_read", "dt_cache_attend", "dt_cache_commit"]
+
+
+def test_tensors_of_another_device_are_refused(on_device):
+    """Each tensor of each call: an address of another GPU is not to reach a kernel."""
+    c, lib = on_device
+    x, good, far = On([8, 1, 64], BF16), chunk(), chunk(1)
+    calls = [lambda: binding.Chunk(On([3], device=1), On([2]), On([2, 4]), 5, 128),
+             lambda: binding.Chunk(On([3]), On([2], device=1), On([2, 4]), 5, 128),
+             lambda: binding.Chunk(On([3]), On([2]), On([2, 4], device=1), 5, 128),
+             lambda: c.append(far, x, x), lambda: c.read(far, out=(x, x)), lambda: attend(c, far),
+             lambda: c.commit(far, On([2, 4]), On([2])),
+             lambda: attend(c, good, mask=On([2, 4, 4], torch.uint8, 1)),
+             lambda: attend(c, good, mask=On([2, 4, 4], torch.uint8), depth=On([2, 4], device=1)),
+             lambda: attend(c, good, workspace=On([1 << 20], torch.uint8, 1)),
+             lambda: attend(c, good, workspace=torch.empty(1 << 20, dtype=torch.uint8)),
+             lambda: c.commit(good, On([2, 4], device=1), On([2])),
+             lambda: c.commit(good, On([2, 4]), On([2], device=1))]
+    for n, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {n} was made")
+    assert set(lib.made) <= {"dt_attend_workspace_size"}
+
+
+def tree(b=2, B=4, device=0):
+    shapes = dict(tokens=[b, B], parents=[b, B], depth=[b, B], position_ids=[b, B], mask=[b, B, B], scores=[b, B],
+                  n_nodes=[b], status=[b])
+    return binding.Tree(**{n: On(s, device=device) for n, s in shapes.items()})
+
+
+def results(**kw):
+    return binding.Accepted(**{**dict(path=On([2, 4]), n_accepted=On([2]), next_token=On([2])), **kw})
+
+
+def test_accept_looks_at_every_tensor(on_device, monkeypatch):
+    """Shapes, types and devices of a tree and of given results, and the current device, before anything is launched."""
+    _, lib = on_device
+    binding.accept_tree(tree(), On([2, 5]), out=results())
+    assert lib.made == ["dt_tree_accept"]
+    bad = [(tree(), On([2, 4]), results()), (tree(), On([2, 5], torch.int64), results()),
+           (tree(device=1), On([2, 5]), results()), (tree(), On([2, 5]), results(path=On([2, 3]))),
+           (tree(), On([2, 5]), results(path=On([2, 4], torch.int64))),
+           (tree(), On([2, 5]), results(n_accepted=On([1]))), (tree(), On([2, 5]), results(next_token=On([2], device=1)))]
+    for name in ("tokens", "parents", "n_nodes"):
+        for x in (On([2, 9]), On(getattr(tree(), name).shape, torch.int64), On(getattr(tree(), name).shape, device=1)):
+            t = tree()
+            setattr(t, name, x)
+            if name != "tokens" or x.shape == (2, 4):     # (tokens' shape is the tree's)
+                bad.append((t, On([2, 5]), results()))
+    for n, (t, target, out) in enumerate(bad):
+        with pytest.raises(ValueError):
+            binding.accept_tree(t, target, out=out)
+            pytest.fail(f"call {n} was made")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    with pytest.raises(ValueError):
+        binding.accept_tree(tree(), On([2, 5]), out=results())
+    assert lib.made == ["dt_tree_accept"]
+
+
 @pytest.fixture
 def cache():
     return binding.Cache(4, 32, 1, 64, torch.bfloat16, device="cpu")

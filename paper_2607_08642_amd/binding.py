@@ -556,13 +556,19 @@ class Chunk:
         self.tensors = starts, lens, table
         self.batch, self.max_chunk, self.max_len = batch, max_chunk, max_len
         self.sizes = (batch, max_chunk, max_len, width)
-        self._c = dt_chunk(batch, 0, max_chunk, max_len, width, starts.data_ptr(), lens.data_ptr(), table.data_ptr())
-        self._ref = ctypes.byref(self._c)
+        self._pointers = starts.data_ptr(), lens.data_ptr(), table.data_ptr()
+        self._views = {}
 
     def as_c(self, rows: int):
-        """The dt_chunk of a call with so many rows (by reference)."""
-        self._c.rows = rows
-        return self._ref
+        """The dt_chunk of a call with so many rows (by reference): one for each number of rows, not written to
+        again, so calls of several host threads may share a Chunk."""
+        ref = self._views.get(rows)
+        if ref is None:
+            if len(self._views) >= 64:   # (a call that holds one keeps it alive)
+                self._views = {}
+            batch, max_chunk, max_len, width = self.sizes
+            ref = self._views[rows] = ctypes.byref(dt_chunk(batch, rows, max_chunk, max_len, width, *self._pointers))
+        return ref
 
 
 @dataclasses.dataclass

@@ -95,6 +95,28 @@ def test_tensors_of_another_device_are_refused(on_device):
     assert set(lib.made) <= {"dt_attend_workspace_size"}
 
 
+def test_calls_of_several_threads_share_a_chunk(on_device):
+    """While one call is under way (its library call lets other threads run) another with other rows is made
+    from the same Chunk: the first call's structure stays as it was."""
+    c, _ = on_device
+    k, rows = chunk(), []
+
+    class Busy(Calls):
+        def __getattr__(self, name):
+            def call(ref, layer, chunk_ref, *rest):
+                if not rows:
+                    rows.append(None)
+                    for n in range(1, 200):      # (also past what a Chunk keeps)
+                        k.as_c(n)
+                rows.append(chunk_ref._obj.rows)
+                return 0
+            return call
+
+    c._lib = Busy()
+    c.append(k, On([8, 1, 64], BF16), On([8, 1, 64], BF16))
+    assert rows == [None, 8]
+
+
 def tree(b=2, B=4, device=0):
     shapes = dict(tokens=[b, B], parents=[b, B], depth=[b, B], position_ids=[b, B], mask=[b, B, B], scores=[b, B],
                   n_nodes=[b], status=[b])

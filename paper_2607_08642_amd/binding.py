@@ -652,7 +652,7 @@ class Cache:
         if st != 0:
             _check(st)
         if stream is not None:
-            _keep(stream, k, v, *chunk.tensors)
+            _keep(stream, self.storage, k, v, *chunk.tensors)
 
     def read(self, chunk: Chunk, rows: Optional[int] = None, layer: int = 0, out=None, stream=None):
         """dt_cache_read: the chunk's keys and values as (k, v) [rows, kv_heads, head_dim].
@@ -678,7 +678,7 @@ class Cache:
         if out is None:
             out = both.unbind(0)
         if stream is not None:
-            _keep(stream, *out, *chunk.tensors)
+            _keep(stream, self.storage, *out, *chunk.tensors)
         return out
 
     def workspace_size(self, chunk: Chunk, rows: int, heads: int, opts: dt_attend_options) -> int:
@@ -749,7 +749,7 @@ class Cache:
         if st != 0:
             _check(st)
         if stream is not None:
-            _keep(stream, q, out, mask, depth, workspace, *chunk.tensors)
+            _keep(stream, self.storage, q, out, mask, depth, workspace, *chunk.tensors)
         return out
 
     def commit(self, chunk: Chunk, path, n_accepted, stream=None) -> None:
@@ -765,7 +765,7 @@ class Cache:
         if st != 0:
             _check(st)
         if stream is not None:
-            _keep(stream, path, n_accepted, *chunk.tensors)
+            _keep(stream, self.storage, path, n_accepted, *chunk.tensors)
 
 
 def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None) -> Accepted:

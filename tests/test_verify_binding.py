@@ -117,6 +117,23 @@ def test_calls_of_several_threads_share_a_chunk(on_device):
     assert rows == [None, 8]
 
 
+def test_a_call_on_another_stream_keeps_all_that_it_uses(on_device, monkeypatch):
+    """The cache's own memory too: a Cache that goes while a stream still works on it must not be allocated anew."""
+    c, _ = on_device
+    kept = []
+    monkeypatch.setattr(binding, "_keep", lambda stream, *tensors: kept.append(tensors))
+    side = type("Stream", (), dict(device_index=0, cuda_stream=5))()
+    k, x, q, path, n = chunk(), On([8, 1, 64], BF16), On([8, 2, 64], BF16), On([2, 4]), On([2])
+    mask, depth, ws = On([2, 4, 4], torch.uint8), On([2, 4]), On([1 << 20], torch.uint8)
+    calls = [(lambda: c.append(k, x, x, stream=side), [x]), (lambda: c.read(k, out=(x, x), stream=side), [x]),
+             (lambda: c.attend(k, q, out=q, mask=mask, depth=depth, workspace=ws, stream=side), [q, mask, depth, ws]),
+             (lambda: c.commit(k, path, n, stream=side), [path, n])]
+    for call, used in calls:
+        kept.clear()
+        call()
+        assert {id(t) for t in (c.storage, k.starts, k.lens, k.table, *used)} <= {id(t) for ts in kept for t in ts}
+
+
 def tree(b=2, B=4, device=0):
     shapes = dict(tokens=[b, B], parents=[b, B], depth=[b, B], position_ids=[b, B], mask=[b, B, B], scores=[b, B],
                   n_nodes=[b], status=[b])

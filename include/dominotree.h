@@ -450,7 +450,7 @@ dt_status dt_cache_read(const dt_cache *cache, int layer, const dt_chunk *chunk,
  * before the nodes.  A row of a padding node (mask row 0) sees the keys before the
  * nodes only; every chunk must hold at least N rows. */
 typedef struct {
-  float scale;         /* of q . k, finite */
+  float scale;         /* of q . k; scale and scale log2 e finite */
   int window;          /* 0: no window */
   int sinks;           /* >= 0; looked at with a window only */
   int tree_nodes;      /* 0: no tree; at most 256 */

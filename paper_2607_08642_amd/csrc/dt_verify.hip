@@ -8,6 +8,8 @@ namespace {
 // Workgroups along a grid's axis: a launch counts its threads (256 or fewer a group here) in 32 bits.
 constexpr int kMaxGroups = 1 << 24;
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 bool positive_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 dt_status check_cache(const dt_cache *c, bool data) {
@@ -88,7 +90,8 @@ dt_status check_attend(const dt_cache *c, const dt_chunk *k, int heads, const dt
   if (heads / c->kv_heads > 1024) return fail(DT_ERR_UNSUPPORTED, "at most 1024 heads per kv head");
   if ((int64_t)k->max_chunk * heads > (int64_t)1 << 28)
     return fail(DT_ERR_UNSUPPORTED, "max_chunk * heads must be <= 2^28");
-  if (!(o->scale - o->scale == 0.0f)) return fail(DT_ERR_SHAPE, "scale must be finite");
+  const float unit = o->scale * kLog2e;  // (exponents are taken to the base of 2)
+  if (!(unit - unit == 0.0f)) return fail(DT_ERR_SHAPE, "scale must be finite, and scale log2 e in fp32");
   if (o->window < 0 || o->sinks < 0 || o->tree_nodes < 0)
     return fail(DT_ERR_SHAPE, "window, sinks and tree_nodes must be >= 0");
   if (o->tree_nodes > kMaxB) return fail(DT_ERR_UNSUPPORTED, "tree_nodes must be <= %d", kMaxB);
@@ -188,7 +191,7 @@ dt_status dt_cache_attend(const dt_cache *cache, int layer, const dt_chunk *chun
   a.heads = heads;
   a.group = heads / cache->kv_heads;
   // a scale of 0 (every seen key alike) as one whose products vanish: infinity * 0 is not needed then
-  a.scale_log2e = opts->scale == 0.0f ? 1e-37f : opts->scale * 1.4426950408889634f;
+  a.scale_log2e = opts->scale == 0.0f ? 1e-37f : opts->scale * kLog2e;
   effective_window(chunk, opts, &a.window, &a.sinks);
   a.nodes = opts->tree_nodes;
   a.mask = opts->mask;

@@ -190,8 +190,7 @@ dt_status dt_cache_attend(const dt_cache *cache, int layer, const dt_chunk *chun
   a.dtype = cache->dtype;
   a.heads = heads;
   a.group = heads / cache->kv_heads;
-  // a scale of 0 (every seen key alike) as one whose products vanish: infinity * 0 is not needed then
-  a.scale_log2e = opts->scale == 0.0f ? 1e-37f : opts->scale * kLog2e;
+  a.scale_log2e = opts->scale * kLog2e;
   effective_window(chunk, opts, &a.window, &a.sinks);
   a.nodes = opts->tree_nodes;
   a.mask = opts->mask;

@@ -50,3 +50,21 @@ def test_values_whose_sum_is_just_finite(dtype, D, chunk):
     got = a.run()
     assert bool(torch.isfinite(got).all())
     a.check(got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f8"])
+@pytest.mark.parametrize("scale", [0.0, -0.0])
+@pytest.mark.parametrize("chunk", [1, 64])
+def test_scale_of_zero(dtype, scale, chunk):
+    """Every key alike, however large its product with the query is (1.3e38 of either sign here)."""
+    print(f"[values] scale {scale} {dtype} chunk={chunk}", flush=True)
+    a = Attend(dtype, [(200, chunk)], 8, 64, 2, 64, seed=7)
+    a.q.fill_(1e19)
+    a.k.copy_(torch.where(a.k[:, :, :1].float() > 0, 2e17, -2e17).expand(a.k.shape))
+    store(a)
+    a.check(a.run(scale=scale), scale=0.0)
+    for x in (float("inf"), float("-inf")):      # (0 times infinity)
+        a.k[5, 1, 3] = x
+        store(a)
+        got = a.run(scale=scale)
+        assert bool(torch.isnan(got[:, 4:]).all()) and bool(torch.isfinite(got[:, :4]).all())

@@ -468,8 +468,10 @@ dt_status dt_attend_workspace_size(const dt_cache *cache, const dt_chunk *chunk,
  * head h reading kv head h / (heads / kv_heads).  heads is a multiple of kv_heads, at most
  * 1024 heads per kv head, max_chunk * heads <= 2^28.  The chunk's own keys and values have to be in the cache.
  * A row that sees nothing gives zeros; NaN and infinities of keys and values that a
- * row does not see leave it untouched, those it sees make its result (or those
- * components of it) non-finite.  Scores, softmax and sums are fp32; with bf16
+ * row does not see leave it untouched.  Those it sees: a score of NaN or +infinity makes the row NaN;
+ * one of -infinity (an infinite element of a key, times one of q of the other sign) is a weight of 0, and
+ * a row of such scores alone gives zeros; NaN and infinities of values make their components non-finite,
+ * whatever the weight.  (DT_F8 holds infinities as NaN.)  Scores, softmax and sums are fp32; with bf16
  * data the probabilities are rounded to bf16 before their product with the
  * values.  scale q . k has to stay below 2^30 in magnitude (an fp32 score beyond that is
  * rounded by whole powers of two of its probability), and sum_j |v_j| over the keys that a row

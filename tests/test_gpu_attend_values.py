@@ -4,7 +4,8 @@ Where a tolerance is needed it is the one of the attention tests (test_gpu_atten
 import pytest
 import torch
 
-from test_gpu_attend import Attend
+import verify_ref as ref
+from test_gpu_attend import Attend, allowed
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +69,35 @@ def test_scale_of_zero(dtype, scale, chunk):
         store(a)
         got = a.run(scale=scale)
         assert bool(torch.isnan(got[:, 4:]).all()) and bool(torch.isfinite(got[:, :4]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,chunk", [(64, 1), (64, 64), (128, 64), (256, 1), (256, 64)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_one_infinite_element_of_a_key(dtype, D, chunk, sign):
+    """Scores of -infinity are weights of 0: the row is what it is without that key.  Those of +infinity make NaN."""
+    print(f"[values] infinite key {dtype} D={D} chunk={chunk} sign={sign}", flush=True)
+    n, at = 200, 90                                  # (a block that every row sees whole)
+    a = Attend(dtype, [(n, chunk)], 8, 64, 2, D, seed=D + chunk)
+    a.k[at, :, 7] = sign * float("inf")
+    store(a)
+    got = a.run().double().cpu()
+    keep = [j for j in range(n) if j != at]
+    ok = ref.visible(chunk, n - chunk, n, 0, 0)[:, keep]
+    k, v = a.k[keep], a.v[keep]
+    want = ref.attend(a.q, k, v, D ** -0.5, ok)
+    tol = allowed(a.q, k, v, D ** -0.5, ok, a.cache.data_dtype)
+    zero = a.q[:, :, 7].double() * sign < 0          # (rows whose score there is -infinity)
+    assert bool(zero.any()) and not bool(zero.all())
+    assert bool(((got - want).abs() <= tol)[zero].all())
+    assert bool(torch.isnan(got[~zero]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_of_minus_infinity_alone(dtype):
+    """No key has a weight: zeros, as where nothing is seen."""
+    a = Attend(dtype, [(70, 40)], 8, 64, 2, 64, seed=8)
+    a.q[:, :, 7] = a.q[:, :, 7].abs().clamp(min=0.1)
+    a.k[:, :, 7] = float("-inf")
+    store(a)
+    assert not a.run().any()

@@ -445,9 +445,10 @@ dt_status dt_cache_read(const dt_cache *cache, int layer, const dt_chunk *chunk,
  * or j < sinks.
  * With tree_nodes = N > 0 the last N rows of every chunk are a tree's nodes (the
  * rows before them, the root among them, see what is said above): node m sees node j
- * where mask[b][m][j] is not 0, and of the keys before the nodes all, or with a window
+ * where mask[b][m][j] is not 0, whatever the window, and of the keys before the nodes all, or with a window
  * those that a token at position r + depth[b][m] sees, r the position of the last row
- * before the nodes.  A row of a padding node (mask row 0) sees the keys before the
+ * before the nodes.  (With a window of depth or less a node sees ancestors that plain decoding would not:
+ * clear their bits in mask for its results.)  A row of a padding node (mask row 0) sees the keys before the
  * nodes only; every chunk must hold at least N rows. */
 typedef struct {
   float scale;         /* of q . k; scale and scale log2 e finite */

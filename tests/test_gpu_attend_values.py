@@ -1,11 +1,13 @@
 """Attention whose result follows from the values alone, and values and scores at the ends of their range.
 
 Where a tolerance is needed it is the one of the attention tests (test_gpu_attend.allowed)."""
+import numpy as np
 import pytest
 import torch
 
 import verify_ref as ref
 from test_gpu_attend import Attend, allowed
+from test_gpu_cache import i32
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +103,21 @@ def test_scores_of_minus_infinity_alone(dtype):
     a.k[:, :, 7] = float("-inf")
     store(a)
     assert not a.run().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f8"])
+@pytest.mark.parametrize("window", [1, 3])
+def test_window_shorter_than_the_tree(dtype, window):
+    """A chain of nodes deeper than the window: the mask alone says which nodes are seen; with its far bits cleared the
+    result is plain decoding's."""
+    N = 12
+    a = Attend(dtype, [(90, N + 1), (N + 1, N + 1)], 8, 32, 2, 64, seed=window)
+    chain = np.tril(np.ones((N, N), np.uint8))
+    near = np.triu(chain, 1 - window)
+    depths = [list(range(1, N + 1))] * 2
+    for mask in (chain, near):
+        got = a.run(mask=torch.from_numpy(np.stack([mask] * 2)).cuda(), depth=i32(depths), window=window, sinks=2)
+        a.check(got, window=window, sinks=2, masks=[mask] * 2, depths=depths)
+    # (sinks among the nodes are the mask's, too; with one, the root of the second sequence, there are none)
+    a.check(a.run(mask=torch.from_numpy(np.stack([near] * 2)).cuda(), depth=i32(depths), window=window, sinks=1),
+            window=window, sinks=1)

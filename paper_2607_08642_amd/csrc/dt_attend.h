@@ -452,10 +452,9 @@ __device__ __forceinline__ float power_of(uint32_t w, int j) {
 #undef DT_SHIFT
   return e;
 }
-// The sum of an operand's elements, two an instruction (products with 1 are exact).
-__device__ __forceinline__ float sum_p(bf16x8 v) {
+// An operand's elements added to a sum, two an instruction (products with 1 are exact).
+__device__ __forceinline__ float sum_p(bf16x8 v, float sum) {
   const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
-  float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[i], v[i + 1]}, one, sum, false);
   return sum;
@@ -493,7 +492,7 @@ struct POperand {
     }
     f[0] = pack_p(p, 0);
     f[1] = pack_p(p, 1);
-    if constexpr (DT != DT_F8) l += sum_p(f[0]) + sum_p(f[1]);
+    if constexpr (DT != DT_F8) l = sum_p(f[0], l) + sum_p(f[1], 0.0f);
   }
 };
 template <bool MASKED>

@@ -306,12 +306,16 @@ AttendPlan attend_plan(const CacheView &c, const ChunkView &k, int dtype, int he
   const int group = heads / c.kv, rows = k.max_chunk * group, sets = (rows + 31) / 32;
   AttendPlan p;
   // Few rows, or fp32: every wave its own blocks; more rows share them through LDS (of 68 rows a head
-  // each wave would read all keys three times over).  Eight waves a workgroup where that still fills the
-  // chip twice with equal work (one chunk of 4,096 over 16,384 tokens: 881 us against 915 with
-  // four); else four (eight ragged chunks of up to 509: 67 against 86, a chunk of 2,047 under a window: 23
-  // against 29).
+  // each wave would read all keys three times over).  Eight waves a workgroup for one sequence that fills the
+  // chip twice with them, but not under a window at up to 128 a head; else four.  One chunk over 16,384 tokens in
+  // eight and in four (us; 4,096 rows of 32 heads over 8, at 256 8,192 rows of 16 over 8): bf16 64 a head 569 and 568,
+  // 96 719 and 729, 128 859 and 889, 256 1,339 and 2,193 (four are one wave a SIMD there; eight spill 116 registers a
+  // lane); 8 bits 812 and 788, 917 and 863, 1,009 and 1,016, 1,705 and 2,074; under a window of 1,024 60 and 57, 76
+  // and 70, 94 and 85, 207 and 278.  Chunks that do not fill it twice: eight ragged ones of up to 509 86 and 67, one of
+  // 2,047 under a window 29 and 23 (when the rule was set).
   p.stream = dtype == DT_F32 || sets == 1;
-  p.waves = p.stream ? stream_blocks(c.D) : k.batch == 1 && (int64_t)c.kv * ((sets + 7) / 8) >= 512 ? 8 : 4;
+  const bool twice = k.batch == 1 && (int64_t)c.kv * ((sets + 7) / 8) >= 512;
+  p.waves = p.stream ? stream_blocks(c.D) : twice && (c.D == 256 || window == 0 || window >= k.max_len) ? 8 : 4;
   const int full = p.stream ? 1 : p.waves;
   p.tiles = (sets + full - 1) / full;
   p.tile_rows = (sets + p.tiles - 1) / p.tiles * 32;  // (even tiles: 9 sets of 32 rows are 3 + 3 + 3, not 4 + 4 + 1)

@@ -15,7 +15,6 @@
 namespace dt {
 namespace att {
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -390,7 +389,12 @@ __device__ __forceinline__ u32x4 lds16(const char *p) { return *reinterpret_cast
 
 // Results of matrix products that are read behind a branch.  The products take cycles that the
 // hardware does not wait for and the compiler has to fill; it has been seen to leave out the
-// wait behind a branch (four of sixteen scores were read too early), so it stands here, in front of it.
+// wait behind a branch (four of sixteen scores were read too early), so it stands here, in front of it:
+// a product of 16 passes (the longest here, fp32) asks for 18 states, these are 20.  Every result that is read behind a
+// branch has one, or needs none because a later product's result has been waited for (products of a wave end in
+// the order in which they are issued): the sums `o` that softmax_block scales and masked_block overwrites were
+// issued before the block's scores, which softmax_block's maximum has read by then.  A new read of `o` or of scores
+// behind a branch has to have either.
 __device__ __forceinline__ void settle(f32x16 &s) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s)); }
 struct Nothing {  // (no branch)
   __device__ __forceinline__ void operator()(f32x16 &) const {}

@@ -541,7 +541,8 @@ class Chunk:
 
     starts [batch + 1], lens [batch] and table [batch, width]: int32 tensors on the cache's device, read when
     the kernels run, so a program may go on changing their contents in place; max_chunk and max_len
-    bound the chunks and the lengths they will hold.
+    bound the chunks and the lengths they will hold (attention is cut up for max_len tokens: a bound far
+    above the lengths is right but slower).
     """
 
     def __init__(self, starts, lens, table, max_chunk: int, max_len: int):

@@ -390,7 +390,7 @@ __device__ __forceinline__ u32x4 lds16(const char *p) { return *reinterpret_cast
 // Results of matrix products that are read behind a branch.  The products take cycles that the
 // hardware does not wait for and the compiler has to fill; it has been seen to leave out the
 // wait behind a branch (four of sixteen scores were read too early), so it stands here, in front of it:
-// a product of 16 passes (the longest here, fp32) asks for 18 states, these are 20.  Every result that is read behind a
+// 20 states, which suffice for the longest product here (fp32: 16 passes).  Every result that is read behind a
 // branch has one, or needs none because a later product's result has been waited for (products of a wave end in
 // the order in which they are issued): the sums `o` that softmax_block scales and masked_block overwrites were
 // issued before the block's scores, which softmax_block's maximum has read by then.  A new read of `o` or of scores

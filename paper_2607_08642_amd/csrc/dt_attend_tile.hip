@@ -7,14 +7,15 @@
 //
 // What bounds it: the issue of instructions.  A wave by itself takes about five cycles an instruction,
 // and a block of 32 tokens of 128 is 16 matrix products (512 cycles of the matrix unit) among
-// some 190 others in bf16, 280 in 8 bits (64 of them widen codes, 36 bring in the values' scales): a
+// some 175 others in bf16, 285 in 8 bits (64 of them widen codes, 36 bring in the values' scales): a
 // block takes 0.5 us of a workgroup by itself, 0.65 in 8 bits, and two workgroups a CU fill each other's
-// gaps.  4,096 rows of 32 heads over 16,384 tokens: 870 to 900 us, 1,070 to 1,100 TFLOP/s of the 1,245 of a large
-// product; in 8 bits 1,029 us.  Eight ragged chunks of 16 heads of 64 in 8 bits: 68 us, 260
+// gaps.  4,096 rows of 32 heads over 16,384 tokens: 858 to 930 us from one card to another (graph-captured; 983
+// under a kernel trace), 1,035 to 1,120 TFLOP/s of the 1,245 of a large product; in 8 bits 1,012 us.  8,192 rows of 16
+// heads of 256 over as many: 1,337 us, 1,230 TFLOP/s.  Eight ragged chunks of 16 heads of 64 in 8 bits: 69 us, 260
 // TFLOP/s (the longest tile's blocks, one after another); 65 rows of 32 heads over 30,011 tokens in 8 bits: 70 us, of which
 // about 20 do not depend on the length (start, masked blocks, parts, join).
 // Measured and not taken: two blocks a turn; the next block's scores between the instructions of
-// the last one's softmax (881 -> 943 us: the number of instructions counts, not their order); all keys of a
+// the last one's softmax (881 -> 943 us then: the number of instructions counts, not their order); all keys of a
 // block read before the first product (897); four waves a SIMD at 64 (a long chunk 303 -> 295, but
 // one under a window 24 -> 26: registers).
 #include "dt_attend.h"

@@ -471,13 +471,14 @@ __device__ __forceinline__ float sum_p(const float (&p)[16]) {
 }
 // The probabilities as the operand of those products (DT_F8: times the tokens' powers of two, `exps`
 // in LDS: exact), and in the row's sum l.  bf16 and 8-bit values are multiplied by probabilities rounded to
-// bf16: a second product with what the rounding leaves would be half as many matrix instructions again, where the
-// result has no more bits than these.  With bf16 values the sum takes them as rounded, so that a row's weights
-// add up to one as they are used (equal values give that value; the error against 64 bits with a sum of the
-// unrounded and of the rounded: a chunk of 4,096 rows 2.27e-3 and 2.24e-3, one of 2,047 under a window 2.27e-3 and
-// 2.16e-3; the result's rounding alone is 1.66e-3).  In 8 bits the product wants them times a power of two, and
-// rounding them once more for the sum took 5% longer (1,024 rows over 8,192 tokens: 177 and 185 us) for values
-// that are themselves off by up to 2^-4: there the sum takes them unrounded.
+// bf16: error against 64 bits 2.2e-3, of which the rounding of the result is 1.66e-3.  A second product with what the
+// rounding leaves makes that 1.66e-3, and was measured and not taken: half as many matrix instructions again where those
+// count, and for single tokens in bf16 0.4 to 7% longer (32 of up to 8,192: 133.7 -> 134.3 us, eight of 2,048: 18.1 ->
+// 19.4), in 8 bits 4 to 13% (87.6 -> 96.4).  With bf16 values the sum takes them as rounded, so that a row's weights
+// add up to one as they are used (equal values give that value; a chunk of 4,096 rows 2.27e-3 with a sum of
+// the unrounded and 2.24e-3, one of 2,047 under a window 2.27e-3 and 2.16e-3).  In 8 bits the product wants them
+// times a power of two, and rounding them once more for the sum took 5% longer (1,024 rows over 8,192 tokens: 177 and
+// 185 us) for values that are themselves off by up to 2^-4: there the sum takes them unrounded.
 template <int DT, bool MASKED>
 struct POperand {
   bf16x8 f[2];

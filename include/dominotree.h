@@ -414,7 +414,8 @@ typedef struct {
   int batch;       /* 1 .. 65535 */
   int rows;        /* rows of the call's tensors, >= 1 */
   int max_chunk;   /* bound of n_b, 1 <= max_chunk <= rows */
-  int max_len;     /* bound of lens[b], 1 <= max_len <= table_width * page_size */
+  int max_len;     /* bound of lens[b], 1 <= max_len <= table_width * page_size
+                      (dt_cache_attend is cut up for it: one far above the lengths is right but slower) */
   int table_width; /* pages of a table row; table_width * page_size < 2^30 */
   const int32_t *starts; /* [batch + 1] */
   const int32_t *lens;   /* [batch] */

@@ -503,6 +503,39 @@ dt_status dt_tree_accept(const dt_tree *tree, int batch, int B, const int32_t *t
 dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int nodes, const int32_t *path,
                           const int32_t *n_accepted, void *stream);
 
+/* ---- heads normed and rotated by position ----
+ *
+ * For every row and head x[0 .. D): with a weight, y = weight x / sqrt(mean(x^2) + eps), else
+ * y = x; then for j < pairs, with the angle a = positions[row] inv_freq[j],
+ *   (y1, y2) -> (y1 cos a - y2 sin a, y2 cos a + y1 sin a)
+ * over the pairs y[j], y[j + pairs], or with interleaved y[2 j], y[2 j + 1]; elements from 2 pairs on
+ * stay as they are.  Angles are reduced in 64 bits (their error is below 2^-52 of the
+ * angle: 1e-9 at 10^6 turns); norms and products are fp32, rounded once to the data type.  sum x^2 has to
+ * stay within fp32's range; NaN and infinities make their head's results non-finite. */
+typedef struct {
+  const int32_t *positions; /* [rows]; any values */
+  const float *inv_freq;    /* [pairs] radians a position */
+  int pairs;                /* a multiple of 8, 8 .. D / 2 */
+  int interleaved;
+  const void *q_weight;     /* [D] in the data type, 16-byte aligned, or NULL: queries are not normed */
+  const void *k_weight;     /* the same for keys */
+  float eps;                /* >= 0, finite */
+} dt_rotary;
+
+/* Queries q [rows, heads, D] and keys k [rows, kv_heads, D] into q_out and k_out (k and k_out NULL and
+ * kv_heads 0: queries alone).  dtype: DT_F32 or DT_BF16; D a multiple of 16, 16 .. 512; heads +
+ * kv_heads < 2^20; rows < 2^26.  An output may be its input (the same address and strides), else tensors must not overlap. */
+dt_status dt_rotate(const dt_rows *q, int heads, const dt_rows *k, int kv_heads, int rows, int D, int dtype,
+                    const dt_rotary *rotary, const dt_rows *q_out, const dt_rows *k_out, void *stream);
+
+/* dt_rotate and dt_cache_append in one: the chunk's queries q [rows, heads, D] normed and rotated into q_out, its
+ * keys normed, rotated and written into the layer (DT_F8: rounded to bf16 first, so the cache holds what the
+ * two calls leave in it), its values written as they are.  Rows that belong to no chunk are not touched.
+ * 1 <= heads < 2^20, and max_chunk * heads / 4 + (max_chunk / 32 + 3) * kv_heads < 2^24. */
+dt_status dt_cache_append_rotated(const dt_cache *cache, int layer, const dt_chunk *chunk, int heads, const dt_rows *q,
+                                  const dt_rows *k, const dt_rows *v, const dt_rotary *rotary, const dt_rows *q_out,
+                                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,7 +39,8 @@ EXPORTS = ("dt_abi_version", "dt_status_string", "dt_last_error", "dt_plan_creat
            "dt_plan_expand_stats", "dt_plan_set_adaptive_budget", "dt_model_create",
            "dt_model_destroy", "dt_plan_create_from_model", "dt_once_workspace_size",
            "dt_build_tree_once", "dt_cache_size", "dt_cache_append", "dt_cache_read",
-           "dt_attend_workspace_size", "dt_cache_attend", "dt_tree_accept", "dt_cache_commit")
+           "dt_attend_workspace_size", "dt_cache_attend", "dt_tree_accept", "dt_cache_commit",
+           "dt_rotate", "dt_cache_append_rotated")
 STAGES = ("scan", "expand")
 
 
@@ -95,6 +96,12 @@ class dt_rows(ctypes.Structure):
 class dt_attend_options(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("window", ctypes.c_int), ("sinks", ctypes.c_int),
                 ("tree_nodes", ctypes.c_int), ("mask", ctypes.c_void_p), ("depth", ctypes.c_void_p)]
+
+
+class dt_rotary(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p), ("pairs", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -169,6 +176,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.dt_tree_accept.argtypes = [ctypes.POINTER(dt_tree), ci, ci, vp, vp, vp, vp, vp]
     lib.dt_cache_commit.restype = ci
     lib.dt_cache_commit.argtypes = [pc, pk, ci, vp, vp, vp]
+    pt = ctypes.POINTER(dt_rotary)
+    lib.dt_rotate.restype = ci
+    lib.dt_rotate.argtypes = [pr, ci, pr, ci, ci, ci, ci, pt, pr, pr, vp]
+    lib.dt_cache_append_rotated.restype = ci
+    lib.dt_cache_append_rotated.argtypes = [pc, ci, pk, ci, pr, pr, pr, pt, pr, vp]
     if lib.dt_abi_version() != ABI_VERSION:
         raise RuntimeError(f"ABI mismatch: library {lib.dt_abi_version()} vs binding {ABI_VERSION}")
     _lib = lib
@@ -580,6 +592,17 @@ class Accepted:
     next_token: "torch.Tensor"  # [b] int32 the target's token after the path
 
 
+def _rotary(torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim, dtype, device) -> dt_rotary:
+    """The dt_rotary of a call."""
+    _want(positions, "positions", (rows,), torch.int32, device)
+    _want(inv_freq, "inv_freq", (inv_freq.numel(),), torch.float32, device)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _want(w, name, (dim,), dtype, device)
+    return dt_rotary(positions.data_ptr(), inv_freq.data_ptr(), inv_freq.numel(), bool(interleaved), _ptr(q_weight),
+                     _ptr(k_weight), eps)
+
+
 class Cache:
     """dt_cache: keys and values of `layers` layers in pages, in the kernels' own order.
 
@@ -654,6 +677,34 @@ class Cache:
             _check(st)
         if stream is not None:
             _keep(stream, self.storage, k, v, *chunk.tensors)
+
+    def append_rotated(self, chunk: Chunk, q, k, v, positions, inv_freq, q_weight=None, k_weight=None,
+                       eps: float = 1e-6, interleaved: bool = False, layer: int = 0, out=None, stream=None):
+        """dt_cache_append_rotated: rotate and append in one: the chunk's keys, normed and rotated, and values
+        into a layer; its queries [rows, heads, head_dim], normed and rotated, as the result (`out` may be q).
+
+        positions, inv_freq, the weights, eps and interleaved are rotate's.  Rows of no chunk are left as they are.
+        """
+        torch = self._torch
+        rows = self._kv(k, v)
+        x, y = dt_rows(), dt_rows()
+        if self._rows(x, q, "q") != rows:
+            raise ValueError(f"q and k have {q.shape[0]} and {rows} rows")
+        heads = q.shape[1]
+        if out is None:
+            out = _empty(torch, (rows, heads, self.head_dim), self.data_dtype, self._at, stream)
+        if self._rows(y, out, "out", heads) != rows:
+            raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
+        r = _rotary(torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, self.head_dim,
+                    self.data_dtype, self._device)
+        st = self._lib.dt_cache_append_rotated(self._ref, layer, self._chunk(chunk, rows), heads, ctypes.byref(x),
+                                               self._aref, self._bref, ctypes.byref(r), ctypes.byref(y),
+                                               self._stream(stream))
+        if st != 0:
+            _check(st)
+        if stream is not None:
+            _keep(stream, self.storage, q, k, v, out, positions, inv_freq, q_weight, k_weight, *chunk.tensors)
+        return out
 
     def read(self, chunk: Chunk, rows: Optional[int] = None, layer: int = 0, out=None, stream=None):
         """dt_cache_read: the chunk's keys and values as (k, v) [rows, kv_heads, head_dim].
@@ -767,6 +818,52 @@ class Cache:
             _check(st)
         if stream is not None:
             _keep(stream, self.storage, path, n_accepted, *chunk.tensors)
+
+
+def _strided(t, name: str, device: int, dtype, shape) -> dt_rows:
+    """The dt_rows of a tensor [rows, heads, dim] (a None of the shape: any)."""
+    if t.dtype != dtype or t.dim() != 3 or t.get_device() != device or \
+            any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name}: want a {dtype} tensor of shape {shape} on cuda:{device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    stride = t.stride()
+    if stride[2] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous (stride {stride[2]})")
+    return dt_rows(t.data_ptr(), stride[0], stride[1])
+
+
+def rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+           out=None, stream=None):
+    """dt_rotate: queries [rows, heads, D] and keys [rows, kv_heads, D] (None: queries alone), float32 or bfloat16,
+    normed (where a weight [D] of their dtype is given) and rotated by position; (q, k).
+
+    positions [rows] int32 (Tree.position_ids, for a tree's nodes); inv_freq [pairs] float32, pairs a multiple of 8
+    and at most D / 2: element j is paired with j + pairs, or with interleaved 2 j with 2 j + 1.
+    out = (q, k) takes given tensors, which may be the inputs themselves.  Runs on torch's current
+    stream of the tensors' device (the current one) unless one is given.
+    """
+    import torch
+    device, dtype = q.get_device(), q.dtype
+    code = _dtype_code(q)
+    s = _raw_stream(torch, device, stream, "q is")
+    x = _strided(q, "q", device, dtype, (None, None, None))
+    rows, heads, dim = q.shape
+    kv = 0 if k is None else k.shape[1]
+    y = None if k is None else _strided(k, "k", device, dtype, (rows, None, dim))
+    if out is None:
+        n = rows * heads * dim
+        both = _empty(torch, (n + rows * kv * dim,), dtype, q.device, stream)
+        out = both[:n].view(rows, heads, dim), None if k is None else both[n:].view(rows, kv, dim)
+    a = _strided(out[0], "out", device, dtype, (rows, heads, dim))
+    b = None if k is None else _strided(out[1], "out", device, dtype, (rows, kv, dim))
+    r = _rotary(torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim, dtype, device)
+    by = lambda c: None if c is None else ctypes.byref(c)  # noqa: E731
+    st = load().dt_rotate(by(x), heads, by(y), kv, rows, dim, code, by(r), by(a), by(b), s)
+    if st != 0:
+        _check(st)
+    if stream is not None:
+        _keep(stream, q, k, positions, inv_freq, q_weight, k_weight, *out)
+    return out
 
 
 def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None) -> Accepted:

@@ -11,18 +11,18 @@
 // elements at a time.
 #include <type_traits>
 
-#include "dt_cache.h"
+#include "dt_rotate.h"
 
 namespace dt {
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
+static_assert(kThreads == 64 * kRotWaves, "a wave for each part of a row");
 constexpr int kPad = 16;  // bytes after each row of the LDS tile: an odd number of 16-byte columns
 
 template <int DT>
@@ -42,37 +42,6 @@ struct Elem<DT_F8> {
   static constexpr int bytes = 1, E = 16;
   typedef uint16_t data;
 };
-
-__device__ inline uint32_t pack_bf16(float a, float b) {
-  const bf16x2 v = {(__bf16)a, (__bf16)b};
-  uint32_t u;
-  __builtin_memcpy(&u, &v, 4);
-  return u;
-}
-
-// eight elements of a row of the caller's tensor, as 32-bit words (bf16: two a word)
-template <bool vec>
-__device__ __forceinline__ void load8(const float *p, uint32_t (&w)[8]) {
-  if (vec) {
-    const u32x4 a = reinterpret_cast<const u32x4 *>(p)[0], b = reinterpret_cast<const u32x4 *>(p)[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = a[i], w[4 + i] = b[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(p[i]);
-  }
-}
-template <bool vec>
-__device__ __forceinline__ void load8(const uint16_t *p, uint32_t (&w)[4]) {
-  if (vec) {
-    const u32x4 a = reinterpret_cast<const u32x4 *>(p)[0];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = a[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
-  }
-}
 
 // The block of this workgroup: blocks of a chunk follow the cache's, so the first and the
 // last may be partial.  False where it has no token.
@@ -100,13 +69,15 @@ __device__ inline bool block_of(const CacheView &c, const ChunkView &k, int b, i
 __device__ inline uint32_t low16(uint32_t a, uint32_t b) { return (a & 0xffffu) | b << 16; }
 __device__ inline uint32_t high16(uint32_t a, uint32_t b) { return a >> 16 | (b & 0xffff0000u); }
 
-// grid: (kv head, block of the chunk), sequence
-template <int DT, int D>
-__global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView k, RowsView kr, RowsView vr) {
+// A workgroup's block: kv head and block of the chunk (blockIdx.x), sequence (blockIdx.y).  kRotate: keys are normed
+// and rotated between their load and the tile; a lane then holds both runs of a unit (dt_rotate.h).
+template <int DT, int D, bool kRotate>
+__device__ __forceinline__ void append_block(const CacheView &c, const ChunkView &k, const RowsView &kr,
+                                             const RowsView &vr, const RotaryView &rot, const void *k_weight) {
   using El = Elem<DT>;
   using T = typename El::data;
   constexpr int E = El::E, kWords = sizeof(T) == 4 ? 8 : 4;  // words of eight elements
-  constexpr int kRow = D * El::bytes + kPad, kRuns = (D / 8 + 7) / 8;
+  constexpr int kRow = D * El::bytes + kPad, kRuns = kRotate ? (D / 16 + 7) / 8 * 2 : (D / 8 + 7) / 8;
   __shared__ __align__(16) char tiles[2][kBlk * kRow];
   const int head = blockIdx.x % c.kv;
   Block bl;
@@ -116,6 +87,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
   const int r = tid >> 3, sub = tid & 7;  // eight lanes a row
   const bool mine = r >= bl.lo && r < bl.hi;
   uint32_t w[2][kRuns][kWords];
+  // the run's first element (of keys in units), and whether there is such a run
+  auto at = [&](int v, int i) __attribute__((always_inline)) {
+    return kRotate && !v ? unit_at(rot, sub + 8 * (i / 2), i & 1) : 8 * (sub + 8 * i);
+  };
+  auto there = [&](int v, int i) __attribute__((always_inline)) {
+    return kRotate && !v ? D % 128 == 0 || sub + 8 * (i / 2) < D / 16
+                         : D % 64 == 0 ? i < D / 64 : sub + 8 * i < D / 8;  // (values may have fewer runs than units)
+  };
   auto load = [&](auto vec) __attribute__((always_inline)) {
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
@@ -124,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
                    (int64_t)head * src.head;
 #pragma unroll
       for (int i = 0; i < kRuns; ++i)
-        if (D % 64 == 0 || sub + 8 * i < D / 8) load8<decltype(vec)::value>(p + 8 * (sub + 8 * i), w[v][i]);
+        if (there(v, i)) load8<decltype(vec)::value>(p + at(v, i), w[v][i]);
     }
   };
   if (mine) {
@@ -132,6 +111,49 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
       load(std::true_type());
     else
       load(std::false_type());
+  }
+  if constexpr (kRotate) {
+    // (the eight lanes of a row are all `mine`, or none is)
+    const int pos = mine ? rot.pos[bl.q.row0 + bl.pos0 + r - bl.q.base] : 0;
+    const T *weight = static_cast<const T *>(k_weight);
+    float x[kRuns / 2][16], sums[kRuns / 2], sum = 0.0f;  // (summed unit by unit, as rotate_row's lanes do)
+#pragma unroll
+    for (int n = 0; n < kRuns / 2; ++n) {
+      sums[n] = 0.0f;
+      if (mine && there(0, 2 * n)) {
+        widen8(w[0][2 * n], x[n]);
+        widen8(w[0][2 * n + 1], x[n] + 8);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sums[n] = fmaf(x[n][j], x[n][j], sums[n]);
+      }
+      for (int o = 1; o < 8; o <<= 1) sums[n] += __shfl_xor(sums[n], o);
+      sum += sums[n];
+    }
+    const float f = rsqrtf(fmaf(sum, 1.0f / D, rot.eps));
+#pragma unroll
+    for (int n = 0; n < kRuns / 2; ++n)
+      if (mine && there(0, 2 * n)) {
+        const int u = sub + 8 * n;
+        if (weight) {
+          float g[16];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t b[kWords];
+            load8<true>(weight + at(0, 2 * n + h), b);
+            widen8(b, g + 8 * h);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[n][j] *= f * g[j];
+        }
+        if (u < rot.pairs / 8) {
+          float2 a[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) a[j] = angle_of(pos, rot.freq[8 * u + j]);
+          turn(x[n], a, rot.interleaved);
+        }
+        round8(x[n], w[0][2 * n]);
+        round8(x[n] + 8, w[0][2 * n + 1]);
+      }
   }
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
@@ -144,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
         if (mine)
 #pragma unroll
           for (int i = 0; i < kRuns; ++i)
-            if (D % 64 == 0 || sub + 8 * i < D / 8)
+            if (there(v, i))
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 u16x2 x;
@@ -168,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
         if (sub == 0) page[c.s_off + (v ? (1 << c.page_shift) : 0) + bl.in_page + r] = (char)byte;
 #pragma unroll
         for (int i = 0; i < kRuns; ++i)
-          if (D % 64 == 0 || sub + 8 * i < D / 8) {
+          if (there(v, i)) {
             uint32_t code[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -188,14 +210,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
                 if (x >= 0x7f80u) code[u / 4] |= 0x7fu << (8 * (u & 3));
               }
             }
-            *reinterpret_cast<uint2 *>(row + 8 * (sub + 8 * i)) = make_uint2(code[0], code[1]);
+            *reinterpret_cast<uint2 *>(row + at(v, i)) = make_uint2(code[0], code[1]);
           }
       }
     } else if (mine) {
 #pragma unroll
       for (int i = 0; i < kRuns; ++i)
-        if (D % 64 == 0 || sub + 8 * i < D / 8) {
-          u32x4 *d = reinterpret_cast<u32x4 *>(row + 8 * El::bytes * (sub + 8 * i));
+        if (there(v, i)) {
+          u32x4 *d = reinterpret_cast<u32x4 *>(row + El::bytes * at(v, i));
 #pragma unroll
           for (int j = 0; j < kWords / 4; ++j)
             d[j] = u32x4{w[v][i][4 * j], w[v][i][4 * j + 1], w[v][i][4 * j + 2], w[v][i][4 * j + 3]};
@@ -250,6 +272,37 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
     else
       *o = *s;
   }
+}
+
+// grid: (kv head, block of the chunk), sequence
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView k, RowsView kr, RowsView vr) {
+  append_block<DT, D, false>(c, k, kr, vr, RotaryView{}, nullptr);
+}
+
+// The same blocks, keys rotated, and after them (blockIdx.x from kv * blocks on) the chunk's queries, a wave for a
+// part of a row.
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void append_rotated_kernel(CacheView c, ChunkView k, RotaryView rot, HeadsView q,
+                                                                  RotatePlan plan, RowsView kr, const void *k_weight,
+                                                                  RowsView vr, int blocks) {
+  const int group = (int)blockIdx.x - c.kv * blocks;
+  if (group < 0) {
+    append_block<DT, D, true>(c, k, kr, vr, rot, k_weight);
+    return;
+  }
+  using T = typename Elem<DT>::data;
+  __shared__ float2 cs[kRotWaves][D / 2];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = group * kRotWaves + wave;
+  const Seq s = seq_of(k, c.page_shift, blockIdx.y);
+  const int row = at / plan.splits, first = at % plan.splits * plan.per;
+  if (row >= s.n) return;
+  const int last = min(first + plan.per, plan.passes);
+  const HeadsView none{};
+  if (q.in.vec && q.out.vec)
+    rotate_row<T, true>(rot, q, none, D, plan.lanes, s.row0 + row, first, last, cs[wave]);
+  else
+    rotate_row<T, false>(rot, q, none, D, plan.lanes, s.row0 + row, first, last, cs[wave]);
 }
 
 // grid as append_kernel's; the tiles hold the data type
@@ -509,6 +562,30 @@ hipError_t launch_read(const CacheView &c, int dtype, const ChunkView &k, const 
   return dtype == DT_F32    ? launch_store<DT_F32>(true, c, k, kr, vr, s)
          : dtype == DT_BF16 ? launch_store<DT_BF16>(true, c, k, kr, vr, s)
                             : launch_store<DT_F8>(true, c, k, kr, vr, s);
+}
+
+hipError_t launch_append_rotated(const CacheView &c, int dtype, const ChunkView &k, const RotaryView &r,
+                                 const HeadsView &q, const RowsView &kr, const void *k_weight, const RowsView &vr,
+                                 hipStream_t s) {
+  const int blocks = chunk_blocks(k);
+  const RotatePlan plan = rotate_plan((int64_t)k.batch * k.max_chunk, q.heads, 0, c.D);
+  const int64_t groups = ((int64_t)k.max_chunk * plan.splits + kRotWaves - 1) / kRotWaves;
+  const dim3 grid((unsigned)(c.kv * blocks + groups), k.batch);
+  auto pick = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    auto f = c.D == 64    ? append_rotated_kernel<DT, 64>
+             : c.D == 96  ? append_rotated_kernel<DT, 96>
+             : c.D == 128 ? append_rotated_kernel<DT, 128>
+                          : append_rotated_kernel<DT, 256>;
+    f<<<grid, kThreads, 0, s>>>(c, k, r, q, plan, kr, k_weight, vr, blocks);
+  };
+  if (dtype == DT_F32)
+    pick(std::integral_constant<int, DT_F32>());
+  else if (dtype == DT_BF16)
+    pick(std::integral_constant<int, DT_BF16>());
+  else
+    pick(std::integral_constant<int, DT_F8>());
+  return hipGetLastError();
 }
 
 hipError_t launch_accept(const dt_tree &t, int batch, int B, const int32_t *target, int32_t *path, int32_t *n,

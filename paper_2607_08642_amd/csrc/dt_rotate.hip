@@ -1,0 +1,49 @@
+// Heads normed and rotated by position, as rows (dt_rotate): the argument checks, how rows are dealt to waves, the kernel.
+// (With the pages of a cache: append_rotated_kernel of dt_cache.hip.)
+#include <math.h>
+
+#include "dt_rotate.h"
+
+namespace dt {
+namespace {
+
+template <typename T>
+__global__ __launch_bounds__(64 * kRotWaves) void rotate_kernel(RotaryView r, HeadsView q, HeadsView k, RotatePlan plan,
+                                                                int rows, int D) {
+  __shared__ float2 cs[kRotWaves][kMaxPairs];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t at = (int64_t)blockIdx.x * kRotWaves + wave;
+  const int64_t row = at / plan.splits;
+  if (row >= rows) return;
+  const int first = (int)(at % plan.splits) * plan.per, last = min(first + plan.per, plan.passes);
+  if (q.in.vec && q.out.vec && k.in.vec && k.out.vec)
+    rotate_row<T, true>(r, q, k, D, plan.lanes, row, first, last, cs[wave]);
+  else
+    rotate_row<T, false>(r, q, k, D, plan.lanes, row, first, last, cs[wave]);
+}
+
+}  // namespace
+
+RotatePlan rotate_plan(int64_t rows, int heads, int kv_heads, int D) {
+  RotatePlan p;
+  p.lanes = 1;
+  while (16 * p.lanes < D) p.lanes *= 2;
+  const int wide = 64 / p.lanes;
+  p.passes = (heads + wide - 1) / wide + (kv_heads + wide - 1) / wide;
+  p.splits = 1;
+  while (p.splits < p.passes && rows * p.splits < 4096) ++p.splits;
+  p.per = (p.passes + p.splits - 1) / p.splits;
+  p.splits = (p.passes + p.per - 1) / p.per;
+  return p;
+}
+
+hipError_t launch_rotate(const RotaryView &r, const HeadsView &q, const HeadsView &k, int rows, int D, int dtype,
+                         hipStream_t s) {
+  const RotatePlan plan = rotate_plan(rows, q.heads, k.heads, D);
+  const int64_t groups = ((int64_t)rows * plan.splits + kRotWaves - 1) / kRotWaves;
+  auto f = dtype == DT_F32 ? rotate_kernel<float> : rotate_kernel<uint16_t>;
+  f<<<(unsigned)groups, 64 * kRotWaves, 0, s>>>(r, q, k, plan, rows, D);
+  return hipGetLastError();
+}
+
+}  // namespace dt

@@ -1,12 +1,16 @@
 // Host side of the verification calls (paged cache, attention, commit): argument checks
 // and launches.
-#include "dt_cache.h"
+#include <cmath>
+
+#include "dt_rotate.h"
 
 namespace dt {
 namespace {
 
 // Workgroups along a grid's axis: a launch counts its threads (256 or fewer a group here) in 32 bits.
 constexpr int kMaxGroups = 1 << 24;
+
+constexpr int kMaxHeads = 1 << 20;  // of a rotation
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -106,6 +110,19 @@ void effective_window(const dt_chunk *k, const dt_attend_options *o, int *window
   *sinks = o->sinks < k->max_len ? o->sinks : k->max_len;
 }
 
+dt_status check_rotary(const dt_rotary *r, int D, RotaryView *v) {
+  if (!r || !r->positions || !r->inv_freq) return fail(DT_ERR_NULL, "rotary (positions, inv_freq) is required");
+  if (r->pairs < 8 || r->pairs % 8 || r->pairs > D / 2)
+    return fail(DT_ERR_SHAPE, "pairs must be a multiple of 8 within [8, %d] (%d)", D / 2, r->pairs);
+  if (!(r->eps >= 0.0f) || std::isinf(r->eps)) return fail(DT_ERR_SHAPE, "eps must be finite and >= 0");
+  if (reinterpret_cast<uintptr_t>(r->positions) % 4 || reinterpret_cast<uintptr_t>(r->inv_freq) % 4)
+    return fail(DT_ERR_ALIGN, "positions and inv_freq must be naturally aligned");
+  if (reinterpret_cast<uintptr_t>(r->q_weight) % 16 || reinterpret_cast<uintptr_t>(r->k_weight) % 16)
+    return fail(DT_ERR_ALIGN, "q_weight and k_weight must be 16-byte aligned");
+  *v = RotaryView{r->positions, r->inv_freq, r->pairs, r->interleaved != 0, r->eps};
+  return DT_OK;
+}
+
 struct AttendWs {
   size_t ml, part, bytes;
 };
@@ -143,6 +160,57 @@ dt_status dt_cache_append(const dt_cache *cache, int layer, const dt_chunk *chun
   const hipError_t e = launch_append(cache_view(*cache, layer), cache->dtype, chunk_view(*chunk), kr, vr,
                                      static_cast<hipStream_t>(stream));
   return e == hipSuccess ? DT_OK : hip_fail(e, "append launch");
+}
+
+dt_status dt_cache_append_rotated(const dt_cache *cache, int layer, const dt_chunk *chunk, int heads, const dt_rows *q,
+                                  const dt_rows *k, const dt_rows *v, const dt_rotary *rotary, const dt_rows *q_out,
+                                  void *stream) {
+  RowsView kr, vr;
+  HeadsView h{};
+  RotaryView r;
+  dt_status st = check_store(cache, layer, chunk, k, v, &kr, &vr);
+  if (st == DT_OK) st = check_rows(q, data_dtype(cache->dtype), "q", &h.in);
+  if (st == DT_OK) st = check_rows(q_out, data_dtype(cache->dtype), "q_out", &h.out);
+  if (st == DT_OK) st = check_rotary(rotary, cache->head_dim, &r);
+  if (st != DT_OK) return st;
+  if (heads < 1 || heads >= kMaxHeads) return fail(DT_ERR_SHAPE, "heads %d outside [1, %d)", heads, kMaxHeads);
+  if (((int64_t)chunk->max_chunk / kBlk + 3) * cache->kv_heads + (int64_t)chunk->max_chunk * heads / kRotWaves + 1 >=
+      kMaxGroups)
+    return fail(DT_ERR_UNSUPPORTED, "max_chunk, kv_heads and heads are too large together");
+  h.weight = rotary->q_weight;
+  h.heads = heads;
+  const hipError_t e = launch_append_rotated(cache_view(*cache, layer), cache->dtype, chunk_view(*chunk), r, h, kr,
+                                             rotary->k_weight, vr, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DT_OK : hip_fail(e, "append launch");
+}
+
+dt_status dt_rotate(const dt_rows *q, int heads, const dt_rows *k, int kv_heads, int rows, int D, int dtype,
+                    const dt_rotary *rotary, const dt_rows *q_out, const dt_rows *k_out, void *stream) {
+  if (dtype != DT_F32 && dtype != DT_BF16) return fail(DT_ERR_DTYPE, "dtype must be DT_F32 or DT_BF16");
+  if (rows < 1 || heads < 1 || kv_heads < 0 || (kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr))
+    return fail(DT_ERR_SHAPE, "need rows (%d) and heads (%d) positive, and kv_heads (%d) with k and k_out only", rows,
+                heads, kv_heads);
+  if (D < 16 || D > 512 || D % 16) return fail(DT_ERR_UNSUPPORTED, "D must be a multiple of 16, at most 512 (%d)", D);
+  if (heads >= kMaxHeads || kv_heads >= kMaxHeads - heads)
+    return fail(DT_ERR_UNSUPPORTED, "heads + kv_heads must be < %d", kMaxHeads);
+  HeadsView qh{}, kh{};
+  RotaryView r;
+  dt_status st = check_rows(q, dtype, "q", &qh.in);
+  if (st == DT_OK) st = check_rows(q_out, dtype, "q_out", &qh.out);
+  if (st == DT_OK && k) st = check_rows(k, dtype, "k", &kh.in);
+  if (st == DT_OK && k) st = check_rows(k_out, dtype, "k_out", &kh.out);
+  if (st == DT_OK) st = check_rotary(rotary, D, &r);
+  if (st != DT_OK) return st;
+  if (!k) kh.in.vec = kh.out.vec = 1;
+  qh.weight = rotary->q_weight;
+  kh.weight = rotary->k_weight;
+  qh.heads = heads;
+  kh.heads = kv_heads;
+  const RotatePlan p = rotate_plan(rows, heads, kv_heads, D);
+  if ((int64_t)rows * p.splits / kRotWaves + 1 >= kMaxGroups)
+    return fail(DT_ERR_UNSUPPORTED, "rows and heads are too large together");
+  const hipError_t e = launch_rotate(r, qh, kh, rows, D, dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DT_OK : hip_fail(e, "rotation launch");
 }
 
 dt_status dt_cache_read(const dt_cache *cache, int layer, const dt_chunk *chunk, const dt_rows *k, const dt_rows *v,

@@ -536,6 +536,38 @@ dt_status dt_cache_append_rotated(const dt_cache *cache, int layer, const dt_chu
                                   const dt_rows *k, const dt_rows *v, const dt_rotary *rotary, const dt_rows *q_out,
                                   void *stream);
 
+/* ---- sampling ----
+ *
+ * A token of each row of logits x [rows, V], by a given random number u in [0, 1).  In the order (logit desc,
+ * id asc), with w = exp((x - max x) / T):
+ *   top-k keeps the first k; top-p of those the ones before which the mass (the sum of w) is below
+ *   p times the mass of what top-k keeps, and the first one; min-p the ones with w >= min_p.
+ * Of what all three keep, the token is the least id at which the sum of w up to and with it passes u times the sum of all.
+ * A temperature of 0 takes the first of the order.  Off: top_k 0 (or >= V), top_p >= 1, min_p 0.
+ * Weights and sums are 64 bits (w to 4e-14 of itself); masses on the way to a border are kept to 2^-45 a token.
+ * NaN counts as -infinity, which is never taken; a row of those alone gives token -1 and
+ * a log-probability of -infinity.  Where a logit is +infinity, those alone have weights (1 each).  u outside
+ * [0, 1): the nearest inside; NaN as 0.  The results of a row do not depend on the other rows. */
+typedef struct {
+  float temperature, top_p, min_p; /* for every row, where there is no tensor for it */
+  int top_k;
+  const float *temperatures;       /* [rows] each, or NULL.  Values that a call refuses in the numbers above count here */
+  const float *top_ps, *min_ps;    /* as the nearest allowed; NaN as a temperature of 0, as off elsewhere */
+  const int32_t *top_ks;
+} dt_sampling;
+
+/* Workspace (bytes) of dt_sample. */
+dt_status dt_sample_workspace_size(int rows, int V, size_t *bytes);
+
+/* Sample tokens [rows] (int32: with a tree's root and nodes as rows, dt_tree_accept's target), and their
+ * log-probabilities within what is kept (logprobs [rows] float, may be NULL).
+ *   logits: rows of V at row_stride elements (>= 0), naturally aligned; DT_F32 or DT_BF16;  u: [rows] float;
+ *   workspace: >= dt_sample_workspace_size bytes, 256-byte aligned, not shared by calls that can overlap.
+ * 1 <= V <= 2^19, rows * (V / 8192 + 2) < 2^24.  Stream-ordered, capturable. */
+dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int logits_dtype, const float *u,
+                    const dt_sampling *how, int32_t *tokens, float *logprobs, void *workspace, size_t ws_bytes,
+                    void *stream);
+
 #ifdef __cplusplus
 }
 #endif

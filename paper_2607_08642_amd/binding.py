@@ -40,7 +40,7 @@ EXPORTS = ("dt_abi_version", "dt_status_string", "dt_last_error", "dt_plan_creat
            "dt_model_destroy", "dt_plan_create_from_model", "dt_once_workspace_size",
            "dt_build_tree_once", "dt_cache_size", "dt_cache_append", "dt_cache_read",
            "dt_attend_workspace_size", "dt_cache_attend", "dt_tree_accept", "dt_cache_commit",
-           "dt_rotate", "dt_cache_append_rotated")
+           "dt_rotate", "dt_cache_append_rotated", "dt_sample_workspace_size", "dt_sample")
 STAGES = ("scan", "expand")
 
 
@@ -102,6 +102,12 @@ class dt_rotary(ctypes.Structure):
     _fields_ = [("positions", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p), ("pairs", ctypes.c_int),
                 ("interleaved", ctypes.c_int), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
                 ("eps", ctypes.c_float)]
+
+
+class dt_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("top_k", ctypes.c_int), ("temperatures", ctypes.c_void_p), ("top_ps", ctypes.c_void_p),
+                ("min_ps", ctypes.c_void_p), ("top_ks", ctypes.c_void_p)]
 
 
 _lib = None
@@ -181,6 +187,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.dt_rotate.argtypes = [pr, ci, pr, ci, ci, ci, ci, pt, pr, pr, vp]
     lib.dt_cache_append_rotated.restype = ci
     lib.dt_cache_append_rotated.argtypes = [pc, ci, pk, ci, pr, pr, pr, pt, pr, vp]
+    lib.dt_sample_workspace_size.restype = ci
+    lib.dt_sample_workspace_size.argtypes = [ci, ci, ctypes.POINTER(sz)]
+    lib.dt_sample.restype = ci
+    lib.dt_sample.argtypes = [vp, ctypes.c_int64, ci, ci, ci, vp, ctypes.POINTER(dt_sampling), vp, vp, vp, sz, vp]
     if lib.dt_abi_version() != ABI_VERSION:
         raise RuntimeError(f"ABI mismatch: library {lib.dt_abi_version()} vs binding {ABI_VERSION}")
     _lib = lib
@@ -513,6 +523,8 @@ def _want(t, name, shape, dtype, device):
 
 def _raw_stream(torch, device: int, stream, what: str):
     """The handle of `stream` (None: torch's current one) for a call on a device, which has to be the current one."""
+    if device < 0:
+        raise ValueError(f"{what} not on a GPU")
     if torch._C._cuda_getDevice() != device:
         raise ValueError(f"{what} on device {device}, which is not the current one")
     if stream is None:
@@ -864,6 +876,65 @@ def rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float =
     if stream is not None:
         _keep(stream, q, k, positions, inv_freq, q_weight, k_weight, *out)
     return out
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, logprobs=False, workspace=None,
+           stream=None):
+    """dt_sample: a token of each row of logits [..., V] (float32 or bfloat16) by random numbers u [...] float32 in
+    [0, 1): int32 tokens [...], with a batch of trees' roots and nodes [b, B + 1, V] accept_tree's target.
+
+    temperature (0: the largest logit), top_k (0: off), top_p (1: off) and min_p (0: off): a number for every row, or a
+    tensor of u's shape (float32; top_k int32).  logprobs=True also returns the tokens' float32 log-probabilities
+    within what is kept: (tokens, logprobs).  out takes given tensors: tokens, or with logprobs both.  The last
+    dimension is contiguous, the others lie at one stride (padded rows do).  Runs on torch's current
+    stream of the tensors' device (the current one) unless one is given.
+    """
+    import torch
+    lib = load()
+    device, shape = logits.get_device(), logits.shape[:-1]
+    code = _dtype_code(logits)
+    s = _raw_stream(torch, device, stream, "logits are")
+    if len(shape) != 1:
+        try:
+            logits = logits.view(-1, logits.shape[-1])
+        except RuntimeError as e:
+            raise ValueError(f"logits: the rows do not lie at one stride ({logits.stride()})") from e
+    rows, V = logits.shape
+    if logits.stride(1) != 1 and V > 1:
+        raise ValueError(f"logits: the last dimension must be contiguous (stride {logits.stride(1)})")
+    f32, i32 = torch.float32, torch.int32
+    _want(u, "u", tuple(shape), f32, device)
+    how = dt_sampling()
+    kept = [logits, u]
+    for name, x, dtype in (("temperature", temperature, f32), ("top_k", top_k, i32), ("top_p", top_p, f32),
+                           ("min_p", min_p, f32)):
+        if isinstance(x, torch.Tensor):
+            setattr(how, name + "s", _want(x, name, tuple(shape), dtype, device).data_ptr())
+            kept.append(x)
+        else:
+            setattr(how, name, x)
+    if out is None:
+        tokens = _empty(torch, shape, i32, logits.device, stream)
+        probs = _empty(torch, shape, f32, logits.device, stream) if logprobs else None
+    else:
+        tokens, probs = out if logprobs else (out, None)
+        _want(tokens, "out", tuple(shape), i32, device)
+        if logprobs:
+            _want(probs, "out", tuple(shape), f32, device)
+    n = ctypes.c_size_t()
+    if workspace is None:
+        _check(lib.dt_sample_workspace_size(rows, V, ctypes.byref(n)))
+        workspace = _empty(torch, (n.value,), torch.uint8, logits.device, stream)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: want a contiguous tensor on cuda:{device}, got one on {workspace.device}")
+    st = lib.dt_sample(logits.data_ptr(), logits.stride(0), rows, V, code, u.data_ptr(), ctypes.byref(how),
+                       tokens.data_ptr(), _ptr(probs), workspace.data_ptr(),
+                       workspace.numel() * workspace.element_size(), s)
+    if st != 0:
+        _check(st)
+    if stream is not None:
+        _keep(stream, tokens, probs, workspace, *kept)
+    return (tokens, probs) if logprobs else tokens
 
 
 def accept_tree(tree: Tree, target, out: Optional[Accepted] = None, stream=None) -> Accepted:

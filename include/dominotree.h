@@ -503,6 +503,51 @@ dt_status dt_tree_accept(const dt_tree *tree, int batch, int B, const int32_t *t
 dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int nodes, const int32_t *path,
                           const int32_t *n_accepted, void *stream);
 
+/* ---- pages of sequences ----
+ *
+ * Which pages of a cache a batch of sequences holds, kept on the device: nothing here waits for the host, so a
+ * round's lengths (dt_tree_accept's results among them) may become pages without a copy back.
+ * Sequence b holds the pages table[b][0 .. held[b]) for lens[b] tokens; a page may be held by several (whole pages
+ * of a common beginning), uses says by how many; 0: it is free.  uses and held start as zeros, table as -1.  The books
+ * have to be consistent and lens[b] <= table_width * page_size; where they are not, no access
+ * leaves the tensors.  table and lens may be a dt_chunk's: a chunk has to lie in pages of its own, as it does
+ * at the end of a sequence grown by dt_pages_fit or made by dt_pages_fork. */
+typedef struct {
+  int pages, page_size;    /* of the cache; pages <= 2^28 */
+  int batch, table_width;  /* as dt_chunk's */
+  int32_t *uses;           /* [pages] */
+  int32_t *held;           /* [batch] */
+  int32_t *lens;           /* [batch] */
+  int32_t *table;          /* [batch, table_width]; -1 from held[b] on */
+  int32_t *missing;        /* [1] written by every call: pages that it lacked (then it did not grow or fork anything) */
+} dt_pages;
+
+/* Workspace (bytes) of the calls below, 256-byte aligned, not to be shared by calls that can overlap
+ * (pointers are not looked at). */
+dt_status dt_pages_workspace_size(const dt_pages *pages, size_t *bytes);
+
+/* Every sequence to ceil(lens[b] / page_size) pages: those past them go first (a length of 0 frees all), then
+ * the lowest free pages are taken, in the order of the sequences; if they do not suffice, no sequence grows. */
+dt_status dt_pages_fit(const dt_pages *pages, void *workspace, size_t ws_bytes, void *stream);
+
+/* Sequence b becomes a copy of sequence source[b], for all b at once (source [batch] int32; its own number or one
+ * out of range: it stays as it is): it holds the source's whole pages too and, for its last tokens, the lowest free page, into
+ * which the source's is copied in every layer; held pages past the source's length stay with it.
+ * lens follow; what it held before goes, and is free after the call.  If the free pages do not suffice, nothing changes.
+ * Samples of a prompt, beams that change places.  batch * (1 + layers * ceil(page bytes / 16384)) < 2^24. */
+dt_status dt_pages_fork(const dt_pages *pages, const dt_cache *cache, const int32_t *source, void *workspace,
+                        size_t ws_bytes, void *stream);
+
+/* The n pages in use become pages 0 .. n - 1: the r-th of those from n on moves, in every layer, to the r-th free
+ * one below n; tables follow. */
+dt_status dt_pages_compact(const dt_pages *pages, const dt_cache *cache, void *workspace, size_t ws_bytes,
+                           void *stream);
+
+/* Pages to[i] become copies of pages from[i] in every layer, i < n (device arrays, int32; pairs out of range or of
+ * one page are left out).  No page may be written twice, or written and read.  n * layers * ceil(page bytes / 16384)
+ * < 2^24. */
+dt_status dt_cache_copy_pages(const dt_cache *cache, const int32_t *from, const int32_t *to, int n, void *stream);
+
 /* ---- heads normed and rotated by position ----
  *
  * For every row and head x[0 .. D): with a weight, y = weight x / sqrt(mean(x^2) + eps), else

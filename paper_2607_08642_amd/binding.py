@@ -40,7 +40,8 @@ EXPORTS = ("dt_abi_version", "dt_status_string", "dt_last_error", "dt_plan_creat
            "dt_model_destroy", "dt_plan_create_from_model", "dt_once_workspace_size",
            "dt_build_tree_once", "dt_cache_size", "dt_cache_append", "dt_cache_read",
            "dt_attend_workspace_size", "dt_cache_attend", "dt_tree_accept", "dt_cache_commit",
-           "dt_rotate", "dt_cache_append_rotated", "dt_sample_workspace_size", "dt_sample")
+           "dt_rotate", "dt_cache_append_rotated", "dt_sample_workspace_size", "dt_sample",
+           "dt_pages_workspace_size", "dt_pages_fit", "dt_pages_fork", "dt_pages_compact", "dt_cache_copy_pages")
 STAGES = ("scan", "expand")
 
 
@@ -108,6 +109,12 @@ class dt_sampling(ctypes.Structure):
     _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
                 ("top_k", ctypes.c_int), ("temperatures", ctypes.c_void_p), ("top_ps", ctypes.c_void_p),
                 ("min_ps", ctypes.c_void_p), ("top_ks", ctypes.c_void_p)]
+
+
+class dt_pages(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("batch", ctypes.c_int),
+                ("table_width", ctypes.c_int), ("uses", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p), ("missing", ctypes.c_void_p)]
 
 
 _lib = None
@@ -191,6 +198,17 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.dt_sample_workspace_size.argtypes = [ci, ci, ctypes.POINTER(sz)]
     lib.dt_sample.restype = ci
     lib.dt_sample.argtypes = [vp, ctypes.c_int64, ci, ci, ci, vp, ctypes.POINTER(dt_sampling), vp, vp, vp, sz, vp]
+    pg = ctypes.POINTER(dt_pages)
+    lib.dt_pages_workspace_size.restype = ci
+    lib.dt_pages_workspace_size.argtypes = [pg, ctypes.POINTER(sz)]
+    lib.dt_pages_fit.restype = ci
+    lib.dt_pages_fit.argtypes = [pg, vp, sz, vp]
+    lib.dt_pages_fork.restype = ci
+    lib.dt_pages_fork.argtypes = [pg, pc, vp, vp, sz, vp]
+    lib.dt_pages_compact.restype = ci
+    lib.dt_pages_compact.argtypes = [pg, pc, vp, sz, vp]
+    lib.dt_cache_copy_pages.restype = ci
+    lib.dt_cache_copy_pages.argtypes = [pc, vp, vp, ci, vp]
     if lib.dt_abi_version() != ABI_VERSION:
         raise RuntimeError(f"ABI mismatch: library {lib.dt_abi_version()} vs binding {ABI_VERSION}")
     _lib = lib
@@ -816,6 +834,17 @@ class Cache:
             _keep(stream, self.storage, q, out, mask, depth, workspace, *chunk.tensors)
         return out
 
+    def copy_pages(self, source, to, stream=None) -> None:
+        """dt_cache_copy_pages: pages `to` [n] become copies of pages `source` [n] (int32) in every layer."""
+        n, i32 = source.numel(), self._torch.int32
+        _want(source, "source", (n,), i32, self._device)
+        _want(to, "to", (n,), i32, self._device)
+        st = self._lib.dt_cache_copy_pages(self._ref, source.data_ptr(), to.data_ptr(), n, self._stream(stream))
+        if st != 0:
+            _check(st)
+        if stream is not None:
+            _keep(stream, self.storage, source, to)
+
     def commit(self, chunk: Chunk, path, n_accepted, stream=None) -> None:
         """dt_cache_commit: the rows of the accepted nodes (Accepted.path, .n_accepted) moved together, in
         every layer; the nodes are the last path.shape[1] rows of each chunk."""
@@ -830,6 +859,64 @@ class Cache:
             _check(st)
         if stream is not None:
             _keep(stream, self.storage, path, n_accepted, *chunk.tensors)
+
+
+class Pages:
+    """dt_pages: which pages of a cache the sequences of a batch hold.
+
+    `lens` [batch] are the sequences' tokens, set by the program (in place); fit() then gives and takes pages,
+    fork() makes sequences copies of others, compact() moves the pages in use together.  `table` and `lens` may be a
+    Chunk's.  All are int32 tensors on the cache's device, views of `state`, which holds the whole books (to be saved and
+    copied back): missing [1], uses [pages], held [batch], lens, table [batch, width].
+    missing: pages that the last call lacked; it then grew and forked nothing.
+    Calls run on torch's current stream of the cache's device unless one is given; they use one workspace, so calls of one
+    Pages (captured ones too) must not overlap, as they change the same books.
+    """
+
+    def __init__(self, cache: Cache, batch: int, width: int):
+        torch = cache._torch
+        self.cache, self.batch, self.width = cache, batch, width
+        c = dt_pages(cache.pages, cache.page_size, batch, width)
+        n = ctypes.c_size_t()
+        _check(cache._lib.dt_pages_workspace_size(ctypes.byref(c), ctypes.byref(n)))
+        sizes = 1, cache.pages, batch, batch, batch * width
+        self.state = torch.zeros(sum(sizes), dtype=torch.int32, device=cache._at)
+        self.missing, self.uses, self.held, self.lens, table = self.state.split(sizes)
+        self.table = table.view(batch, width)
+        self.table.fill_(-1)
+        self._ws = torch.empty(n.value, dtype=torch.uint8, device=cache._at)
+        c.uses, c.held, c.lens, c.table, c.missing = (t.data_ptr() for t in (self.uses, self.held, self.lens, self.table,
+                                                                             self.missing))
+        self._c, self._ref, self._bytes = c, ctypes.byref(c), n.value
+
+    def fit(self, stream=None) -> None:
+        """dt_pages_fit: every sequence holds the pages of its lens, no more and, if all can be served, no fewer."""
+        cache = self.cache
+        st = cache._lib.dt_pages_fit(self._ref, self._ws.data_ptr(), self._bytes, cache._stream(stream))
+        if st != 0:
+            _check(st)
+        if stream is not None:
+            _keep(stream, self.state, self._ws)
+
+    def fork(self, source, stream=None) -> None:
+        """dt_pages_fork: sequence b becomes a copy of sequence source[b] ([batch] int32), for all b at once."""
+        cache = self.cache
+        _want(source, "source", (self.batch,), cache._torch.int32, cache._device)
+        st = cache._lib.dt_pages_fork(self._ref, cache._ref, source.data_ptr(), self._ws.data_ptr(), self._bytes,
+                                      cache._stream(stream))
+        if st != 0:
+            _check(st)
+        if stream is not None:
+            _keep(stream, self.state, self._ws, cache.storage, source)
+
+    def compact(self, stream=None) -> None:
+        """dt_pages_compact: the n pages in use become the cache's first n."""
+        cache = self.cache
+        st = cache._lib.dt_pages_compact(self._ref, cache._ref, self._ws.data_ptr(), self._bytes, cache._stream(stream))
+        if st != 0:
+            _check(st)
+        if stream is not None:
+            _keep(stream, self.state, self._ws, cache.storage)
 
 
 def _strided(t, name: str, device: int, dtype, shape) -> dt_rows:

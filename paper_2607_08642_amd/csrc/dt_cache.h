@@ -108,6 +108,9 @@ __host__ __device__ inline int v_token(int g, int j) {
 // exponents of DT_F8: byte e + 127 of 2^e
 __device__ inline float exp_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Whether a cache is one (dt_verify.hip); data: its memory too.
+dt_status check_cache(const dt_cache *c, bool data);
+
 // launchers (dt_cache.hip, dt_attend*.hip)
 struct AttendArgs {
   CacheView cache;

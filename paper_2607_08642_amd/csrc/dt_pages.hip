@@ -1,0 +1,440 @@
+// Pages of a cache (dt_pages): which of them the sequences of a batch hold, and copies of whole pages.
+//
+// The books are a few thousand numbers and every decision depends on all of them (the lowest free pages, in the order
+// of the sequences), so one workgroup keeps them: bound by latency.  Data moves in launches of their own over the whole
+// card, bound by memory traffic.
+#include "dt_cache.h"
+
+namespace dt {
+namespace {
+
+constexpr int kBookThreads = 1024, kBookWaves = kBookThreads / 64;
+constexpr int kCopyThreads = 256;
+constexpr int kCopyBytes = kCopyThreads * 16 * 4;  // of a workgroup's step
+constexpr int kMaxGroups = 1 << 24;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct Book {
+  int pages, page_size, batch, width;
+  int32_t *uses, *held, *lens, *table, *missing;
+};
+
+// What a call needs besides: lists of pages, one plan a sequence, and a new table.
+struct Scratch {
+  int32_t *head;          // [64]: how many copies, the pages in use
+  int32_t *from, *to;     // [pages] copies (fit, fork: `to` holds the free pages taken)
+  int32_t *rank;          // [pages] a moving page's place in `from`
+  int32_t *first;         // [batch] a sequence's first place in `to`
+  int32_t *source, *full; // [batch] fork: where a sequence's pages come from (-1: it keeps its own), how many are shared
+  int32_t *len;           // [batch] fork: new lengths
+  int32_t *rows;          // [batch, width] fork: new rows
+};
+
+size_t scratch(const dt_pages &p, char *at, Scratch *s) {
+  size_t n = 0;
+  auto take = [&](size_t ints) {
+    int32_t *q = reinterpret_cast<int32_t *>(at + n);
+    n += align_up(ints * 4, 256);
+    return q;
+  };
+  s->head = take(64);
+  s->from = take(p.pages);
+  s->to = take(p.pages);
+  s->rank = take(p.pages);
+  s->first = take(p.batch);
+  s->source = take(p.batch);
+  s->full = take(p.batch);
+  s->len = take(p.batch);
+  s->rows = take((size_t)p.batch * p.table_width);
+  return n;
+}
+
+// The sum over the workgroup's threads before this one, and over all.
+__device__ int before_thread(int x, int *tmp, int *whole) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int run = x;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(run, o);
+    if (lane >= o) run += y;
+  }
+  __syncthreads();
+  if (lane == 63) tmp[wave] = run;
+  __syncthreads();
+  int first = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kBookWaves; ++w) {
+    const int t = tmp[w];
+    if (w < wave) first += t;
+    all += t;
+  }
+  *whole = all;
+  return first + run - x;
+}
+
+// What other threads of the workgroup wrote to memory is there after it.
+__device__ inline void meet() {
+  __threadfence();
+  __syncthreads();
+  __threadfence();
+}
+
+__device__ inline int held_of(const Book &k, int b) { return min(max(k.held[b], 0), k.width); }
+__device__ inline int len_of(const Book &k, int b) { return min(max(k.lens[b], 0), k.width * k.page_size); }
+
+// The `want` lowest free pages into list[]; how many there are (all of them counted only where they do not suffice)
+__device__ int lowest_free(const Book &k, int want, int32_t *list, int *tmp) {
+  int found = 0;
+  for (int p0 = 0; p0 < k.pages && found < want; p0 += 4 * kBookThreads) {
+    const int p = p0 + 4 * (int)threadIdx.x;
+    int free = 0, all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < k.pages && k.uses[p + i] <= 0) free |= 1 << i;
+    int at = found + before_thread(__popc(free), tmp, &all);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (free >> i & 1) {
+        if (at < want) list[at] = p + i;
+        ++at;
+      }
+    found += all;
+  }
+  return found;
+}
+
+__global__ __launch_bounds__(kBookThreads) void fit_kernel(Book k, Scratch s) {
+  __shared__ int tmp[kBookWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // pages that go, a wave for a sequence; then how many each one lacks
+  for (int b = wave; b < k.batch; b += kBookWaves) {
+    const int want = (len_of(k, b) + k.page_size - 1) / k.page_size, held = held_of(k, b);
+    int32_t *row = k.table + (int64_t)b * k.width;
+    for (int e = want + lane; e < held; e += 64) {
+      const int p = row[e];
+      if (p >= 0 && p < k.pages) atomicSub(k.uses + p, 1);
+      row[e] = -1;
+    }
+  }
+  int total = 0;
+  for (int b0 = 0; b0 < k.batch; b0 += kBookThreads) {
+    const int b = b0 + tid;
+    int lacks = 0, all;
+    if (b < k.batch) lacks = max((len_of(k, b) + k.page_size - 1) / k.page_size - held_of(k, b), 0);
+    const int at = before_thread(lacks, tmp, &all);
+    if (b < k.batch) s.first[b] = total + at;
+    total += all;
+  }
+  meet();
+  const int found = total ? lowest_free(k, total, s.to, tmp) : 0;
+  const bool served = found >= total;
+  if (tid == 0) *k.missing = max(total - found, 0);
+  meet();
+  for (int b = wave; b < k.batch; b += kBookWaves) {
+    const int want = (len_of(k, b) + k.page_size - 1) / k.page_size, held = held_of(k, b);
+    int32_t *row = k.table + (int64_t)b * k.width;
+    if (served)
+      for (int e = held + lane; e < want; e += 64) {
+        const int p = s.to[s.first[b] + e - held];
+        row[e] = p;
+        k.uses[p] = 1;
+      }
+    if (lane == 0 && (served || want < held)) k.held[b] = want;
+  }
+}
+
+// Fork, first: where each sequence's pages come from, and a free page for each partial one.
+__global__ __launch_bounds__(kBookThreads) void fork_plan_kernel(Book k, Scratch s, const int32_t *source) {
+  __shared__ int tmp[kBookWaves];
+  const int tid = threadIdx.x;
+  int total = 0;
+  for (int b0 = 0; b0 < k.batch; b0 += kBookThreads) {
+    const int b = b0 + tid;
+    int from = -1, full = 0, part = 0, len = 0, all;
+    if (b < k.batch) {
+      from = source[b];
+      if (from < 0 || from >= k.batch || from == b) from = -1;
+      if (from >= 0) {
+        const int held = held_of(k, from);
+        len = len_of(k, from);
+        full = min(len / k.page_size, held);
+        part = full < held && len > full * k.page_size;
+      }
+    }
+    const int at = before_thread(part, tmp, &all);
+    if (b < k.batch) {
+      s.source[b] = from;
+      s.full[b] = full;
+      s.len[b] = len;
+      s.first[b] = part ? total + at : -1;
+    }
+    total += all;
+  }
+  meet();
+  const int found = total ? lowest_free(k, total, s.to, tmp) : 0;
+  if (tid == 0) {
+    *k.missing = max(total - found, 0);
+    s.head[0] = found >= total;
+  }
+}
+
+// Copy `bytes` (a multiple of 16) by a workgroup, at most kCopyBytes of them.
+__device__ __forceinline__ void copy_step(const char *from, char *to, int bytes) {
+  u32x4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = ((int)threadIdx.x + i * kCopyThreads) * 16;
+    if (at < bytes) v[i] = *reinterpret_cast<const u32x4 *>(from + at);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = ((int)threadIdx.x + i * kCopyThreads) * 16;
+    if (at < bytes) *reinterpret_cast<u32x4 *>(to + at) = v[i];
+  }
+}
+
+// Steps of a copy of a page in every layer, and one of them.
+struct Copies {
+  CacheView c;  // layer 0
+  int layers, steps;  // steps of a page of a layer
+  int64_t layer_bytes;
+};
+__device__ __forceinline__ void copy_part(const Copies &c, int from, int to, int part) {
+  const int64_t at = (int64_t)(part / c.steps) * c.layer_bytes + (int64_t)(part % c.steps) * kCopyBytes;
+  const int64_t left = c.c.page_bytes - (int64_t)(part % c.steps) * kCopyBytes;
+  copy_step(c.c.base + from * c.c.page_bytes + at, c.c.base + to * c.c.page_bytes + at,
+            left < kCopyBytes ? (int)left : kCopyBytes);
+}
+
+// Fork, second: new rows and their uses (workgroups [0, batch)), copies of partial pages.  Nothing that is read
+// here changes here: pages copied into are free, rows are put together apart.
+__global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Book k, Scratch s, Copies c) {
+  if (!s.head[0]) return;
+  const int parts = c.layers * c.steps;
+  if ((int)blockIdx.x < k.batch) {
+    const int b = blockIdx.x, from = s.source[b];
+    if (from < 0) return;
+    const int full = s.full[b];
+    const int32_t *old = k.table + (int64_t)from * k.width;
+    int32_t *row = s.rows + (int64_t)b * k.width;
+    for (int e = threadIdx.x; e < full; e += kCopyThreads) {
+      const int p = old[e];
+      row[e] = p;
+      if (p >= 0 && p < k.pages) atomicAdd(k.uses + p, 1);
+    }
+    if (threadIdx.x == 0 && s.first[b] >= 0) {
+      row[full] = s.to[s.first[b]];
+      k.uses[row[full]] = 1;
+    }
+    return;
+  }
+  const int b = ((int)blockIdx.x - k.batch) / parts;
+  if (s.source[b] < 0 || s.first[b] < 0) return;
+  const int p = k.table[(int64_t)s.source[b] * k.width + s.full[b]];
+  if (p >= 0 && p < k.pages) copy_part(c, p, s.to[s.first[b]], ((int)blockIdx.x - k.batch) % parts);
+}
+
+// Fork, third: the old rows' uses go, the new rows and lengths come.
+__global__ __launch_bounds__(kCopyThreads) void fork_rows_kernel(Book k, Scratch s) {
+  const int b = blockIdx.x;
+  if (!s.head[0] || s.source[b] < 0) return;
+  const int now = s.full[b] + (s.first[b] >= 0), held = held_of(k, b);
+  int32_t *row = k.table + (int64_t)b * k.width;
+  const int32_t *next = s.rows + (int64_t)b * k.width;
+  for (int e = threadIdx.x; e < max(held, now); e += kCopyThreads) {
+    const int p = row[e];
+    if (e < held && p >= 0 && p < k.pages) atomicSub(k.uses + p, 1);
+    row[e] = e < now ? next[e] : -1;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    k.held[b] = now;
+    k.lens[b] = s.len[b];
+  }
+}
+// Compact, first: the pages in use that lie beyond their number, and the free ones before it.
+__global__ __launch_bounds__(kBookThreads) void compact_plan_kernel(Book k, Scratch s) {
+  __shared__ int tmp[kBookWaves];
+  const int tid = threadIdx.x;
+  int mine = 0, live;
+  for (int p = tid; p < k.pages; p += kBookThreads) mine += k.uses[p] > 0;
+  before_thread(mine, tmp, &live);
+  int moves = 0, holes = 0;
+  for (int p0 = 0; p0 < k.pages; p0 += kBookThreads) {
+    const int p = p0 + tid;
+    const bool used = p < k.pages && k.uses[p] > 0;
+    const int high = used && p >= live, hole = p < live && !used;
+    int all_high, all_hole;
+    const int at_high = moves + before_thread(high, tmp, &all_high), at_hole = holes + before_thread(hole, tmp, &all_hole);
+    if (high) {
+      s.from[at_high] = p;
+      s.rank[p] = at_high;
+    }
+    if (hole) s.to[at_hole] = p;
+    moves += all_high;
+    holes += all_hole;
+  }
+  meet();
+  for (int i = tid; i < moves; i += kBookThreads) {
+    k.uses[s.to[i]] = k.uses[s.from[i]];
+    k.uses[s.from[i]] = 0;
+  }
+  if (tid == 0) {
+    s.head[0] = moves;
+    s.head[1] = live;
+    *k.missing = 0;
+  }
+}
+
+// Compact, second: the table's entries (workgroups [0, batch)), the pages' data.
+__global__ __launch_bounds__(kCopyThreads) void compact_copy_kernel(Book k, Scratch s, Copies c, int copiers) {
+  const int moves = s.head[0], live = s.head[1];
+  if (moves == 0) return;
+  if ((int)blockIdx.x < k.batch) {
+    int32_t *row = k.table + (int64_t)blockIdx.x * k.width;
+    const int held = held_of(k, blockIdx.x);
+    for (int e = threadIdx.x; e < held; e += kCopyThreads) {
+      const int p = row[e];
+      if (p >= live && p < k.pages) {
+        const int r = s.rank[p];
+        if (r >= 0 && r < moves && s.from[r] == p) row[e] = s.to[r];
+      }
+    }
+    return;
+  }
+  const int parts = c.layers * c.steps;
+  for (int64_t i = (int)blockIdx.x - k.batch; i < (int64_t)moves * parts; i += copiers)
+    copy_part(c, s.from[i / parts], s.to[i / parts], (int)(i % parts));
+}
+
+__global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(Copies c, const int32_t *from, const int32_t *to) {
+  const int parts = c.layers * c.steps, i = blockIdx.x / parts, f = from[i], t = to[i];
+  if (f >= 0 && f < c.c.pages && t >= 0 && t < c.c.pages && f != t) copy_part(c, f, t, blockIdx.x % parts);
+}
+
+Copies copies_of(const dt_cache &cache) {
+  Copies c;
+  c.c = cache_view(cache, 0);
+  c.layers = cache.layers;
+  c.steps = (int)((c.c.page_bytes + kCopyBytes - 1) / kCopyBytes);
+  c.layer_bytes = c.c.page_bytes * cache.pages;
+  return c;
+}
+
+dt_status check_pages(const dt_pages *p, bool data) {
+  if (!p) return fail(DT_ERR_NULL, "pages is required");
+  if (p->pages < 1 || p->batch < 1 || p->table_width < 1)
+    return fail(DT_ERR_SHAPE, "sizes must be positive (pages=%d batch=%d table_width=%d)", p->pages, p->batch,
+                p->table_width);
+  if (p->page_size != 32 && p->page_size != 64 && p->page_size != 128 && p->page_size != 256)
+    return fail(DT_ERR_UNSUPPORTED, "page_size must be 32, 64, 128 or 256 (%d)", p->page_size);
+  if (p->pages > 1 << 28 || p->batch > 65535 || (int64_t)p->table_width * p->page_size >= (int64_t)1 << 30)
+    return fail(DT_ERR_UNSUPPORTED, "need pages <= 2^28, batch <= 65535, table_width * page_size < 2^30");
+  if (!data) return DT_OK;
+  for (const void *q : {(const void *)p->uses, (const void *)p->held, (const void *)p->lens, (const void *)p->table,
+                        (const void *)p->missing}) {
+    if (!q) return fail(DT_ERR_NULL, "uses, held, lens, table and missing are required");
+    if (reinterpret_cast<uintptr_t>(q) % 4) return fail(DT_ERR_ALIGN, "tensors must be naturally aligned");
+  }
+  return DT_OK;
+}
+
+dt_status check_scratch(const dt_pages *p, void *workspace, size_t bytes, Scratch *s) {
+  const size_t need = scratch(*p, static_cast<char *>(workspace), s);
+  if (!workspace || bytes < need)
+    return fail(DT_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, workspace ? bytes : 0);
+  if (reinterpret_cast<uintptr_t>(workspace) % 256) return fail(DT_ERR_ALIGN, "workspace must be 256-byte aligned");
+  return DT_OK;
+}
+
+dt_status check_both(const dt_pages *p, const dt_cache *cache) {
+  dt_status st = check_pages(p, true);
+  if (st == DT_OK) st = check_cache(cache, true);
+  if (st == DT_OK && (cache->pages != p->pages || cache->page_size != p->page_size))
+    st = fail(DT_ERR_SHAPE, "the cache has %d pages of %d tokens, the books %d of %d", cache->pages, cache->page_size,
+              p->pages, p->page_size);
+  return st;
+}
+
+Book book_of(const dt_pages &p) {
+  return Book{p.pages, p.page_size, p.batch, p.table_width, p.uses, p.held, p.lens, p.table, p.missing};
+}
+
+}  // namespace
+}  // namespace dt
+
+using namespace dt;
+
+extern "C" {
+
+dt_status dt_pages_workspace_size(const dt_pages *pages, size_t *bytes) {
+  if (!bytes) return fail(DT_ERR_NULL, "bytes is required");
+  const dt_status st = check_pages(pages, false);
+  if (st != DT_OK) return st;
+  Scratch s;
+  *bytes = scratch(*pages, nullptr, &s);
+  return DT_OK;
+}
+
+dt_status dt_pages_fit(const dt_pages *pages, void *workspace, size_t ws_bytes, void *stream) {
+  Scratch s;
+  dt_status st = check_pages(pages, true);
+  if (st == DT_OK) st = check_scratch(pages, workspace, ws_bytes, &s);
+  if (st != DT_OK) return st;
+  fit_kernel<<<1, kBookThreads, 0, static_cast<hipStream_t>(stream)>>>(book_of(*pages), s);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DT_OK : hip_fail(e, "pages launch");
+}
+
+dt_status dt_pages_fork(const dt_pages *pages, const dt_cache *cache, const int32_t *source, void *workspace,
+                        size_t ws_bytes, void *stream) {
+  Scratch s;
+  dt_status st = check_both(pages, cache);
+  if (st == DT_OK) st = check_scratch(pages, workspace, ws_bytes, &s);
+  if (st != DT_OK) return st;
+  if (!source) return fail(DT_ERR_NULL, "source is required");
+  if (reinterpret_cast<uintptr_t>(source) % 4) return fail(DT_ERR_ALIGN, "source must be naturally aligned");
+  const Book k = book_of(*pages);
+  const Copies c = copies_of(*cache);
+  const int64_t groups = k.batch + (int64_t)k.batch * c.layers * c.steps;
+  if (groups >= kMaxGroups) return fail(DT_ERR_UNSUPPORTED, "batch, layers and pages are too large together");
+  hipStream_t q = static_cast<hipStream_t>(stream);
+  fork_plan_kernel<<<1, kBookThreads, 0, q>>>(k, s, source);
+  fork_copy_kernel<<<(unsigned)groups, kCopyThreads, 0, q>>>(k, s, c);
+  fork_rows_kernel<<<k.batch, kCopyThreads, 0, q>>>(k, s);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DT_OK : hip_fail(e, "pages launch");
+}
+
+dt_status dt_pages_compact(const dt_pages *pages, const dt_cache *cache, void *workspace, size_t ws_bytes,
+                           void *stream) {
+  Scratch s;
+  dt_status st = check_both(pages, cache);
+  if (st == DT_OK) st = check_scratch(pages, workspace, ws_bytes, &s);
+  if (st != DT_OK) return st;
+  const Book k = book_of(*pages);
+  const Copies c = copies_of(*cache);
+  const int64_t most = (int64_t)(k.pages / 2) * c.layers * c.steps;  // (a page that moves leaves one for a hole)
+  const int copiers = (int)(most < 8192 ? most : 8192);
+  hipStream_t q = static_cast<hipStream_t>(stream);
+  compact_plan_kernel<<<1, kBookThreads, 0, q>>>(k, s);
+  compact_copy_kernel<<<(unsigned)(k.batch + copiers), kCopyThreads, 0, q>>>(k, s, c, copiers);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DT_OK : hip_fail(e, "pages launch");
+}
+
+dt_status dt_cache_copy_pages(const dt_cache *cache, const int32_t *from, const int32_t *to, int n, void *stream) {
+  const dt_status st = check_cache(cache, true);
+  if (st != DT_OK) return st;
+  if (!from || !to) return fail(DT_ERR_NULL, "from and to are required");
+  if (reinterpret_cast<uintptr_t>(from) % 4 || reinterpret_cast<uintptr_t>(to) % 4)
+    return fail(DT_ERR_ALIGN, "from and to must be naturally aligned");
+  if (n < 1) return fail(DT_ERR_SHAPE, "n must be positive (%d)", n);
+  const Copies c = copies_of(*cache);
+  if ((double)n * c.layers * c.steps >= kMaxGroups) return fail(DT_ERR_UNSUPPORTED, "too many pages in one call");
+  copy_pages_kernel<<<(unsigned)(n * c.layers * c.steps), kCopyThreads, 0, static_cast<hipStream_t>(stream)>>>(c, from, to);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? DT_OK : hip_fail(e, "copy launch");
+}
+
+}  // extern "C"

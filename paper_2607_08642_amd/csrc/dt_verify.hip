@@ -5,16 +5,8 @@
 #include "dt_rotate.h"
 
 namespace dt {
-namespace {
 
-// Workgroups along a grid's axis: a launch counts its threads (256 or fewer a group here) in 32 bits.
-constexpr int kMaxGroups = 1 << 24;
-
-constexpr int kMaxHeads = 1 << 20;  // of a rotation
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-bool positive_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
+static bool positive_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 dt_status check_cache(const dt_cache *c, bool data) {
   if (!c) return fail(DT_ERR_NULL, "cache is required");
@@ -35,6 +27,15 @@ dt_status check_cache(const dt_cache *c, bool data) {
     return fail(DT_ERR_ALIGN, "cache.data must be 256-byte aligned");
   return DT_OK;
 }
+
+namespace {
+
+// Workgroups along a grid's axis: a launch counts its threads (256 or fewer a group here) in 32 bits.
+constexpr int kMaxGroups = 1 << 24;
+
+constexpr int kMaxHeads = 1 << 20;  // of a rotation
+
+constexpr float kLog2e = 1.4426950408889634f;
 
 dt_status check_layer(const dt_cache *c, int layer) {
   if (layer < 0 || layer >= c->layers) return fail(DT_ERR_SHAPE, "layer %d outside [0, %d)", layer, c->layers);

@@ -16,13 +16,19 @@
 namespace dt {
 namespace {
 
+typedef unsigned long long u64;
+
 constexpr int kSeg = 2048;          // elements of a segment
 constexpr int kLane = kSeg / 64;    // of them with one lane
 constexpr int kMaxV = 1 << 19;
 constexpr int kMaxSegs = kMaxV / kSeg + 1;   // (a row may begin inside a 16-byte piece)
 constexpr int kWaves = 4;           // of a workgroup of segments_kernel
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
+constexpr int kGroupLanes = 4, kGroups = 64 / kGroupLanes;  // a segment's maxima are kept for groups of 128 elements
 constexpr int kBins = 2048;
+constexpr int kList = 1024;  // elements that a row's end is found among in LDS
+constexpr int kFew = kRowThreads;  // elements ranked by a thread each
+constexpr int kPart = 8;     // segments (waves) of a workgroup of the passes for large rows
 constexpr int kMaxGroups = 1 << 24;
 constexpr double kOne = 17592186044416.0;  // 2^44: masses in the bins are whole numbers of 2^-44 (2^19 of them fit 63 bits)
 
@@ -45,6 +51,9 @@ struct Row {
   double p, q;
   int k;
   bool greedy;
+  __device__ bool filters() const { return k || p <= 1.0 || q > 0.0; }
+  // whether the weights of all elements are summed: nothing is left out, or top-p is of all
+  __device__ bool sums() const { return !greedy && !k && (p <= 1.0 || !(q > 0.0)); }
 };
 __device__ inline Row row_of(const Settings &s, int row, int V) {
   const float t = s.temperatures ? s.temperatures[row] : s.temperature;
@@ -76,7 +85,7 @@ __device__ __forceinline__ double pow2(double t) {
   return ldexp(fma(g, f, 1.0), (int)n);
 }
 
-// the weight of x against a maximum m (an infinite maximum: its equals alone)
+// the weight of x against a maximum m (of infinities alone: 1 each; the segments that have one count, if any has)
 __device__ __forceinline__ double weight(float x, float m, double a) {
   if (m == INFINITY) return x == m ? 1.0 : 0.0;
   return pow2(((double)x - (double)m) * a);
@@ -92,11 +101,18 @@ __device__ __forceinline__ float value(T x) {
   return v == v ? v : -INFINITY;  // (NaN: never chosen)
 }
 
-// A row as segments of aligned 16-byte pieces: element i of segment s has the id s * kSeg + i - before.
+// A row as segments of aligned 16-byte pieces: element i of segment s has the id s * kSeg + i - before.  Where the
+// maximum is +infinity, its equals are read as 0 and the rest as -infinity.
 template <typename T>
 struct RowAt {
   const T *base;
   int before, V;
+  bool infinite;
+
+  __device__ __forceinline__ float at(T x) const {
+    const float v = value(x);
+    return infinite ? v == INFINITY ? 0.0f : -INFINITY : v;
+  }
 };
 template <typename T>
 __device__ inline RowAt<T> row_at(const Logits &l, int row) {
@@ -105,10 +121,11 @@ __device__ inline RowAt<T> row_at(const Logits &l, int row) {
   r.before = (int)(reinterpret_cast<uintptr_t>(p) % 16) / (int)sizeof(T);
   r.base = reinterpret_cast<const T *>(p) - r.before;
   r.V = l.V;
+  r.infinite = false;
   return r;
 }
 
-// N elements from `at` (a multiple of a piece) of the row's pieces on; those that are not the row's: -infinity
+// N elements from place `at` (a multiple of a piece, or within one) of the row on; those that are not the row's: -infinity
 template <int N, typename T>
 __device__ __forceinline__ void load_run(const RowAt<T> &r, int at, float *x) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -120,23 +137,27 @@ __device__ __forceinline__ void load_run(const RowAt<T> &r, int at, float *x) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if constexpr (sizeof(T) == 4)
-        x[i] = value<uint32_t>(w[i]);
+        x[i] = r.at(w[i]);
       else
-        x[i] = value<uint16_t>((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+        x[i] = r.at((uint16_t)(w[i / 2] >> (16 * (i & 1))));
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = at + i >= lo && at + i < hi ? value<T>(r.base[at + i]) : -INFINITY;
+    for (int i = 0; i < N; ++i) x[i] = at + i >= lo && at + i < hi ? r.at(r.base[at + i]) : -INFINITY;
   }
 }
 
-// A segment by a wave: lane l holds piece l + 64 j as x[j * piece ..]; its first element's place
+// The place of piece j of a lane in a segment's order: lane l holds pieces l + 64 j.
+template <typename T>
+__device__ __forceinline__ int piece_at(int seg, int lane, int j) {
+  return seg * kSeg + (j * 64 + lane) * (16 / (int)sizeof(T));
+}
 template <typename T>
 __device__ __forceinline__ void load_segment(const RowAt<T> &r, int seg, float (&x)[kLane]) {
   constexpr int kPiece = 16 / sizeof(T);
 #pragma unroll
   for (int j = 0; j < kLane / kPiece; ++j)
-    load_run<kPiece>(r, seg * kSeg + (j * 64 + (threadIdx.x & 63)) * kPiece, x + j * kPiece);
+    load_run<kPiece>(r, piece_at<T>(seg, threadIdx.x & 63, j), x + j * kPiece);
 }
 
 __device__ inline double wave_sum(double x) {
@@ -148,7 +169,7 @@ __device__ inline double wave_sum(double x) {
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Settings s, int groups, float *maxima,
                                                                double *sums) {
-  const int row = blockIdx.x / groups;
+  const int row = blockIdx.x / groups, lane = threadIdx.x & 63;
   const int seg = (int)(blockIdx.x % groups) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (seg >= l.segs) return;
   const RowAt<T> r = row_at<T>(l, row);
@@ -157,21 +178,22 @@ __global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Setting
   float m = x[0];
 #pragma unroll
   for (int i = 1; i < kLane; ++i) m = fmaxf(m, x[i]);
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  for (int o = 1; o < kGroupLanes; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   const Row ask = row_of(s, row, l.V);
   const int64_t at = (int64_t)row * l.segs + seg;
-  if ((threadIdx.x & 63) == 0) maxima[at] = m;
-  if (ask.greedy || ask.k || (ask.q > 0.0 && ask.p > 1.0)) return;  // (no sum over all is asked for)
+  if (lane % kGroupLanes == 0) maxima[at * kGroups + lane / kGroupLanes] = m;
+  if (!ask.sums()) return;
+  for (int o = kGroupLanes; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   double z = 0.0;
   if (m > -INFINITY) {
 #pragma unroll
     for (int i = 0; i < kLane; ++i) z += weight(x[i], m, ask.a);
     z = wave_sum(z);
   }
-  if ((threadIdx.x & 63) == 0) sums[at] = z;
+  if (lane == 0) sums[at] = z;
 }
 
-// Sums over a workgroup of row_kernel in the order of its threads: what comes before a thread, and the whole.
+// Sums over a workgroup in the order of its threads: what comes before a thread, and the whole.
 template <typename N>
 __device__ N before_thread(N x, N *tmp, N *whole) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -186,8 +208,9 @@ __device__ N before_thread(N x, N *tmp, N *whole) {
   N first = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kRowWaves; ++w) {
-    if (w < wave) first += tmp[w];
-    all += tmp[w];
+    const N t = tmp[w];
+    if (w < wave) first += t;
+    all += t;
   }
   *whole = all;
   return first + (run - x);
@@ -202,18 +225,54 @@ __device__ inline int block_min(int x, int *tmp) {
   for (int w = 0; w < kRowWaves; ++w) x = min(x, tmp[w]);
   return x;
 }
+// floats by their order (no NaN)
+__device__ inline float block_max(float x, int *tmp) {
+  const int top = block_min(~(int)(ordered_bits(x) ^ 0x80000000u), tmp);
+  return ordered_to_float((uint32_t)~top ^ 0x80000000u);
+}
+__device__ inline float block_min(float x, int *tmp) {
+  const int low = block_min((int)(ordered_bits(x) ^ 0x80000000u), tmp);
+  return ordered_to_float((uint32_t)low ^ 0x80000000u);
+}
+
+// Whole numbers in bins, found again by their running sums.
+struct Bins {
+  uint32_t count[kBins];
+  u64 mass[kBins];
+};
 
 struct Shared {
-  float maxima[kMaxSegs];
-  double mass[kMaxSegs];   // of a segment's kept elements
-  int ties[kMaxSegs];      // its elements at the border
-  uint32_t count[kBins];
-  unsigned long long bin[kBins];
+  float groups[kMaxSegs * kGroups];  // maxima
+  double mass[kMaxSegs];             // of a segment's kept elements
+  int ties[kMaxSegs];                // its elements at the border
+  union {
+    Bins bins;
+    struct {
+      u64 few[kFew];
+    };
+  };
+  u64 list[kList];   // keys (make_key) of candidates
   double tmp_d[kRowWaves];
-  unsigned long long tmp_u[kRowWaves];
+  u64 tmp_u[kRowWaves];
   int tmp_i[kRowWaves];
-  int at;
+  int at, n;
+  u64 u;
   double before;
+};
+
+// What the large rows of a call pass from one launch to the next.
+struct Large {
+  int on;            // 1: the border is looked for in bins; 2: all from `lo` on is kept
+  float m, lo, scale;
+  double whole;
+  int infinite, listed;
+};
+
+struct Work {
+  Large *large;  // [rows], NULL: no row of the call can be one
+  u64 *bins;     // [rows][kBins]
+  u64 *list;     // [rows][kList] the elements in the border's bin
+  u64 *above;    // [rows] the mass before that bin
 };
 
 // Where an order's prefix ends: elements above `key` are kept, and `ties` of those equal to it.
@@ -222,6 +281,11 @@ struct Border {
   int ties;
   double mass;  // of what is kept
 };
+
+__device__ __forceinline__ u64 whole_number(double w) { return (u64)(w * kOne + 0.5); }
+
+// bins of equal ranges of values from m down, monotone in x
+__device__ __forceinline__ int bin_of(float x, float m, float scale) { return min((int)((m - x) * scale), kBins - 1); }
 
 // One workgroup's view of its row.
 template <typename T>
@@ -232,125 +296,184 @@ struct Finish {
   int segs;
   float m;
 
+  __device__ float segment_max(int seg) const {
+    float x = sh.groups[seg * kGroups];
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) x = fmaxf(x, sh.groups[seg * kGroups + g]);
+    return x;
+  }
+
   // f(segment, elements) by the waves for every segment with an element >= lo
   template <typename F>
   __device__ void each_segment(float lo, F f) {
     for (int seg = threadIdx.x >> 6; seg < segs; seg += kRowWaves) {
-      if (sh.maxima[seg] < lo || sh.maxima[seg] == -INFINITY) continue;
+      const float top = segment_max(seg);
+      if (top < lo || top == -INFINITY) continue;
       float x[kLane];
       load_segment(r, seg, x);
       f(seg, x);
     }
   }
 
+  __device__ void clear_bins() {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kRowThreads) sh.bins.count[i] = 0, sh.bins.mass[i] = 0;
+    __syncthreads();
+  }
+  __device__ void add(int bin, double w) {
+    atomicAdd(&sh.bins.count[bin], 1u);
+    atomicAdd(&sh.bins.mass[bin], whole_number(w));
+  }
+
+  // The first bin (from `first_bin` 0 up) at which f(elements, mass up to and with it) holds; the last that has
+  // any, if none.  *n, *w: what lies before it; *all_w: all masses.
+  template <typename F>
+  __device__ int find_bin(F f, int *n_before, u64 *w_before, u64 *all) {
+    __syncthreads();
+    constexpr int kEach = kBins / kRowThreads;
+    uint32_t n[kEach];
+    u64 w[kEach], sum_w = 0, all_w;
+    int sum_n = 0, all_n;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      n[i] = sh.bins.count[kEach * threadIdx.x + i];
+      w[i] = sh.bins.mass[kEach * threadIdx.x + i];
+      sum_n += (int)n[i];
+      sum_w += w[i];
+    }
+    const int before_n = before_thread(sum_n, sh.tmp_i, &all_n);
+    const u64 before_w = before_thread(sum_w, sh.tmp_u, &all_w);
+    int mine = 2 * kBins, run_n = before_n;
+    u64 run_w = before_w;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      run_n += (int)n[i];
+      run_w += w[i];
+      if (!n[i]) continue;
+      const int at = kEach * (int)threadIdx.x + i;
+      if (f(run_n, run_w)) mine = min(mine, at);
+      else if (run_n == all_n) mine = min(mine, at + kBins);   // (the last)
+    }
+    const int found = block_min(mine, sh.tmp_i), bin = found % kBins;
+    if (mine == found && found < 2 * kBins) {
+      int at_n = before_n;
+      u64 at_w = before_w;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (kEach * (int)threadIdx.x + i < bin) at_n += (int)n[i], at_w += w[i];
+      sh.at = at_n;
+      sh.u = at_w;
+    }
+    __syncthreads();
+    *n_before = sh.at;
+    *w_before = sh.u;
+    *all = all_w;
+    return found < 2 * kBins ? bin : -1;
+  }
+
   // The border of the first `want` elements (by_mass: of the elements before which the mass is below `want`), known to
-  // lie at keys >= key(lo).  Bins of equal ranges of keys, then of the border's bin, until a bin is a key.
+  // lie at keys >= key(lo), by passes over the row: bins of equal ranges of keys, then of the border's
+  // bin, until a bin is a key.  Right for every row, and the slowest way.
   __device__ Border select(bool by_mass, double want, float lo_value) {
     uint32_t lo = ordered_bits(lo_value), hi = ordered_bits(m);
-    double above_n = 0.0;
-    unsigned long long above_m = 0;
+    int above_n = 0;
+    u64 above_w = 0;
     for (;;) {
       const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
-      for (int i = threadIdx.x; i < kBins; i += kRowThreads) sh.count[i] = 0, sh.bin[i] = 0;
-      __syncthreads();
+      clear_bins();
       each_segment(ordered_to_float(lo), [&](int, const float (&x)[kLane]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kLane; ++i) {
           const uint32_t key = ordered_bits(x[i]);
           if (key < lo || key > hi || x[i] == -INFINITY) continue;
-          const int b = (int)((key - lo) >> shift);
-          atomicAdd(&sh.count[b], 1u);
-          atomicAdd(&sh.bin[b], (unsigned long long)(weight(x[i], m, ask.a) * kOne + 0.5));
+          add((int)((hi - key) >> shift), weight(x[i], m, ask.a));
         }
       });
+      int n;
+      u64 w, all;
+      const int b = find_bin([&](int run_n, u64 run_w) {
+        return by_mass ? (double)(above_w + run_w) / kOne >= want : (double)above_n + run_n >= want;
+      }, &n, &w, &all);
+      above_n += n;
+      above_w += w;
+      const int here = (int)sh.bins.count[b];
       __syncthreads();
-      // the bins from the top: thread t has bins top - 4 t .. top - 4 t - 3
-      constexpr int kEach = kBins / kRowThreads;
-      uint32_t n[kEach];
-      unsigned long long w[kEach], sum_w = 0, all_w;
-      int sum_n = 0, all_n;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int b = kBins - 1 - (kEach * (int)threadIdx.x + i);
-        n[i] = sh.count[b];
-        w[i] = sh.bin[b];
-        sum_n += (int)n[i];
-        sum_w += w[i];
-      }
-      int run_n = before_thread(sum_n, sh.tmp_i, &all_n);
-      unsigned long long run_w = before_thread(sum_w, sh.tmp_u, &all_w);
-      // the first bin (from the top) whose elements reach the wanted number or mass; else the last that has any
-      int mine = kBins;
-      const bool reaches = by_mass ? (double)(above_m + all_w) / kOne >= want : above_n + all_n >= want;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        run_n += (int)n[i];
-        run_w += w[i];
-        const bool there = reaches ? (by_mass ? (double)(above_m + run_w) / kOne >= want : above_n + run_n >= want)
-                                   : run_n == all_n;
-        if (there && n[i] && mine == kBins) mine = kEach * (int)threadIdx.x + i;
-      }
-      const int found = block_min(mine, sh.tmp_i);   // (counted from the top)
-      if (mine == found && found < kBins) {
-        const int i = found - kEach * (int)threadIdx.x;
-        int n_above = run_n;
-        unsigned long long w_above = run_w;
-#pragma unroll
-        for (int j = kEach - 1; j >= 0; --j)
-          if (j >= i) n_above -= (int)n[j], w_above -= w[j];
-        sh.at = n_above;
-        sh.tmp_u[0] = w_above;
-      }
-      __syncthreads();
-      const int b = kBins - 1 - found;
-      above_n += sh.at;
-      above_m += sh.tmp_u[0];
-      const int here = (int)sh.count[b];
-      __syncthreads();
-      lo += (uint32_t)b << shift;
-      hi = min(hi, lo + ((1u << shift) - 1));
+      hi -= (uint32_t)b << shift;
+      lo = max(lo, hi - min(hi, (1u << shift) - 1));
       if (shift == 0) {
         Border o;
         o.key = lo;
-        const double w1 = weight(ordered_to_float(lo), m, ask.a), mass = (double)above_m / kOne;
+        const double w1 = weight(ordered_to_float(lo), m, ask.a), mass = (double)above_w / kOne;
         double ties = by_mass ? ceil((want - mass) / w1) : want - above_n;
         if (!(ties < (double)here)) ties = here;   // (NaN: a weight of 0)
-        o.ties = max((int)ties, above_n > 0.0 ? 0 : 1);
+        o.ties = max((int)ties, above_n > 0 ? 0 : 1);
         o.mass = mass + o.ties * w1;
         return o;
       }
     }
   }
 
+  // The kept mass of every segment: what lies above the border and, in the order of ids, the ties.
+  __device__ void segment_masses(const Border &edge, float lo) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < segs; i += kRowThreads) sh.mass[i] = 0.0, sh.ties[i] = 0;
+    __syncthreads();
+    each_segment(lo, [&](int seg, const float (&x)[kLane]) __attribute__((always_inline)) {
+      double z = 0.0;
+      int ties = 0;
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) {
+        const uint32_t key = ordered_bits(x[i]);
+        if (x[i] < lo || x[i] == -INFINITY) continue;
+        if (key == edge.key) {
+          ++ties;
+        } else if (key > edge.key) {
+          const double w = weight(x[i], m, ask.a);
+          if (w >= ask.q) z += w;
+        }
+      }
+      z = wave_sum(z);
+      for (int o = 1; o < 64; o <<= 1) ties += __shfl_xor(ties, o);
+      if ((threadIdx.x & 63) == 0) sh.mass[seg] = z, sh.ties[seg] = ties;
+    });
+    __syncthreads();
+    if (!edge.key) return;
+    double w = weight(ordered_to_float(edge.key), m, ask.a);
+    if (w < ask.q) w = 0.0;
+    int t = 0, all;
+    const int each = (segs + kRowThreads - 1) / kRowThreads, first = (int)threadIdx.x * each;
+    for (int i = first; i < min(first + each, segs); ++i) t += sh.ties[i];
+    int run = before_thread(t, sh.tmp_i, &all);
+    for (int i = first; i < min(first + each, segs); ++i) {
+      sh.mass[i] += min(max(edge.ties - run, 0), sh.ties[i]) * w;
+      run += sh.ties[i];
+    }
+    __syncthreads();
+  }
+
   // The element where the running sum of kept weights, in the order of ids, passes u of the whole: segment masses are in
-  // sh.mass, ties in sh.ties.  All threads return it; weight: its own, whole: of all kept.
+  // sh.mass, ties in sh.ties.  All threads return it; own: its weight, whole: of all kept.
   __device__ int pick(double u, const Border &edge, double *own, double *whole) {
     double z = 0.0, left = 0.0;
     int tied = 0;
-    // (a few hundred segments: every thread would add the same numbers; one wave's lanes take a run each)
-    const int each = (segs + kRowThreads - 1) / kRowThreads;
+    const int each = (segs + kRowThreads - 1) / kRowThreads, first = (int)threadIdx.x * each;
     double x = 0.0;
     int t = 0, n_all;
-    for (int i = 0; i < each; ++i) {
-      const int s = (int)threadIdx.x * each + i;
-      if (s < segs) x += sh.mass[s], t += sh.ties[s];
-    }
+    for (int i = first; i < min(first + each, segs); ++i) x += sh.mass[i], t += sh.ties[i];
     double run = before_thread(x, sh.tmp_d, &z);
     int run_t = before_thread(t, sh.tmp_i, &n_all);
     const double at = u * z;
     int mine = segs, last = 0;
-    for (int i = 0; i < each; ++i) {
-      const int s = (int)threadIdx.x * each + i;
-      if (s >= segs) break;
-      if (run + sh.mass[s] > at && sh.mass[s] > 0.0 && mine == segs) {
-        mine = s;
+    for (int i = first; i < min(first + each, segs); ++i) {
+      if (run + sh.mass[i] > at && sh.mass[i] > 0.0 && mine == segs) {
+        mine = i;
         left = run;
         tied = run_t;
       }
-      run += sh.mass[s];
-      run_t += sh.ties[s];
+      run += sh.mass[i];
+      run_t += sh.ties[i];
     }
-    int seg = block_min(mine, sh.tmp_i);
+    const int seg = block_min(mine, sh.tmp_i);
     if (seg == segs) return -1;   // (no weight anywhere: not with a maximum)
     if (mine == seg) sh.before = left, sh.at = tied;
     __syncthreads();
@@ -401,35 +524,256 @@ struct Finish {
     *whole = z;
     return seg * kSeg + found - r.before;
   }
+
+  // ---- rows of which few elements can be kept: a list of them in LDS ----
+
+  // Of the list's elements with f, in their order: the n-th (from 0), or by_mass the last one before which the mass is
+  // below `want`.  *kept: the mass down to and with it.  *fits: whether they are few enough to be ranked (else nothing
+  // is found).
+  template <typename F>
+  __device__ u64 among(F f, bool by_mass, int n, double want, double *kept, bool *fits) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.at = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
+      const u64 key = sh.list[i];
+      if (!f(key_value(key))) continue;
+      const int at = atomicAdd(&sh.at, 1);
+      if (at < kFew) sh.few[at] = key;
+    }
+    __syncthreads();
+    const int c = sh.at;
+    *fits = c <= kFew;
+    if (!*fits) return 0;
+    // (the bins are no longer there: the keys lie in their place)
+    u64 key = 0, found = 0;
+    int rank = 0;
+    if ((int)threadIdx.x < c) {
+      key = sh.few[threadIdx.x];
+      for (int i = 0; i < c; ++i) rank += sh.few[i] > key;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < c) sh.few[rank] = key;
+    __syncthreads();
+    // every thread walks them (few)
+    double mass = 0.0, w = 0.0;
+    uint32_t last = 0;
+    for (int i = 0; i < c; ++i) {
+      if (by_mass ? i > 0 && !(mass < want) : i > n) break;
+      found = sh.few[i];
+      if ((uint32_t)(found >> 32) != last) w = weight(key_value(found), m, ask.a);
+      last = (uint32_t)(found >> 32);
+      mass += w;
+    }
+    *kept = mass;
+    return found;
+  }
+
+  // Of the list (all elements >= lo of the row): the token.  False: it does not fit the bins' second step.
+  __device__ bool from_list(double u, double whole, int *token, double *own, double *kept) {
+    // the list's smallest value bounds the bins
+    float low = m;
+    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) low = fminf(low, key_value(sh.list[i]));
+    low = block_min(low, sh.tmp_i);
+    const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
+    u64 border = 0;   // the last kept element
+    const auto fill = [&] {
+      clear_bins();
+      for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
+        const float x = key_value(sh.list[i]);
+        add(bin_of(x, m, scale), weight(x, m, ask.a));
+      }
+    };
+    int n;
+    u64 w, all;
+    bool fits;
+    double part;
+    if (ask.k && ask.k < sh.n) {
+      fill();
+      const int k = ask.k, b = find_bin([&](int run_n, u64) { return run_n >= k; }, &n, &w, &all);
+      border = among([&](float x) { return bin_of(x, m, scale) == b; }, false, k - 1 - n, 0.0, &part, &fits);
+      if (!fits) return false;
+      whole = (double)w / kOne + part;
+    } else if (ask.k) {
+      fill();
+      find_bin([](int, u64) { return false; }, &n, &w, &all);
+      whole = (double)all / kOne;
+    }
+    if (ask.p <= 1.0) {
+      const double want = ask.p * whole;
+      fill();
+      const int b = find_bin([&](int, u64 run_w) { return (double)run_w / kOne >= want; }, &n, &w, &all);
+      const u64 edge = among([&](float x) { return bin_of(x, m, scale) == b; }, true, 0, want - (double)w / kOne, &part, &fits);
+      if (!fits) return false;
+      border = max(border, edge);
+    }
+    // by ids
+    clear_bins();
+    const int shift = max(0, 32 - __clz(r.V) - 11);
+    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
+      const u64 key = sh.list[i];
+      const double x = weight(key_value(key), m, ask.a);
+      if (key >= border && x >= ask.q && x > 0.0) add((int)(key_index(key) >> shift), x);
+    }
+    double z;
+    {
+      // (the whole first)
+      u64 mine = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < kBins; i += kRowThreads) mine += sh.bins.mass[i];
+      before_thread(mine, sh.tmp_u, &all);
+      z = (double)all / kOne;
+    }
+    const double at = u * z;
+    const int b = find_bin([&](int, u64 run_w) { return (double)run_w / kOne > at; }, &n, &w, &all);
+    // the bin's elements by their ids (keys with the value left out: the least id is the greatest key)
+    __syncthreads();
+    if (threadIdx.x == 0) sh.at = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
+      const u64 key = sh.list[i];
+      if ((int)(key_index(key) >> shift) != b || key < border) continue;
+      const double x = weight(key_value(key), m, ask.a);
+      if (!(x >= ask.q && x > 0.0)) continue;
+      const int to = atomicAdd(&sh.at, 1);
+      if (to < kFew) sh.few[to] = key;
+    }
+    __syncthreads();
+    const int c = sh.at;
+    if (c > kFew) return false;
+    u64 key = 0;
+    int rank = 0;
+    if ((int)threadIdx.x < c) {
+      key = sh.few[threadIdx.x];
+      for (int i = 0; i < c; ++i) rank += key_index(sh.few[i]) < key_index(key);
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < c) sh.few[rank] = key;
+    __syncthreads();
+    double run = (double)w / kOne;
+    for (int i = 0; i < c; ++i) {
+      key = sh.few[i];
+      const double x = weight(key_value(key), m, ask.a);
+      run += x;
+      *own = x;
+      *token = (int)key_index(key);
+      if (run > at) break;
+    }
+    *kept = z;
+    return true;
+  }
+
+  // The elements >= lo into the list, from the groups that have any; false: they are too many.
+  __device__ bool gather(float lo) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0, sh.at = 0;
+    __syncthreads();
+    int *const found = reinterpret_cast<int *>(sh.bins.mass);   // groups
+    for (int g = threadIdx.x; g < segs * kGroups; g += kRowThreads)
+      if (sh.groups[g] >= lo && sh.groups[g] > -INFINITY) {
+        const int to = atomicAdd(&sh.at, 1);
+        if (to < kList) found[to] = g;
+      }
+    __syncthreads();
+    const int c = sh.at;
+    if (c > kList) return false;   // (an element each)
+    // a group's pieces with neighbouring lanes
+    constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece * kGroupLanes;
+    for (int i = threadIdx.x; i < c * kPieces; i += kRowThreads) {
+      const int g = found[i / kPieces], piece = i % kPieces;
+      const int at = piece_at<T>(g / kGroups, g % kGroups * kGroupLanes + piece % kGroupLanes, piece / kGroupLanes);
+      float x[kPiece];
+      load_run<kPiece>(r, at, x);
+#pragma unroll
+      for (int j = 0; j < kPiece; ++j)
+        if (x[j] >= lo && x[j] > -INFINITY) {
+          const int to = atomicAdd(&sh.n, 1);
+          if (to < kList) sh.list[to] = make_key(x[j], (uint32_t)(at + j - r.before));
+        }
+    }
+    __syncthreads();
+    return sh.n <= kList;
+  }
+
+  // A value such that the elements >= it reach `want` (their number, or by_mass their weights): by the groups' maxima
+  // alone, which is less than there is.  -infinity: not reached.
+  __device__ float reach(bool by_mass, double want) {
+    float low = m;
+    const int n_groups = segs * kGroups;
+    for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
+      if (sh.groups[g] > -INFINITY) low = fminf(low, sh.groups[g]);
+    low = block_min(low, sh.tmp_i);
+    const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
+    clear_bins();
+    for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
+      if (sh.groups[g] > -INFINITY) add(bin_of(sh.groups[g], m, scale), by_mass ? weight(sh.groups[g], m, ask.a) : 0.0);
+    int n;
+    u64 w, all;
+    const auto holds = [&](int run_n, u64 run_w) { return by_mass ? (double)run_w / kOne >= want : (double)run_n >= want; };
+    const int b = find_bin(holds, &n, &w, &all);
+    if (!holds(n + (int)sh.bins.count[b], w + sh.bins.mass[b])) return -INFINITY;
+    float least = m;
+    for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
+      if (sh.groups[g] > -INFINITY && bin_of(sh.groups[g], m, scale) <= b) least = fminf(least, sh.groups[g]);
+    return block_min(least, sh.tmp_i);
+  }
+
+  // The row by passes over it.
+  __device__ int by_passes(double u, double whole, float lo, double *own, double *kept) {
+    Border edge{0u, 0, 0.0};
+    if (ask.k) edge = select(false, (double)ask.k, lo);
+    if (ask.k && ask.p <= 1.0) {
+      whole = edge.mass;
+      lo = ordered_to_float(edge.key);
+    }
+    if (ask.p <= 1.0) edge = select(true, ask.p * whole, lo);
+    segment_masses(edge, edge.key ? fmaxf(ordered_to_float(edge.key), lo) : lo);
+    return pick(u, edge, own, kept);
+  }
 };
+
+__device__ inline double number_of(const float *u, int row) { return fmin(fmax((double)u[row], 0.0), 0.99999999999); }
+
+__device__ inline void answer(int row, int token, double own, double whole, int32_t *tokens, float *logprobs) {
+  if (threadIdx.x != 0) return;
+  tokens[row] = token;
+  if (logprobs) logprobs[row] = (float)log(own / whole);
+}
 
 // grid: rows
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void row_kernel(Logits l, Settings s, const float *u, const float *maxima,
-                                                          const double *sums, int32_t *tokens, float *logprobs) {
+                                                          const double *sums, Work work, int32_t *tokens,
+                                                          float *logprobs) {
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x;
   Finish<T> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, 0.0f};
   Row &ask = f.ask;
   const int64_t first = (int64_t)row * l.segs;
   float m = -INFINITY;
-  for (int i = tid; i < l.segs; i += kRowThreads) {
-    const float x = maxima[first + i];
-    sh.maxima[i] = x;
+  for (int i = tid; i < l.segs * kGroups; i += kRowThreads) {
+    const float x = maxima[first * kGroups + i];
+    sh.groups[i] = x;
     m = fmaxf(m, x);
   }
-  // (ordered bits' top: as a signed whole number, smallest first)
-  const int top = block_min(~(int)(ordered_bits(m) ^ 0x80000000u), sh.tmp_i);
-  m = f.m = ordered_to_float((uint32_t)~top ^ 0x80000000u);
+  m = block_max(m, sh.tmp_i);
+  if (m == INFINITY) {
+    f.r.infinite = true;
+    for (int i = tid; i < l.segs * kGroups; i += kRowThreads) sh.groups[i] = sh.groups[i] == INFINITY ? 0.0f : -INFINITY;
+    m = 0.0f;
+  }
+  f.m = m;
+  __syncthreads();
   int token = -1;
   double own = 1.0, whole = 1.0;
+  bool large = false;
   if (m == -INFINITY) {
     own = 0.0;
   } else if (ask.greedy) {
-    int seg = l.segs;
-    for (int i = tid; i < l.segs && seg == l.segs; i += kRowThreads)
-      if (sh.maxima[i] == m) seg = i;
-    seg = block_min(seg, sh.tmp_i);
+    int group = l.segs * kGroups;
+    for (int i = tid; i < l.segs * kGroups; i += kRowThreads)
+      if (sh.groups[i] == m) group = min(group, i);
+    const int seg = block_min(group, sh.tmp_i) / kGroups;
     constexpr int kEach = kSeg / kRowThreads;
     float v[kEach];
     load_run<kEach>(f.r, seg * kSeg + kEach * tid, v);
@@ -439,87 +783,224 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(Logits l, Settings s, 
       if (v[i] == m) mine = kEach * tid + i;
     token = seg * kSeg + block_min(mine, sh.tmp_i) - f.r.before;
   } else {
-    const double at = fmin(fmax((double)u[row], 0.0), 0.99999999999);   // (NaN: 0)
-    Border edge{0u, 0, 0.0};
-    const bool sums_there = !ask.k && !(ask.q > 0.0 && ask.p > 1.0);
-    if (sums_there) {
+    const double at = number_of(u, row);
+    if (ask.sums()) {
       double z = 0.0;
       for (int i = tid; i < l.segs; i += kRowThreads) {
-        const double x = sh.maxima[i] > -INFINITY ? sums[first + i] * weight(sh.maxima[i], m, ask.a) : 0.0;
+        const float top = f.segment_max(i);
+        const double x = top > -INFINITY ? sums[first + i] * weight(top, m, ask.a) : 0.0;
         sh.mass[i] = x;
         sh.ties[i] = 0;
         z += x;
       }
       before_thread(z, sh.tmp_d, &whole);
     }
-    if (ask.k || ask.p <= 1.0 || ask.q > 0.0) {
+    if (ask.filters()) {
       // below these nothing is kept: weights under min_p (and a little less), weights that all together are
-      // less than 1 - top_p of the whole
-      float lo = -INFINITY;
-      if (m < INFINITY) {
-        // (top-p after top-k is of the mass of all k, those under min_p among them)
-        double t = ask.q > 0.0 && !(ask.k && ask.p <= 1.0) ? log2(ask.q) - 1e-6 : -INFINITY;
-        if (ask.p <= 1.0 && sums_there) t = fmax(t, log2((1.0 - ask.p) * whole / l.V) - 1e-6);
-        const double x = (double)m + t / ask.a;
-        lo = (float)(x - 1e-6 * fabs(x));
-        if (!(lo <= m)) lo = -INFINITY;
-      }
+      // less than 1 - top_p of the whole.  (top-p after top-k is of the mass of all k, those under min_p among them)
+      double t = ask.q > 0.0 && !(ask.k && ask.p <= 1.0) ? log2(ask.q) - 1e-6 : -INFINITY;
+      if (ask.p <= 1.0 && !ask.k) t = fmax(t, log2((1.0 - ask.p) * whole / l.V) - 1e-6);
+      const double x = (double)m + t / ask.a;
+      float lo = (float)(x - 1e-6 * fabs(x));
+      if (!(lo <= m)) lo = -INFINITY;
       lo = fmaxf(lo, -3.4028235e38f);
-      if (ask.k) edge = f.select(false, (double)ask.k, lo);
-      if (ask.k && ask.p <= 1.0) {
-        whole = edge.mass;
-        lo = ordered_to_float(edge.key);
+      float near = lo;
+      if (ask.k)
+        near = fmaxf(near, f.reach(false, (double)ask.k));
+      else if (ask.p <= 1.0)
+        near = fmaxf(near, f.reach(true, ask.p * whole * (1.0 + 1e-9)));
+      if (!f.gather(near) || !f.from_list(at, whole, &token, &own, &whole)) {
+        if (work.large && !ask.k) {
+          large = true;
+          Large &x = work.large[row];
+          if (tid == 0) x = Large{ask.p <= 1.0 ? 1 : 2, m, lo, m > lo ? (float)(kBins - 1) / (m - lo) : 0.0f, whole, f.r.infinite, 0};
+          for (int i = tid; i < kBins; i += kRowThreads) work.bins[(int64_t)row * kBins + i] = 0;
+        } else {
+          token = f.by_passes(at, whole, lo, &own, &whole);
+        }
       }
-      if (ask.p <= 1.0) edge = f.select(true, ask.p * whole, lo);
-      for (int i = tid; i < l.segs; i += kRowThreads) sh.mass[i] = 0.0, sh.ties[i] = 0;
-      __syncthreads();
-      // the kept mass of every segment: what lies above the border, and the ties
-      const float border = fmaxf(edge.key ? ordered_to_float(edge.key) : lo, lo);
-      f.each_segment(border, [&](int seg, const float (&x)[kLane]) __attribute__((always_inline)) {
-        double z = 0.0;
-        int ties = 0;
+    } else {
+      token = f.pick(at, Border{0u, 0, 0.0}, &own, &whole);
+    }
+  }
+  if (large) return;
+  if (work.large && tid == 0) work.large[row].on = 0;
+  answer(row, token, own, whole, tokens, logprobs);
+}
+
+// ---- rows of which many elements are kept: the passes over all workgroups ----
+
+// Masses in bins of values, from m down to lo.  grid: rows x parts
+template <typename T>
+__global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, int parts, const float *maxima, Work work) {
+  const int row = blockIdx.x / parts;
+  const Large x = work.large[row];
+  if (x.on != 1) return;
+  __shared__ u64 bins[kBins];
+  for (int i = threadIdx.x; i < kBins; i += 64 * kPart) bins[i] = 0;
+  __syncthreads();
+  const int seg = (int)(blockIdx.x % parts) * kPart + (threadIdx.x >> 6);
+  if (seg < l.segs) {
+    RowAt<T> r = row_at<T>(l, row);
+    r.infinite = x.infinite;
+    const Row ask = row_of(s, row, l.V);
+    float v[kLane];
+    load_segment(r, seg, v);
 #pragma unroll
-        for (int i = 0; i < kLane; ++i) {
-          const uint32_t key = ordered_bits(x[i]);
-          if (x[i] < border || x[i] == -INFINITY) continue;
-          if (key == edge.key) {
-            ++ties;
-          } else if (key > edge.key) {
-            const double w = weight(x[i], m, ask.a);
-            if (w >= ask.q) z += w;
-          }
+    for (int i = 0; i < kLane; ++i)
+      if (v[i] >= x.lo) atomicAdd(&bins[bin_of(v[i], x.m, x.scale)], whole_number(weight(v[i], x.m, ask.a)));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += 64 * kPart)
+    if (bins[i]) atomicAdd(&work.bins[(int64_t)row * kBins + i], bins[i]);
+}
+
+// The border's bin (each workgroup finds it again); the mass of each segment's elements before it, and the elements in it into a
+// list.  grid: rows x parts
+template <typename T>
+__global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s, int parts, double *masses, Work work) {
+  const int row = blockIdx.x / parts, tid = threadIdx.x;
+  const Large x = work.large[row];
+  if (!x.on) return;
+  __shared__ u64 tmp[kRowWaves];
+  __shared__ int tmp_i[kRowWaves];
+  const Row ask = row_of(s, row, l.V);
+  int border = kBins;
+  if (x.on == 1) {
+    constexpr int kEach = kBins / (64 * kPart);
+    static_assert(kPart == kRowWaves, "sums over a workgroup");
+    u64 w[kEach], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += w[i] = work.bins[(int64_t)row * kBins + kEach * tid + i];
+    u64 run = before_thread(sum, tmp, &all);
+    const double want = ask.p * x.whole;
+    int mine = kBins;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const u64 before = run;
+      run += w[i];
+      if (w[i] && (double)run / kOne >= want && mine == kBins) mine = kEach * tid + i, sum = before;
+    }
+    border = block_min(mine, tmp_i);
+    // (never reached: all is kept)
+    if (border < kBins && border == mine && blockIdx.x % parts == 0) work.above[row] = sum;
+  }
+  const int seg = (int)(blockIdx.x % parts) * kPart + (tid >> 6);
+  if (seg >= l.segs) return;
+  RowAt<T> r = row_at<T>(l, row);
+  r.infinite = x.infinite;
+  float v[kLane];
+  load_segment(r, seg, v);
+  constexpr int kPiece = 16 / sizeof(T);
+  double z = 0.0;
+#pragma unroll
+  for (int i = 0; i < kLane; ++i) {
+    if (!(v[i] >= x.lo)) continue;
+    const int b = bin_of(v[i], x.m, x.scale);
+    if (b < border) {
+      const double w = weight(v[i], x.m, ask.a);
+      if (w >= ask.q) z += w;
+    } else if (b == border) {
+      const int to = atomicAdd(&work.large[row].listed, 1);
+      if (to < kList)
+        work.list[(int64_t)row * kList + to] =
+            make_key(v[i], (uint32_t)(piece_at<T>(seg, tid & 63, i / kPiece) + i % kPiece - r.before));
+    }
+  }
+  z = wave_sum(z);
+  if ((tid & 63) == 0) masses[(int64_t)row * l.segs + seg] = z;
+}
+
+// The border among its bin's elements, and the token.  grid: rows
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s, const float *u, const float *maxima,
+                                                            const double *masses, Work work, int32_t *tokens,
+                                                            float *logprobs) {
+  const int row = blockIdx.x, tid = threadIdx.x;
+  const Large x = work.large[row];
+  if (!x.on) return;
+  __shared__ Shared sh;
+  Finish<T> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, x.m};
+  f.r.infinite = x.infinite;
+  const int64_t first = (int64_t)row * l.segs;
+  const double at = number_of(u, row);
+  double own = 1.0, whole = x.whole;
+  int token;
+  bool fits = x.listed <= kList;
+  Border edge{0u, 0, 0.0};
+  if (fits) {
+    if (tid == 0) sh.n = x.listed;
+    for (int i = tid; i < x.listed; i += kRowThreads) sh.list[i] = work.list[(int64_t)row * kList + i];
+    for (int i = tid; i < l.segs; i += kRowThreads) sh.mass[i] = masses[first + i], sh.ties[i] = 0;
+    __syncthreads();
+    if (x.listed) {
+      double part;
+      const double want = f.ask.p * x.whole - (double)work.above[row] / kOne;
+      const u64 border = f.among([](float) { return true; }, true, 0, want, &part, &fits);
+      if (fits) {
+        // the kept ones of the bin join their segments (whole numbers: in any order); of the border's equals only those
+        // up to it are kept
+        u64 *const more = sh.bins.mass;
+        __syncthreads();
+        for (int i = tid; i < l.segs; i += kRowThreads) more[i] = 0;
+        if (tid == 0) sh.at = 0;
+        __syncthreads();
+        edge.key = ordered_bits(key_value(border));
+        for (int i = tid; i < x.listed; i += kRowThreads) {
+          const u64 key = sh.list[i];
+          const uint32_t bits = (uint32_t)(key >> 32);
+          const int seg = ((int)key_index(key) + f.r.before) / kSeg;
+          if (bits == edge.key) atomicAdd(&sh.ties[seg], 1);
+          if (key < border) continue;
+          if (bits == edge.key) atomicAdd(&sh.at, 1);
+          const double w = weight(key_value(key), x.m, f.ask.a);
+          if (w >= f.ask.q) atomicAdd(&more[seg], whole_number(w));
         }
-        z = wave_sum(z);
-        for (int o = 1; o < 64; o <<= 1) ties += __shfl_xor(ties, o);
-        if ((tid & 63) == 0) sh.mass[seg] = z, sh.ties[seg] = ties;
-      });
-      __syncthreads();
-      if (edge.key) {
-        double w = weight(ordered_to_float(edge.key), m, ask.a);
-        if (w < ask.q) w = 0.0;
-        int t = 0, all;
-        const int each = (l.segs + kRowThreads - 1) / kRowThreads;
-        for (int i = 0; i < each; ++i)
-          if (tid * each + i < l.segs) t += sh.ties[tid * each + i];
-        int run = before_thread(t, sh.tmp_i, &all);
-        for (int i = 0; i < each; ++i) {
-          const int seg = tid * each + i;
-          if (seg >= l.segs) break;
-          sh.mass[seg] += min(max(edge.ties - run, 0), sh.ties[seg]) * w;
-          run += sh.ties[seg];
-        }
+        __syncthreads();
+        edge.ties = sh.at;
+        for (int i = tid; i < l.segs; i += kRowThreads) sh.mass[i] += (double)more[i] / kOne;
+        __syncthreads();
       }
     }
-    __syncthreads();
+  }
+  if (fits) {
+    if (!edge.key) edge = Border{ordered_bits(x.lo), 1 << 30, 0.0};   // (all from lo on)
     token = f.pick(at, edge, &own, &whole);
+  } else {
+    __syncthreads();
+    for (int i = tid; i < l.segs * kGroups; i += kRowThreads) {
+      const float g = maxima[first * kGroups + i];
+      sh.groups[i] = x.infinite ? g == INFINITY ? 0.0f : -INFINITY : g;
+    }
+    __syncthreads();
+    token = f.by_passes(at, x.whole, x.lo, &own, &whole);
   }
-  if (tid == 0) {
-    tokens[row] = token;
-    if (logprobs) logprobs[row] = (float)log(own / whole);
-  }
+  answer(row, token, own, whole, tokens, logprobs);
 }
 
 int segments(int V) { return (V + 15 + kSeg - 1) / kSeg; }
+
+struct Layout {
+  size_t sums, maxima, large, above, bins, list, bytes;
+};
+Layout layout(int rows, int V) {
+  Layout w;
+  size_t n = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = n;
+    n += align_up(bytes, 256);
+    return at;
+  };
+  const size_t segs = (size_t)rows * segments(V);
+  w.sums = take(segs * sizeof(double));
+  w.maxima = take(segs * kGroups * sizeof(float));
+  w.large = take(rows * sizeof(Large));
+  w.above = take(rows * sizeof(u64));
+  w.bins = take((size_t)rows * kBins * sizeof(u64));
+  w.list = take((size_t)rows * kList * sizeof(u64));
+  w.bytes = n;
+  return w;
+}
 
 }  // namespace
 }  // namespace dt
@@ -534,8 +1015,7 @@ dt_status dt_sample_workspace_size(int rows, int V, size_t *bytes) {
   if (V > kMaxV) return fail(DT_ERR_UNSUPPORTED, "V must be <= %d (%d)", kMaxV, V);
   const int64_t groups = (segments(V) + kWaves - 1) / kWaves;
   if (rows * groups >= kMaxGroups) return fail(DT_ERR_UNSUPPORTED, "rows and V are too large together");
-  const size_t n = (size_t)rows * segments(V);
-  *bytes = align_up(n * sizeof(double), 256) + align_up(n * sizeof(float), 256);
+  *bytes = layout(rows, V).bytes;
   return DT_OK;
 }
 
@@ -565,15 +1045,27 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   const Logits l{static_cast<const char *>(logits), row_stride * (int64_t)es, rows, V, segments(V)};
   const Settings s{how->temperature, how->top_p, how->min_p, how->top_k, how->temperatures, how->top_ps, how->min_ps,
                    how->top_ks};
-  double *sums = static_cast<double *>(workspace);
-  float *maxima = reinterpret_cast<float *>(static_cast<char *>(workspace) +
-                                            align_up((size_t)rows * l.segs * sizeof(double), 256));
-  const int groups = (l.segs + kWaves - 1) / kWaves;
+  const Layout w = layout(rows, V);
+  char *const at = static_cast<char *>(workspace);
+  double *sums = reinterpret_cast<double *>(at + w.sums);
+  float *maxima = reinterpret_cast<float *>(at + w.maxima);
+  // (thousands of tokens are kept by top-p or min-p, if by anything; top-k's passes, where its elements are too many, are
+  // its row's workgroup's)
+  const bool can_be_large = (how->top_ks || how->top_k == 0) &&
+                            (how->top_ps || how->top_p < 1.0f || how->min_ps || how->min_p > 0.0f);
+  const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<u64 *>(at + w.bins),
+                  reinterpret_cast<u64 *>(at + w.list), reinterpret_cast<u64 *>(at + w.above)};
+  const int groups = (l.segs + kWaves - 1) / kWaves, parts = (l.segs + kPart - 1) / kPart;
   hipStream_t q = static_cast<hipStream_t>(stream);
   auto launch = [&](auto t) {
     using T = decltype(t);
     segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums);
-    row_kernel<T><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, tokens, logprobs);
+    row_kernel<T><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
+    if (can_be_large) {
+      bins_kernel<T><<<(unsigned)(rows * parts), 64 * kPart, 0, q>>>(l, s, parts, maxima, work);
+      masses_kernel<T><<<(unsigned)(rows * parts), 64 * kPart, 0, q>>>(l, s, parts, sums, work);
+      large_kernel<T><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
+    }
   };
   if (logits_dtype == DT_F32)
     launch(uint32_t());

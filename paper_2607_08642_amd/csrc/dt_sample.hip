@@ -23,12 +23,13 @@ constexpr int kLane = kSeg / 64;    // of them with one lane
 constexpr int kMaxV = 1 << 19;
 constexpr int kMaxSegs = kMaxV / kSeg + 1;   // (a row may begin inside a 16-byte piece)
 constexpr int kWaves = 4;           // of a workgroup of segments_kernel
-constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
+constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
 constexpr int kGroupLanes = 4, kGroups = 64 / kGroupLanes;  // a segment's maxima are kept for groups of 128 elements
+constexpr int kFewSegs = 8;  // rows of no more are not large: their workgroup's own passes are short
 constexpr int kBins = 2048;
 constexpr int kList = 1024;  // elements that a row's end is found among in LDS
 constexpr int kFew = kRowThreads;  // elements ranked by a thread each
-constexpr int kPart = 8;     // segments (waves) of a workgroup of the passes for large rows
+constexpr int kPart = 4;     // segments (waves) of a workgroup of the passes for large rows
 constexpr int kMaxGroups = 1 << 24;
 constexpr double kOne = 17592186044416.0;  // 2^44: masses in the bins are whole numbers of 2^-44 (2^19 of them fit 63 bits)
 
@@ -69,55 +70,54 @@ __device__ inline Row row_of(const Settings &s, int row, int V) {
 }
 
 // 2^t, t <= 0 (NaN and less than -2000 as -2000: 0).  2^f = 1 + f g(f) for |f| <= 1/2, g interpolated at the nine
-// Chebyshev points: 4e-14 of the result at most, and 2^0 is 1.
-__device__ __forceinline__ double pow2(double t) {
-  t = fmax(t, -2000.0);
-  const double n = rint(t), f = t - n;
-  double g = 1.0203121063391729e-07;
-  g = fma(g, f, 1.3255224878668817e-06);
-  g = fma(g, f, 1.525268684626772e-05);
-  g = fma(g, f, 0.00015403455852453838);
-  g = fma(g, f, 0.0013333558179043112);
-  g = fma(g, f, 0.009618129159402558);
-  g = fma(g, f, 0.055504108664760424);
-  g = fma(g, f, 0.2402265069581299);
-  g = fma(g, f, 0.6931471805599453);
-  return ldexp(fma(g, f, 1.0), (int)n);
-}
+// Chebyshev points: 4e-14 of the result at most, and 2^0 is 1.  The coefficients are kept in scalar registers (as
+// literals each step would move one to the vector registers first: half of all instructions).
+struct Pow2 {
+  double c[9] = {1.0203121063391729e-07, 1.3255224878668817e-06, 1.525268684626772e-05, 0.00015403455852453838,
+                 0.0013333558179043112,  0.009618129159402558,   0.055504108664760424,  0.2402265069581299,
+                 0.6931471805599453};
+  __device__ __forceinline__ Pow2() {
+#pragma unroll
+    for (int i = 0; i < 9; ++i) asm("" : "+s"(c[i]));
+  }
+  __device__ __forceinline__ double operator()(double t) const {
+    t = fmax(t, -2000.0);
+    const double n = rint(t), f = t - n;
+    double g = c[0];
+#pragma unroll
+    for (int i = 1; i < 9; ++i) g = fma(g, f, c[i]);
+    return ldexp(fma(g, f, 1.0), (int)n);
+  }
+};
 
-// the weight of x against a maximum m (of infinities alone: 1 each; the segments that have one count, if any has)
-__device__ __forceinline__ double weight(float x, float m, double a) {
-  if (m == INFINITY) return x == m ? 1.0 : 0.0;
+// the weight of x against a finite maximum m
+__device__ __forceinline__ double weight(float x, float m, double a, const Pow2 &pow2 = Pow2()) {
   return pow2(((double)x - (double)m) * a);
 }
 
-template <typename T>
-__device__ __forceinline__ float value(T x) {
-  float v;
-  if constexpr (sizeof(T) == 4)
-    v = __uint_as_float(x);
-  else
-    v = bf16_to_f32(x);
-  return v == v ? v : -INFINITY;  // (NaN: never chosen)
-}
+__device__ __forceinline__ float widen(uint32_t x) { return __uint_as_float(x); }
+__device__ __forceinline__ float widen(uint16_t x) { return bf16_to_f32(x); }
 
 // A row as segments of aligned 16-byte pieces: element i of segment s has the id s * kSeg + i - before.  Where the
 // maximum is +infinity, its equals are read as 0 and the rest as -infinity.
-template <typename T>
+// raw: as they are, NaN too (a maximum and pow2 take no notice of it).
+template <typename T, bool raw = false>
 struct RowAt {
   const T *base;
   int before, V;
   bool infinite;
 
   __device__ __forceinline__ float at(T x) const {
-    const float v = value(x);
-    return infinite ? v == INFINITY ? 0.0f : -INFINITY : v;
+    const float v = widen(x);
+    if (raw) return v;
+    if (infinite) return v == INFINITY ? 0.0f : -INFINITY;
+    return v == v ? v : -INFINITY;   // (NaN: never chosen)
   }
 };
-template <typename T>
-__device__ inline RowAt<T> row_at(const Logits &l, int row) {
+template <typename T, bool raw = false>
+__device__ inline RowAt<T, raw> row_at(const Logits &l, int row) {
   const char *p = l.p + row * l.stride;
-  RowAt<T> r;
+  RowAt<T, raw> r;
   r.before = (int)(reinterpret_cast<uintptr_t>(p) % 16) / (int)sizeof(T);
   r.base = reinterpret_cast<const T *>(p) - r.before;
   r.V = l.V;
@@ -125,26 +125,40 @@ __device__ inline RowAt<T> row_at(const Logits &l, int row) {
   return r;
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <int N, typename T, bool raw>
+__device__ __forceinline__ void unpack(const RowAt<T, raw> &r, u32x4 w, float *x) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(T) == 4)
+      x[i] = r.at(w[i]);
+    else
+      x[i] = r.at((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+  }
+}
+
 // N elements from place `at` (a multiple of a piece, or within one) of the row on; those that are not the row's: -infinity
-template <int N, typename T>
-__device__ __forceinline__ void load_run(const RowAt<T> &r, int at, float *x) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int N, typename T, bool raw>
+__device__ __forceinline__ void load_run(const RowAt<T, raw> &r, int at, float *x) {
   constexpr int kPiece = 16 / sizeof(T);
   static_assert(N <= kPiece, "one piece at most");
   const int lo = r.before, hi = r.before + r.V;
   if (N == kPiece && at >= lo && at + N <= hi) {
-    const u32x4 w = *reinterpret_cast<const u32x4 *>(r.base + at);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if constexpr (sizeof(T) == 4)
-        x[i] = r.at(w[i]);
-      else
-        x[i] = r.at((uint16_t)(w[i / 2] >> (16 * (i & 1))));
-    }
+    unpack<N>(r, *reinterpret_cast<const u32x4 *>(r.base + at), x);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = at + i >= lo && at + i < hi ? r.at(r.base[at + i]) : -INFINITY;
   }
+}
+
+// a thread's share of a segment, in the order of ids
+constexpr int kOwn = kSeg / kRowThreads;
+template <typename T>
+__device__ __forceinline__ void load_own(const RowAt<T> &r, int seg, float (&x)[kOwn]) {
+  constexpr int kPiece = 16 / sizeof(T);
+#pragma unroll
+  for (int j = 0; j < kOwn; j += kPiece) load_run<kPiece>(r, seg * kSeg + kOwn * (int)threadIdx.x + j, x + j);
 }
 
 // The place of piece j of a lane in a segment's order: lane l holds pieces l + 64 j.
@@ -152,12 +166,26 @@ template <typename T>
 __device__ __forceinline__ int piece_at(int seg, int lane, int j) {
   return seg * kSeg + (j * 64 + lane) * (16 / (int)sizeof(T));
 }
-template <typename T>
-__device__ __forceinline__ void load_segment(const RowAt<T> &r, int seg, float (&x)[kLane]) {
+template <typename T, bool raw>
+__device__ __forceinline__ void load_segment(const RowAt<T, raw> &r, int seg, float (&x)[kLane]) {
   constexpr int kPiece = 16 / sizeof(T);
+  if (seg * kSeg >= r.before && (seg + 1) * kSeg <= r.before + r.V) {   // (the same for the whole wave)
+    u32x4 w[kLane / kPiece];
 #pragma unroll
-  for (int j = 0; j < kLane / kPiece; ++j)
-    load_run<kPiece>(r, piece_at<T>(seg, threadIdx.x & 63, j), x + j * kPiece);
+    for (int j = 0; j < kLane / kPiece; ++j)
+      w[j] = *reinterpret_cast<const u32x4 *>(r.base + piece_at<T>(seg, threadIdx.x & 63, j));
+#pragma unroll
+    for (int j = 0; j < kLane / kPiece; ++j) unpack<kPiece>(r, w[j], x + j * kPiece);
+    return;
+  }
+#pragma unroll 1
+  for (int j = 0; j < kLane / kPiece; ++j) {
+    float y[kPiece];
+    load_run<kPiece>(r, piece_at<T>(seg, threadIdx.x & 63, j), y);
+#pragma unroll
+    for (int i = 0; i < kLane; ++i)
+      if (i / kPiece == j) x[i] = y[i % kPiece];
+  }
 }
 
 __device__ inline double wave_sum(double x) {
@@ -172,12 +200,12 @@ __global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Setting
   const int row = blockIdx.x / groups, lane = threadIdx.x & 63;
   const int seg = (int)(blockIdx.x % groups) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (seg >= l.segs) return;
-  const RowAt<T> r = row_at<T>(l, row);
+  const RowAt<T, true> r = row_at<T, true>(l, row);
   float x[kLane];
   load_segment(r, seg, x);
-  float m = x[0];
+  float m = -INFINITY;
 #pragma unroll
-  for (int i = 1; i < kLane; ++i) m = fmaxf(m, x[i]);
+  for (int i = 0; i < kLane; ++i) m = fmaxf(m, x[i]);
   for (int o = 1; o < kGroupLanes; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   const Row ask = row_of(s, row, l.V);
   const int64_t at = (int64_t)row * l.segs + seg;
@@ -185,9 +213,16 @@ __global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Setting
   if (!ask.sums()) return;
   for (int o = kGroupLanes; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   double z = 0.0;
+  m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m)));
   if (m > -INFINITY) {
+    const Pow2 pow2;
+    if (m == INFINITY) {
 #pragma unroll
-    for (int i = 0; i < kLane; ++i) z += weight(x[i], m, ask.a);
+      for (int i = 0; i < kLane; ++i) z += x[i] == m;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLane; ++i) z += pow2(((double)x[i] - (double)m) * ask.a);
+    }
     z = wave_sum(z);
   }
   if (lane == 0) sums[at] = z;
@@ -303,15 +338,21 @@ struct Finish {
     return x;
   }
 
-  // f(segment, elements) by the waves for every segment with an element >= lo
-  template <typename F>
-  __device__ void each_segment(float lo, F f) {
+  // By the waves, for every segment with an element >= lo: piece(its elements) by every lane, piece after piece (few
+  // registers: these are the slow rows' loops, and share a kernel with the others), then done(segment).
+  template <typename F, typename G>
+  __device__ __forceinline__ void each_segment(float lo, F piece, G done) {
+    constexpr int kPiece = 16 / sizeof(T);
     for (int seg = threadIdx.x >> 6; seg < segs; seg += kRowWaves) {
       const float top = segment_max(seg);
       if (top < lo || top == -INFINITY) continue;
-      float x[kLane];
-      load_segment(r, seg, x);
-      f(seg, x);
+#pragma unroll 1
+      for (int j = 0; j < kLane / kPiece; ++j) {
+        float x[kPiece];
+        load_run<kPiece>(r, piece_at<T>(seg, threadIdx.x & 63, j), x);
+        piece(x);
+      }
+      done(seg);
     }
   }
 
@@ -381,14 +422,14 @@ struct Finish {
     for (;;) {
       const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
       clear_bins();
-      each_segment(ordered_to_float(lo), [&](int, const float (&x)[kLane]) __attribute__((always_inline)) {
+      each_segment(ordered_to_float(lo), [&](const float(&x)[16 / sizeof(T)]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < kLane; ++i) {
-          const uint32_t key = ordered_bits(x[i]);
-          if (key < lo || key > hi || x[i] == -INFINITY) continue;
-          add((int)((hi - key) >> shift), weight(x[i], m, ask.a));
+        for (const float v : x) {
+          const uint32_t key = ordered_bits(v);
+          if (key < lo || key > hi || v == -INFINITY) continue;
+          add((int)((hi - key) >> shift), weight(v, m, ask.a));
         }
-      });
+      }, [](int) {});
       int n;
       u64 w, all;
       const int b = find_bin([&](int run_n, u64 run_w) {
@@ -418,23 +459,26 @@ struct Finish {
     __syncthreads();
     for (int i = threadIdx.x; i < segs; i += kRowThreads) sh.mass[i] = 0.0, sh.ties[i] = 0;
     __syncthreads();
-    each_segment(lo, [&](int seg, const float (&x)[kLane]) __attribute__((always_inline)) {
-      double z = 0.0;
-      int ties = 0;
+    double z = 0.0;
+    int ties = 0;
+    each_segment(lo, [&](const float(&x)[16 / sizeof(T)]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < kLane; ++i) {
-        const uint32_t key = ordered_bits(x[i]);
-        if (x[i] < lo || x[i] == -INFINITY) continue;
+      for (const float v : x) {
+        const uint32_t key = ordered_bits(v);
+        if (v < lo || v == -INFINITY) continue;
         if (key == edge.key) {
           ++ties;
         } else if (key > edge.key) {
-          const double w = weight(x[i], m, ask.a);
+          const double w = weight(v, m, ask.a);
           if (w >= ask.q) z += w;
         }
       }
+    }, [&](int seg) {
       z = wave_sum(z);
       for (int o = 1; o < 64; o <<= 1) ties += __shfl_xor(ties, o);
       if ((threadIdx.x & 63) == 0) sh.mass[seg] = z, sh.ties[seg] = ties;
+      z = 0.0;
+      ties = 0;
     });
     __syncthreads();
     if (!edge.key) return;
@@ -479,10 +523,9 @@ struct Finish {
     __syncthreads();
     left = sh.before;
     tied = sh.at;
-    // four neighbours a thread
-    constexpr int kEach = kSeg / kRowThreads;
+    constexpr int kEach = kOwn;
     float v[kEach];
-    load_run<kEach>(r, seg * kSeg + kEach * (int)threadIdx.x, v);
+    load_own(r, seg, v);
     int equal = 0, all_equal;
     uint32_t key[kEach];
 #pragma unroll
@@ -555,22 +598,70 @@ struct Finish {
     __syncthreads();
     if ((int)threadIdx.x < c) sh.few[rank] = key;
     __syncthreads();
-    // every thread walks them (few)
-    double mass = 0.0, w = 0.0;
-    uint32_t last = 0;
-    for (int i = 0; i < c; ++i) {
-      if (by_mass ? i > 0 && !(mass < want) : i > n) break;
-      found = sh.few[i];
-      if ((uint32_t)(found >> 32) != last) w = weight(key_value(found), m, ask.a);
-      last = (uint32_t)(found >> 32);
-      mass += w;
-    }
+    const int tid = threadIdx.x;
+    key = tid < c ? sh.few[tid] : 0;
+    const double w = tid < c ? weight(key_value(key), m, ask.a) : 0.0;
+    double all;
+    const double before = before_thread(w, sh.tmp_d, &all);
+    const bool in = tid < c && (by_mass ? tid == 0 || before < want : tid <= n);
+    // (weights fall and sums do not: what is kept is the first few)
+    const int count = block_min(in ? kRowThreads : tid, sh.tmp_i);
+    const int last = min(count, c) - 1;
+    if (tid == last) sh.u = key, sh.before = before + w;
+    __syncthreads();
+    found = sh.u;
+    const double mass = sh.before;
     *kept = mass;
     return found;
   }
 
+  // The same of a list of at most an element a thread, put in order.
+  __device__ void from_short_list(double u, double whole, int *token, double *own, double *kept) {
+    const int tid = threadIdx.x, n = sh.n;
+    u64 key = tid < n ? sh.list[tid] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += sh.list[i] > key;
+    u64 *const order = sh.bins.mass;
+    double *const weights = reinterpret_cast<double *>(sh.bins.mass + kRowThreads);
+    if (tid < n) order[rank] = key;
+    __syncthreads();
+    key = tid < n ? order[tid] : 0;
+    const double w = tid < n ? weight(key_value(key), m, ask.a) : 0.0;
+    const bool first_k = tid < n && (!ask.k || tid < ask.k);
+    bool in = first_k && w >= ask.q;
+    if (ask.p <= 1.0) {
+      double z;
+      const double before = before_thread(first_k ? w : 0.0, sh.tmp_d, &z);
+      in = in && (tid == 0 || before < ask.p * (ask.k ? z : whole));
+    }
+    // what is kept is the first few of the order; their running sums in the order of ids
+    weights[tid] = w;
+    const int c = block_min(in ? n : tid, sh.tmp_i);
+    const uint32_t id = key_index(key);
+    double run = 0.0, z = 0.0;
+    for (int i = 0; i < c; ++i) {
+      const double x = weights[i];
+      z += x;
+      if (key_index(order[i]) <= id) run += x;
+    }
+    const double at = u * z;
+    const bool passes = tid < c && run > at && w > 0.0;
+    int least = block_min(passes ? (int)id : 0x7fffffff, sh.tmp_i);
+    // (the sums' last bits: the last id)
+    if (least == 0x7fffffff) least = -block_min(tid < c && w > 0.0 ? -(int)id : 0, sh.tmp_i);
+    if (tid < c && (int)id == least) sh.before = w;
+    __syncthreads();
+    *own = sh.before;
+    *token = least;
+    *kept = z;
+  }
+
   // Of the list (all elements >= lo of the row): the token.  False: it does not fit the bins' second step.
   __device__ bool from_list(double u, double whole, int *token, double *own, double *kept) {
+    if (sh.n <= kRowThreads) {
+      from_short_list(u, whole, token, own, kept);
+      return true;
+    }
     // the list's smallest value bounds the bins
     float low = m;
     for (int i = threadIdx.x; i < sh.n; i += kRowThreads) low = fminf(low, key_value(sh.list[i]));
@@ -650,15 +741,15 @@ struct Finish {
     __syncthreads();
     if ((int)threadIdx.x < c) sh.few[rank] = key;
     __syncthreads();
-    double run = (double)w / kOne;
-    for (int i = 0; i < c; ++i) {
-      key = sh.few[i];
-      const double x = weight(key_value(key), m, ask.a);
-      run += x;
-      *own = x;
-      *token = (int)key_index(key);
-      if (run > at) break;
-    }
+    const int tid = threadIdx.x;
+    key = tid < c ? sh.few[tid] : 0;
+    const double x = tid < c ? weight(key_value(key), m, ask.a) : 0.0;
+    const double run = x + (double)w / kOne + before_thread(x, sh.tmp_d, &part);
+    const int which = min(block_min(tid < c && run > at ? tid : kRowThreads, sh.tmp_i), c - 1);
+    if (tid == which) sh.u = key, sh.before = x;
+    __syncthreads();
+    *own = sh.before;
+    *token = (int)key_index(sh.u);
     *kept = z;
     return true;
   }
@@ -695,9 +786,38 @@ struct Finish {
     return sh.n <= kList;
   }
 
+  // The same by an order of the threads' maxima (of every kRowThreads-th group each), where they suffice.
+  __device__ float reach_of_few(bool by_mass, double want) {
+    const int tid = threadIdx.x;
+    float top = -INFINITY;
+    for (int g = tid; g < segs * kGroups; g += kRowThreads) top = fmaxf(top, sh.groups[g]);
+    float *const tops = reinterpret_cast<float *>(sh.bins.count), *const order = tops + kRowThreads;
+    tops[tid] = top;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < kRowThreads; i += 4) {
+      const float4 v = *reinterpret_cast<const float4 *>(tops + i);
+      rank += (v.x > top || (v.x == top && i < tid)) + (v.y > top || (v.y == top && i + 1 < tid)) +
+              (v.z > top || (v.z == top && i + 2 < tid)) + (v.w > top || (v.w == top && i + 3 < tid));
+    }
+    order[rank] = top;
+    __syncthreads();
+    if (!by_mass) return order[(int)want - 1];
+    const float x = order[tid];
+    double all;
+    const double w = x > -INFINITY ? weight(x, m, ask.a) : 0.0, run = w + before_thread(w, sh.tmp_d, &all);
+    const int at = block_min(run >= want ? tid : kRowThreads, sh.tmp_i);
+    return at < kRowThreads ? order[at] : -INFINITY;
+  }
+
   // A value such that the elements >= it reach `want` (their number, or by_mass their weights): by the groups' maxima
   // alone, which is less than there is.  -infinity: not reached.
   __device__ float reach(bool by_mass, double want) {
+    if (by_mass || want <= kRowThreads) {
+      const float x = reach_of_few(by_mass, want);
+      if (x > -INFINITY) return x;
+    }
     float low = m;
     const int n_groups = segs * kGroups;
     for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
@@ -742,7 +862,7 @@ __device__ inline void answer(int row, int token, double own, double whole, int3
 
 // grid: rows
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void row_kernel(Logits l, Settings s, const float *u, const float *maxima,
+__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))) void row_kernel(Logits l, Settings s, const float *u, const float *maxima,
                                                           const double *sums, Work work, int32_t *tokens,
                                                           float *logprobs) {
   __shared__ Shared sh;
@@ -774,9 +894,9 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(Logits l, Settings s, 
     for (int i = tid; i < l.segs * kGroups; i += kRowThreads)
       if (sh.groups[i] == m) group = min(group, i);
     const int seg = block_min(group, sh.tmp_i) / kGroups;
-    constexpr int kEach = kSeg / kRowThreads;
+    constexpr int kEach = kOwn;
     float v[kEach];
-    load_run<kEach>(f.r, seg * kSeg + kEach * tid, v);
+    load_own(f.r, seg, v);
     int mine = kSeg;
 #pragma unroll
     for (int i = kEach - 1; i >= 0; --i)
@@ -846,9 +966,10 @@ __global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, 
     const Row ask = row_of(s, row, l.V);
     float v[kLane];
     load_segment(r, seg, v);
+    const Pow2 pow2;
 #pragma unroll
     for (int i = 0; i < kLane; ++i)
-      if (v[i] >= x.lo) atomicAdd(&bins[bin_of(v[i], x.m, x.scale)], whole_number(weight(v[i], x.m, ask.a)));
+      if (v[i] >= x.lo) atomicAdd(&bins[bin_of(v[i], x.m, x.scale)], whole_number(weight(v[i], x.m, ask.a, pow2)));
   }
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += 64 * kPart)
@@ -892,13 +1013,14 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
   float v[kLane];
   load_segment(r, seg, v);
   constexpr int kPiece = 16 / sizeof(T);
+  const Pow2 pow2;
   double z = 0.0;
 #pragma unroll
   for (int i = 0; i < kLane; ++i) {
     if (!(v[i] >= x.lo)) continue;
     const int b = bin_of(v[i], x.m, x.scale);
     if (b < border) {
-      const double w = weight(v[i], x.m, ask.a);
+      const double w = weight(v[i], x.m, ask.a, pow2);
       if (w >= ask.q) z += w;
     } else if (b == border) {
       const int to = atomicAdd(&work.large[row].listed, 1);
@@ -943,6 +1065,7 @@ __global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s
         u64 *const more = sh.bins.mass;
         __syncthreads();
         for (int i = tid; i < l.segs; i += kRowThreads) more[i] = 0;
+        __syncthreads();
         if (tid == 0) sh.at = 0;
         __syncthreads();
         edge.key = ordered_bits(key_value(border));
@@ -1051,7 +1174,7 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   float *maxima = reinterpret_cast<float *>(at + w.maxima);
   // (thousands of tokens are kept by top-p or min-p, if by anything; top-k's passes, where its elements are too many, are
   // its row's workgroup's)
-  const bool can_be_large = (how->top_ks || how->top_k == 0) &&
+  const bool can_be_large = l.segs > kFewSegs && (how->top_ks || how->top_k == 0) &&
                             (how->top_ps || how->top_p < 1.0f || how->min_ps || how->min_p > 0.0f);
   const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<u64 *>(at + w.bins),
                   reinterpret_cast<u64 *>(at + w.list), reinterpret_cast<u64 *>(at + w.above)};

@@ -27,10 +27,11 @@ constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
 constexpr int kGroupLanes = 4, kGroups = 64 / kGroupLanes;  // a segment's maxima are kept for groups of 128 elements
 constexpr int kFewSegs = 8;  // rows of no more are not large: their workgroup's own passes are short
 constexpr int kBins = 2048;
+constexpr int kPad = 64;
 constexpr int kList = 1024;  // elements that a row's end is found among in LDS
-constexpr int kFew = kRowThreads;  // elements ranked by a thread each
 constexpr int kPart = 4;     // segments (waves) of a workgroup of the passes for large rows
 constexpr int kMaxGroups = 1 << 24;
+constexpr int kSpread = 1024;   // workgroups of the passes for large rows (four a CU): launches that find no such row end soon
 constexpr double kOne = 17592186044416.0;  // 2^44: masses in the bins are whole numbers of 2^-44 (2^19 of them fit 63 bits)
 
 struct Settings {
@@ -88,6 +89,17 @@ struct Pow2 {
     for (int i = 1; i < 9; ++i) g = fma(g, f, c[i]);
     return ldexp(fma(g, f, 1.0), (int)n);
   }
+  // 2^((x - m) a) for x with (x - m) a >= -1000, in three steps less: the nearest whole number is left in the low bits of a
+  // sum with 1.5 2^52, and added to the exponent.
+  __device__ __forceinline__ double near(float x, double m, double a) const {
+    constexpr double kWhole = 6755399441055744.0;
+    const double d = (double)x - m, u = fma(d, a, kWhole), f = fma(d, a, kWhole - u);
+    double g = c[0];
+#pragma unroll
+    for (int i = 1; i < 9; ++i) g = fma(g, f, c[i]);
+    g = fma(g, f, 1.0);
+    return __hiloint2double(__double2hiint(g) + (__double2loint(u) << 20), __double2loint(g));
+  }
 };
 
 // the weight of x against a finite maximum m
@@ -103,6 +115,7 @@ __device__ __forceinline__ float widen(uint16_t x) { return bf16_to_f32(x); }
 // raw: as they are, NaN too (a maximum and pow2 take no notice of it).
 template <typename T, bool raw = false>
 struct RowAt {
+  static constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;   // -infinity in every element of a word
   const T *base;
   int before, V;
   bool infinite;
@@ -138,18 +151,33 @@ __device__ __forceinline__ void unpack(const RowAt<T, raw> &r, u32x4 w, float *x
   }
 }
 
-// N elements from place `at` (a multiple of a piece, or within one) of the row on; those that are not the row's: -infinity
+template <int N, typename T, bool raw>
+__device__ __forceinline__ bool inside(const RowAt<T, raw> &r, int at) {
+  return at >= r.before && at + N <= r.before + r.V;
+}
+
+// A piece at the row's beginning or end: the elements that are not the row's are -infinity.
+template <typename T, bool raw>
+__device__ __forceinline__ u32x4 edge_piece(const RowAt<T, raw> &r, int at) {
+  constexpr int kPiece = 16 / sizeof(T);
+  u32x4 w = {r.none, r.none, r.none, r.none};
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i)
+    if (at + i >= r.before && at + i < r.before + r.V) {
+      const uint32_t x = r.base[at + i];
+      if constexpr (sizeof(T) == 4)
+        w[i] = x;
+      else
+        w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | x << 16 : (w[i / 2] & 0xffff0000u) | x;
+    }
+  return w;
+}
+
+// A piece's elements from place `at`; those that are not the row's: -infinity
 template <int N, typename T, bool raw>
 __device__ __forceinline__ void load_run(const RowAt<T, raw> &r, int at, float *x) {
-  constexpr int kPiece = 16 / sizeof(T);
-  static_assert(N <= kPiece, "one piece at most");
-  const int lo = r.before, hi = r.before + r.V;
-  if (N == kPiece && at >= lo && at + N <= hi) {
-    unpack<N>(r, *reinterpret_cast<const u32x4 *>(r.base + at), x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = at + i >= lo && at + i < hi ? r.at(r.base[at + i]) : -INFINITY;
-  }
+  static_assert(N == 16 / sizeof(T), "a piece");
+  unpack<N>(r, inside<N>(r, at) ? *reinterpret_cast<const u32x4 *>(r.base + at) : edge_piece(r, at), x);
 }
 
 // a thread's share of a segment, in the order of ids
@@ -188,15 +216,44 @@ __device__ __forceinline__ void load_segment(const RowAt<T, raw> &r, int seg, fl
   }
 }
 
+// ---- over a wave, by moves between its lanes ----
+template <int ctrl, int rows>
+__device__ __forceinline__ int moved(int x, int none) {
+  return __builtin_amdgcn_update_dpp(none, x, ctrl, rows, 0xf, false);
+}
+template <int ctrl, int rows>
+__device__ __forceinline__ double moved(double x, double none) {
+  return __hiloint2double(moved<ctrl, rows>(__double2hiint(x), __double2hiint(none)),
+                          moved<ctrl, rows>(__double2loint(x), __double2loint(none)));
+}
+template <int ctrl, int rows>
+__device__ __forceinline__ u64 moved(u64 x, u64 none) {
+  return (u64)(uint32_t)moved<ctrl, rows>((int)(x >> 32), (int)(none >> 32)) << 32 |
+         (uint32_t)moved<ctrl, rows>((int)x, (int)none);
+}
+// f over the lanes up to and with this one (rows of 16 lanes, then across them); none: f's neutral element
+template <typename N, typename F>
+__device__ __forceinline__ N wave_scan(N x, N none, F f) {
+  x = f(x, moved<0x111, 0xf>(x, none));
+  x = f(x, moved<0x112, 0xf>(x, none));
+  x = f(x, moved<0x114, 0xf>(x, none));
+  x = f(x, moved<0x118, 0xf>(x, none));
+  x = f(x, moved<0x142, 0xa>(x, none));
+  return f(x, moved<0x143, 0xc>(x, none));
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+__device__ __forceinline__ double last_lane(double x) {
+  return __hiloint2double(last_lane(__double2hiint(x)), last_lane(__double2loint(x)));
+}
 __device__ inline double wave_sum(double x) {
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-  return x;
+  return last_lane(wave_scan(x, 0.0, [](double a, double b) { return a + b; }));
 }
 
 // grid: rows x groups of kWaves segments
 template <typename T>
-__global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Settings s, int groups, float *maxima,
-                                                               double *sums) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(7))) void segments_kernel(
+    Logits l, Settings s, int groups, float *maxima, double *sums, int *large_rows) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *large_rows = 0;
   const int row = blockIdx.x / groups, lane = threadIdx.x & 63;
   const int seg = (int)(blockIdx.x % groups) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (seg >= l.segs) return;
@@ -220,8 +277,16 @@ __global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Setting
 #pragma unroll
       for (int i = 0; i < kLane; ++i) z += x[i] == m;
     } else {
+      // (what lies further below counts as 2^-990: masked elements, NaN; the sum is 1 or more)
+      const float lo = (float)((double)m - 990.0 / ask.a);
+      const double down = ((double)lo - (double)m) * ask.a;
+      if (down >= -1000.0 && down <= -900.0) {   // (not where fp32 has no such value)
 #pragma unroll
-      for (int i = 0; i < kLane; ++i) z += pow2(((double)x[i] - (double)m) * ask.a);
+        for (int i = 0; i < kLane; ++i) z += pow2.near(fmaxf(x[i], lo), m, ask.a);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) z += pow2(((double)x[i] - (double)m) * ask.a);
+      }
     }
     z = wave_sum(z);
   }
@@ -232,11 +297,7 @@ __global__ __launch_bounds__(64 * kWaves) void segments_kernel(Logits l, Setting
 template <typename N>
 __device__ N before_thread(N x, N *tmp, N *whole) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  N run = x;
-  for (int o = 1; o < 64; o <<= 1) {
-    const N y = __shfl_up(run, o);
-    if (lane >= o) run += y;
-  }
+  const N run = wave_scan(x, (N)0, [](N a, N b) { return a + b; });
   __syncthreads();
   if (lane == 63) tmp[wave] = run;
   __syncthreads();
@@ -252,7 +313,7 @@ __device__ N before_thread(N x, N *tmp, N *whole) {
 }
 
 __device__ inline int block_min(int x, int *tmp) {
-  for (int o = 1; o < 64; o <<= 1) x = min(x, __shfl_xor(x, o));
+  x = last_lane(wave_scan(x, 0x7fffffff, [](int a, int b) { return min(a, b); }));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -280,13 +341,8 @@ struct Shared {
   float groups[kMaxSegs * kGroups];  // maxima
   double mass[kMaxSegs];             // of a segment's kept elements
   int ties[kMaxSegs];                // its elements at the border
-  union {
-    Bins bins;
-    struct {
-      u64 few[kFew];
-    };
-  };
-  u64 list[kList];   // keys (make_key) of candidates
+  Bins bins;                         // or arrays of their size
+  u64 list[kList + kPad];            // keys (make_key) of candidates
   double tmp_d[kRowWaves];
   u64 tmp_u[kRowWaves];
   int tmp_i[kRowWaves];
@@ -305,6 +361,7 @@ struct Large {
 
 struct Work {
   Large *large;  // [rows], NULL: no row of the call can be one
+  int *rows;     // [1 + rows] how many there are, which
   u64 *bins;     // [rows][kBins]
   u64 *list;     // [rows][kList] the elements in the border's bin
   u64 *above;    // [rows] the mass before that bin
@@ -330,6 +387,9 @@ struct Finish {
   Row ask;
   int segs;
   float m;
+  Pow2 pow2;
+
+  __device__ __forceinline__ double weight_of(float x) const { return pow2(((double)x - (double)m) * ask.a); }
 
   __device__ float segment_max(int seg) const {
     float x = sh.groups[seg * kGroups];
@@ -427,7 +487,7 @@ struct Finish {
         for (const float v : x) {
           const uint32_t key = ordered_bits(v);
           if (key < lo || key > hi || v == -INFINITY) continue;
-          add((int)((hi - key) >> shift), weight(v, m, ask.a));
+          add((int)((hi - key) >> shift), weight_of(v));
         }
       }, [](int) {});
       int n;
@@ -444,7 +504,7 @@ struct Finish {
       if (shift == 0) {
         Border o;
         o.key = lo;
-        const double w1 = weight(ordered_to_float(lo), m, ask.a), mass = (double)above_w / kOne;
+        const double w1 = weight_of(ordered_to_float(lo)), mass = (double)above_w / kOne;
         double ties = by_mass ? ceil((want - mass) / w1) : want - above_n;
         if (!(ties < (double)here)) ties = here;   // (NaN: a weight of 0)
         o.ties = max((int)ties, above_n > 0 ? 0 : 1);
@@ -469,7 +529,7 @@ struct Finish {
         if (key == edge.key) {
           ++ties;
         } else if (key > edge.key) {
-          const double w = weight(v, m, ask.a);
+          const double w = weight_of(v);
           if (w >= ask.q) z += w;
         }
       }
@@ -482,7 +542,7 @@ struct Finish {
     });
     __syncthreads();
     if (!edge.key) return;
-    double w = weight(ordered_to_float(edge.key), m, ask.a);
+    double w = weight_of(ordered_to_float(edge.key));
     if (w < ask.q) w = 0.0;
     int t = 0, all;
     const int each = (segs + kRowThreads - 1) / kRowThreads, first = (int)threadIdx.x * each;
@@ -540,7 +600,7 @@ struct Finish {
       w[i] = 0.0;
       if (v[i] == -INFINITY) continue;
       if (key[i] > edge.key || (key[i] == edge.key && rank < edge.ties)) {
-        w[i] = weight(v[i], m, ask.a);
+        w[i] = weight_of(v[i]);
         if (w[i] < ask.q) w[i] = 0.0;
       }
       rank += key[i] == edge.key;
@@ -570,254 +630,263 @@ struct Finish {
 
   // ---- rows of which few elements can be kept: a list of them in LDS ----
 
-  // Of the list's elements with f, in their order: the n-th (from 0), or by_mass the last one before which the mass is
-  // below `want`.  *kept: the mass down to and with it.  *fits: whether they are few enough to be ranked (else nothing
-  // is found).
-  template <typename F>
-  __device__ u64 among(F f, bool by_mass, int n, double want, double *kept, bool *fits) {
-    __syncthreads();
-    if (threadIdx.x == 0) sh.at = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
-      const u64 key = sh.list[i];
-      if (!f(key_value(key))) continue;
-      const int at = atomicAdd(&sh.at, 1);
-      if (at < kFew) sh.few[at] = key;
-    }
-    __syncthreads();
-    const int c = sh.at;
-    *fits = c <= kFew;
-    if (!*fits) return 0;
-    // (the bins are no longer there: the keys lie in their place)
-    u64 key = 0, found = 0;
-    int rank = 0;
-    if ((int)threadIdx.x < c) {
-      key = sh.few[threadIdx.x];
-      for (int i = 0; i < c; ++i) rank += sh.few[i] > key;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < c) sh.few[rank] = key;
-    __syncthreads();
-    const int tid = threadIdx.x;
-    key = tid < c ? sh.few[tid] : 0;
-    const double w = tid < c ? weight(key_value(key), m, ask.a) : 0.0;
-    double all;
-    const double before = before_thread(w, sh.tmp_d, &all);
-    const bool in = tid < c && (by_mass ? tid == 0 || before < want : tid <= n);
-    // (weights fall and sums do not: what is kept is the first few)
-    const int count = block_min(in ? kRowThreads : tid, sh.tmp_i);
-    const int last = min(count, c) - 1;
-    if (tid == last) sh.u = key, sh.before = before + w;
-    __syncthreads();
-    found = sh.u;
-    const double mass = sh.before;
-    *kept = mass;
-    return found;
-  }
-
-  // The same of a list of at most an element a thread, put in order.
-  __device__ void from_short_list(double u, double whole, int *token, double *own, double *kept) {
+  // Of the list's elements, in their order, the last one before which the mass is below `want`.
+  __device__ u64 last_below(double want) {
+    constexpr int kEach = kList / kRowThreads;
     const int tid = threadIdx.x, n = sh.n;
-    u64 key = tid < n ? sh.list[tid] : 0;
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += sh.list[i] > key;
-    u64 *const order = sh.bins.mass;
-    double *const weights = reinterpret_cast<double *>(sh.bins.mass + kRowThreads);
-    if (tid < n) order[rank] = key;
-    __syncthreads();
-    key = tid < n ? order[tid] : 0;
-    const double w = tid < n ? weight(key_value(key), m, ask.a) : 0.0;
-    const bool first_k = tid < n && (!ask.k || tid < ask.k);
-    bool in = first_k && w >= ask.q;
-    if (ask.p <= 1.0) {
-      double z;
-      const double before = before_thread(first_k ? w : 0.0, sh.tmp_d, &z);
-      in = in && (tid == 0 || before < ask.p * (ask.k ? z : whole));
+    put_in_order(sh.list, n, (u64)0, [](u64 a, u64 b) { return a > b; });
+    double w[kEach], sum = 0.0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = kEach * tid + i;
+      w[i] = at < n ? weight_of(key_value(sh.list[at])) : 0.0;
+      sum += w[i];
     }
-    // what is kept is the first few of the order; their running sums in the order of ids
-    weights[tid] = w;
-    const int c = block_min(in ? n : tid, sh.tmp_i);
-    const uint32_t id = key_index(key);
-    double run = 0.0, z = 0.0;
-    for (int i = 0; i < c; ++i) {
-      const double x = weights[i];
-      z += x;
-      if (key_index(order[i]) <= id) run += x;
+    double before = before_thread(sum, sh.tmp_d, &all);
+    int first_out = n;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = kEach * tid + i;
+      if (at > 0 && !(before < want)) first_out = min(first_out, at);
+      before += w[i];
     }
-    const double at = u * z;
-    const bool passes = tid < c && run > at && w > 0.0;
-    int least = block_min(passes ? (int)id : 0x7fffffff, sh.tmp_i);
-    // (the sums' last bits: the last id)
-    if (least == 0x7fffffff) least = -block_min(tid < c && w > 0.0 ? -(int)id : 0, sh.tmp_i);
-    if (tid < c && (int)id == least) sh.before = w;
-    __syncthreads();
-    *own = sh.before;
-    *token = least;
-    *kept = z;
+    return sh.list[block_min(first_out, sh.tmp_i) - 1];
   }
 
-  // Of the list (all elements >= lo of the row): the token.  False: it does not fit the bins' second step.
-  __device__ bool from_list(double u, double whole, int *token, double *own, double *kept) {
-    if (sh.n <= kRowThreads) {
-      from_short_list(u, whole, token, own, kept);
-      return true;
-    }
-    // the list's smallest value bounds the bins
-    float low = m;
-    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) low = fminf(low, key_value(sh.list[i]));
-    low = block_min(low, sh.tmp_i);
-    const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
-    u64 border = 0;   // the last kept element
-    const auto fill = [&] {
-      clear_bins();
-      for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
-        const float x = key_value(sh.list[i]);
-        add(bin_of(x, m, scale), weight(x, m, ask.a));
-      }
-    };
-    int n;
-    u64 w, all;
-    bool fits;
-    double part;
-    if (ask.k && ask.k < sh.n) {
-      fill();
-      const int k = ask.k, b = find_bin([&](int run_n, u64) { return run_n >= k; }, &n, &w, &all);
-      border = among([&](float x) { return bin_of(x, m, scale) == b; }, false, k - 1 - n, 0.0, &part, &fits);
-      if (!fits) return false;
-      whole = (double)w / kOne + part;
-    } else if (ask.k) {
-      fill();
-      find_bin([](int, u64) { return false; }, &n, &w, &all);
-      whole = (double)all / kOne;
-    }
-    if (ask.p <= 1.0) {
-      const double want = ask.p * whole;
-      fill();
-      const int b = find_bin([&](int, u64 run_w) { return (double)run_w / kOne >= want; }, &n, &w, &all);
-      const u64 edge = among([&](float x) { return bin_of(x, m, scale) == b; }, true, 0, want - (double)w / kOne, &part, &fits);
-      if (!fits) return false;
-      border = max(border, edge);
-    }
-    // by ids
-    clear_bins();
-    const int shift = max(0, 32 - __clz(r.V) - 11);
-    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
-      const u64 key = sh.list[i];
-      const double x = weight(key_value(key), m, ask.a);
-      if (key >= border && x >= ask.q && x > 0.0) add((int)(key_index(key) >> shift), x);
-    }
-    double z;
-    {
-      // (the whole first)
-      u64 mine = 0;
-      __syncthreads();
-      for (int i = threadIdx.x; i < kBins; i += kRowThreads) mine += sh.bins.mass[i];
-      before_thread(mine, sh.tmp_u, &all);
-      z = (double)all / kOne;
-    }
-    const double at = u * z;
-    const int b = find_bin([&](int, u64 run_w) { return (double)run_w / kOne > at; }, &n, &w, &all);
-    // the bin's elements by their ids (keys with the value left out: the least id is the greatest key)
-    __syncthreads();
-    if (threadIdx.x == 0) sh.at = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < sh.n; i += kRowThreads) {
-      const u64 key = sh.list[i];
-      if ((int)(key_index(key) >> shift) != b || key < border) continue;
-      const double x = weight(key_value(key), m, ask.a);
-      if (!(x >= ask.q && x > 0.0)) continue;
-      const int to = atomicAdd(&sh.at, 1);
-      if (to < kFew) sh.few[to] = key;
-    }
-    __syncthreads();
-    const int c = sh.at;
-    if (c > kFew) return false;
-    u64 key = 0;
-    int rank = 0;
-    if ((int)threadIdx.x < c) {
-      key = sh.few[threadIdx.x];
-      for (int i = 0; i < c; ++i) rank += key_index(sh.few[i]) < key_index(key);
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < c) sh.few[rank] = key;
-    __syncthreads();
+  // n numbers of LDS, all different, in order (more(a, b): a comes first), by counting those before each one.  kMine
+  // numbers a thread; where there are fewer, several threads share a number's count.  `last`: a number that comes after all,
+  // which fills the list up to whole 16-byte reads (kPad numbers more than n).
+  template <int kMine, typename N, typename F>
+  __device__ void put_in_order(N *list, int n, N last, F more) {
+    constexpr int kRead = 16 / sizeof(N);
     const int tid = threadIdx.x;
-    key = tid < c ? sh.few[tid] : 0;
-    const double x = tid < c ? weight(key_value(key), m, ask.a) : 0.0;
-    const double run = x + (double)w / kOne + before_thread(x, sh.tmp_d, &part);
-    const int which = min(block_min(tid < c && run > at ? tid : kRowThreads, sh.tmp_i), c - 1);
-    if (tid == which) sh.u = key, sh.before = x;
+    int split = 1;
+    if (kMine == 1)
+      while (split < 16 && n * split * 2 <= kRowThreads) split *= 2;
+    if (tid < kPad) list[n + tid] = last;
     __syncthreads();
-    *own = sh.before;
-    *token = (int)key_index(sh.u);
+    const int e = tid / split, part = tid % split, reads = (n + split * kRead - 1) / (split * kRead);
+    N mine[kMine];
+    int rank[kMine] = {};
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) mine[i] = list[min(e + i * kRowThreads, n)];
+    typedef N Read __attribute__((ext_vector_type(kRead)));
+#pragma unroll 4
+    for (int j = 0; j < reads; ++j) {
+      const Read x = *reinterpret_cast<const Read *>(list + (j * split + part) * kRead);
+#pragma unroll
+      for (int v = 0; v < kRead; ++v)
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) rank[i] += more(x[v], mine[i]);
+    }
+    if (kMine == 1)
+      for (int o = 1; o < split; o <<= 1) rank[0] += __shfl_xor(rank[0], o);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+      if (e + i * kRowThreads < n && part == 0) list[rank[i]] = mine[i];
+    __syncthreads();
+  }
+  template <typename N, typename F>
+  __device__ void put_in_order(N *list, int n, N last, F more) {
+    if (n <= kRowThreads)
+      put_in_order<1>(list, n, last, more);
+    else if (n <= 2 * kRowThreads)
+      put_in_order<2>(list, n, last, more);
+    else
+      put_in_order<kList / kRowThreads>(list, n, last, more);
+  }
+
+  // Of the list (all elements >= lo of the row): the token.  kEach elements a thread.
+  template <int kEach>
+  __device__ void from_list(double u, double whole, int *token, double *own, double *kept) {
+    const int tid = threadIdx.x, n = sh.n;
+    put_in_order(sh.list, n, (u64)0, [](u64 a, u64 b) { return a > b; });
+    uint32_t *const by_id = sh.bins.count;
+    double *const weights = reinterpret_cast<double *>(sh.bins.mass);
+    u64 key[kEach];
+    double w[kEach], sum = 0.0, z;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = kEach * tid + i;
+      key[i] = at < n ? sh.list[at] : 0;
+      w[i] = at < n && (!ask.k || at < ask.k) ? weight_of(key_value(key[i])) : 0.0;
+      sum += w[i];
+    }
+    double before = 0.0, want = INFINITY;
+    if (ask.p <= 1.0) {
+      before = before_thread(sum, sh.tmp_d, &z);
+      want = ask.p * (ask.k ? z : whole);
+    }
+    // what is kept is the first few of the order
+    int first_out = n;
+#pragma unroll
+    for (int i = kEach - 1; i >= 0; --i) {
+      const int at = kEach * tid + i;
+      double b = before;
+#pragma unroll
+      for (int j = 0; j < i; ++j) b += w[j];
+      const bool in = at < n && (!ask.k || at < ask.k) && w[i] >= ask.q && (at == 0 || b < want);
+      if (!in) first_out = min(first_out, at);
+    }
+    const int c = block_min(first_out, sh.tmp_i);
+    // their running sums in the order of ids: an id with its place in the order
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = kEach * tid + i;
+      if (at >= c) continue;
+      weights[at] = w[i];
+      by_id[at] = key_index(key[i]) << 10 | (uint32_t)at;
+    }
+    __syncthreads();
+    put_in_order(by_id, c, 0xffffffffu, [](uint32_t a, uint32_t b) { return a < b; });
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = kEach * tid + i;
+      w[i] = at < c ? weights[by_id[at] & (kList - 1)] : 0.0;
+      sum += w[i];
+    }
+    double run = before_thread(sum, sh.tmp_d, &z);
+    const double at = u * z;
+    int mine = kList, last = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      run += w[i];
+      if (w[i] > 0.0) last = kEach * tid + i;
+      if (run > at && w[i] > 0.0 && mine == kList) mine = kEach * tid + i;
+    }
+    int found = block_min(mine, sh.tmp_i);
+    if (found == kList) found = -block_min(-last, sh.tmp_i);   // (the sums' last bits)
+    const uint32_t id = by_id[found];
+    *own = weights[id & (kList - 1)];
+    *token = (int)(id >> 10);
     *kept = z;
-    return true;
   }
 
   // The elements >= lo into the list, from the groups that have any; false: they are too many.
   __device__ bool gather(float lo) {
+    const int tid = threadIdx.x, n_groups = segs * kGroups;
     __syncthreads();
-    if (threadIdx.x == 0) sh.n = 0, sh.at = 0;
-    __syncthreads();
+    if (tid == 0) sh.n = 0;
     int *const found = reinterpret_cast<int *>(sh.bins.mass);   // groups
-    for (int g = threadIdx.x; g < segs * kGroups; g += kRowThreads)
-      if (sh.groups[g] >= lo && sh.groups[g] > -INFINITY) {
-        const int to = atomicAdd(&sh.at, 1);
-        if (to < kList) found[to] = g;
-      }
-    __syncthreads();
-    const int c = sh.at;
+    int mine = 0, c;
+    for (int g = tid; g < n_groups; g += kRowThreads) mine += sh.groups[g] >= lo && sh.groups[g] > -INFINITY;
+    int to = before_thread(mine, sh.tmp_i, &c);
     if (c > kList) return false;   // (an element each)
-    // a group's pieces with neighbouring lanes
-    constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece * kGroupLanes;
-    for (int i = threadIdx.x; i < c * kPieces; i += kRowThreads) {
+    for (int g = tid; g < n_groups; g += kRowThreads)
+      if (sh.groups[g] >= lo && sh.groups[g] > -INFINITY) found[to++] = g;
+    __syncthreads();
+    // a group's pieces with neighbouring lanes.  (The code is kept short here and in what follows: a row passes through
+    // once, so fetching instructions counts for more than running them.)
+    constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece * kGroupLanes, kAtOnce = 64 / kPiece;
+    const auto place_of = [&](int i) {
       const int g = found[i / kPieces], piece = i % kPieces;
-      const int at = piece_at<T>(g / kGroups, g % kGroups * kGroupLanes + piece % kGroupLanes, piece / kGroupLanes);
-      float x[kPiece];
-      load_run<kPiece>(r, at, x);
+      return piece_at<T>(g / kGroups, g % kGroups * kGroupLanes + piece % kGroupLanes, piece / kGroupLanes);
+    };
+    const float bound = r.infinite ? INFINITY : lo;   // (of the elements as they are; NaN is not above it)
+    for (int i0 = tid; i0 < (c * kPieces + kRowThreads - 1) / kRowThreads * kRowThreads; i0 += kAtOnce * kRowThreads) {
+      u32x4 w[kAtOnce];   // (all in flight: a round takes as long as memory does)
 #pragma unroll
-      for (int j = 0; j < kPiece; ++j)
-        if (x[j] >= lo && x[j] > -INFINITY) {
-          const int to = atomicAdd(&sh.n, 1);
-          if (to < kList) sh.list[to] = make_key(x[j], (uint32_t)(at + j - r.before));
+      for (int n = 0; n < kAtOnce; ++n) {
+        const int i = i0 + n * kRowThreads;
+        w[n] = u32x4{r.none, r.none, r.none, r.none};
+        if (i >= c * kPieces) continue;
+        const int at = place_of(i);
+        if (inside<kPiece>(r, at)) w[n] = *reinterpret_cast<const u32x4 *>(r.base + at);
+      }
+      // 64 elements a lane: a bit each
+      uint32_t hits[2] = {};
+#pragma unroll
+      for (int n = 0; n < kAtOnce; ++n)
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) {
+          float x;
+          if constexpr (sizeof(T) == 4)
+            x = __uint_as_float(w[n][j]);
+          else
+            x = __uint_as_float(j & 1 ? w[n][j / 2] & 0xffff0000u : w[n][j / 2] << 16);
+          uint32_t &h = hits[(n * kPiece + j) / 32];
+          h = h + h + (x >= bound);
         }
+      mine = __popc(hits[0]) + __popc(hits[1]);
+      int place = wave_scan(mine, 0, [](int a, int b) { return a + b; });
+      const int all = last_lane(place);
+      if (!all) continue;
+      int base = 0;
+      if ((tid & 63) == 0) base = atomicAdd(&sh.n, all);
+      place += __builtin_amdgcn_readfirstlane(base) - mine;
+      u64 left = (u64)hits[0] << 32 | hits[1];   // (the first element in the highest bit)
+      while (left) {
+        const int e = __clzll((long long)left);
+        left &= ~(0x8000000000000000ull >> e);
+        const int at = place_of(i0 + e / kPiece * kRowThreads) + e % kPiece;
+        if (place < kList) sh.list[place] = make_key(r.at(r.base[at]), (uint32_t)(at - r.before));
+        ++place;
+      }
+    }
+    // the pieces at the row's beginning and end
+#pragma unroll 1
+    for (int i = tid; i < c * kPieces; i += kRowThreads) {
+      const int at = place_of(i);
+      if (inside<kPiece>(r, at)) continue;
+#pragma unroll 1
+      for (int e = max(at, r.before); e < min(at + kPiece, r.before + r.V); ++e) {
+        const float x = r.at(r.base[e]);
+        if (!(x >= lo)) continue;
+        const int place = atomicAdd(&sh.n, 1);
+        if (place < kList) sh.list[place] = make_key(x, (uint32_t)(e - r.before));
+      }
     }
     __syncthreads();
     return sh.n <= kList;
   }
 
-  // The same by an order of the threads' maxima (of every kRowThreads-th group each), where they suffice.
+  // reach() by the order of the maxima of kTops parts of the groups, where they suffice.
+  template <int kTops>
   __device__ float reach_of_few(bool by_mass, double want) {
-    const int tid = threadIdx.x;
+    constexpr int kSplit = kRowThreads / kTops;   // threads a maximum
+    const int tid = threadIdx.x, e = tid / kSplit, part = tid % kSplit;
     float top = -INFINITY;
     for (int g = tid; g < segs * kGroups; g += kRowThreads) top = fmaxf(top, sh.groups[g]);
-    float *const tops = reinterpret_cast<float *>(sh.bins.count), *const order = tops + kRowThreads;
-    tops[tid] = top;
+    for (int o = 1; o < kSplit; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    // (their ordered bits with a number in the last eight: all different, and no value is above its maximum)
+    static_assert(kTops <= 256, "eight bits of a number");
+    uint32_t *const tops = sh.bins.count, *const order = tops + kTops;
+    const uint32_t mine = (ordered_bits(top) & ~255u) | (uint32_t)e;
+    if (part == 0) tops[e] = mine;
     __syncthreads();
     int rank = 0;
 #pragma unroll 4
-    for (int i = 0; i < kRowThreads; i += 4) {
-      const float4 v = *reinterpret_cast<const float4 *>(tops + i);
-      rank += (v.x > top || (v.x == top && i < tid)) + (v.y > top || (v.y == top && i + 1 < tid)) +
-              (v.z > top || (v.z == top && i + 2 < tid)) + (v.w > top || (v.w == top && i + 3 < tid));
+    for (int i = part * 4; i < kTops; i += 4 * kSplit) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(tops + i);
+      rank += (v.x > mine) + (v.y > mine) + (v.z > mine) + (v.w > mine);
     }
-    order[rank] = top;
+    for (int o = 1; o < kSplit; o <<= 1) rank += __shfl_xor(rank, o);
+    if (part == 0) order[rank] = mine;
     __syncthreads();
-    if (!by_mass) return order[(int)want - 1];
-    const float x = order[tid];
+    const auto value_at = [&](int i) {
+      const uint32_t bits = order[i] & ~255u;
+      return bits > ordered_bits(-INFINITY) ? ordered_to_float(bits) : -INFINITY;
+    };
+    if (!by_mass) return value_at((int)want - 1);
+    const float x = tid < kTops ? value_at(tid) : -INFINITY;
     double all;
-    const double w = x > -INFINITY ? weight(x, m, ask.a) : 0.0, run = w + before_thread(w, sh.tmp_d, &all);
+    const double w = x > -INFINITY ? weight_of(x) : 0.0, run = w + before_thread(w, sh.tmp_d, &all);
     const int at = block_min(run >= want ? tid : kRowThreads, sh.tmp_i);
-    return at < kRowThreads ? order[at] : -INFINITY;
+    return at < kTops ? value_at(at) : -INFINITY;
   }
 
   // A value such that the elements >= it reach `want` (their number, or by_mass their weights): by the groups' maxima
   // alone, which is less than there is.  -infinity: not reached.
   __device__ float reach(bool by_mass, double want) {
-    if (by_mass || want <= kRowThreads) {
-      const float x = reach_of_few(by_mass, want);
-      if (x > -INFINITY) return x;
-    }
+    // (few, as their order costs the square of their number; so many that most of those looked for are in parts of their own)
+    float x = -INFINITY;
+    if (by_mass || want <= 64.0)
+      x = reach_of_few<128>(by_mass, want);
+    else if (want <= kRowThreads)
+      x = reach_of_few<kRowThreads>(false, want);
+    if (x > -INFINITY) return x;
     float low = m;
     const int n_groups = segs * kGroups;
     for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
@@ -826,7 +895,7 @@ struct Finish {
     const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
     clear_bins();
     for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
-      if (sh.groups[g] > -INFINITY) add(bin_of(sh.groups[g], m, scale), by_mass ? weight(sh.groups[g], m, ask.a) : 0.0);
+      if (sh.groups[g] > -INFINITY) add(bin_of(sh.groups[g], m, scale), by_mass ? weight_of(sh.groups[g]) : 0.0);
     int n;
     u64 w, all;
     const auto holds = [&](int run_n, u64 run_w) { return by_mass ? (double)run_w / kOne >= want : (double)run_n >= want; };
@@ -871,10 +940,19 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
   Row &ask = f.ask;
   const int64_t first = (int64_t)row * l.segs;
   float m = -INFINITY;
-  for (int i = tid; i < l.segs * kGroups; i += kRowThreads) {
-    const float x = maxima[first * kGroups + i];
-    sh.groups[i] = x;
-    m = fmaxf(m, x);
+  for (int i0 = tid; i0 < l.segs * kGroups; i0 += 8 * kRowThreads) {
+    float x[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const int i = i0 + n * kRowThreads;
+      x[n] = i < l.segs * kGroups ? maxima[first * kGroups + i] : -INFINITY;
+    }
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const int i = i0 + n * kRowThreads;
+      if (i < l.segs * kGroups) sh.groups[i] = x[n];
+      m = fmaxf(m, x[n]);
+    }
   }
   m = block_max(m, sh.tmp_i);
   if (m == INFINITY) {
@@ -908,7 +986,7 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
       double z = 0.0;
       for (int i = tid; i < l.segs; i += kRowThreads) {
         const float top = f.segment_max(i);
-        const double x = top > -INFINITY ? sums[first + i] * weight(top, m, ask.a) : 0.0;
+        const double x = top > -INFINITY ? sums[first + i] * f.weight_of(top) : 0.0;
         sh.mass[i] = x;
         sh.ties[i] = 0;
         z += x;
@@ -929,10 +1007,16 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
         near = fmaxf(near, f.reach(false, (double)ask.k));
       else if (ask.p <= 1.0)
         near = fmaxf(near, f.reach(true, ask.p * whole * (1.0 + 1e-9)));
-      if (!f.gather(near) || !f.from_list(at, whole, &token, &own, &whole)) {
+      if (f.gather(near)) {
+        if (sh.n <= kRowThreads)
+          f.template from_list<1>(at, whole, &token, &own, &whole);
+        else
+          f.template from_list<kList / kRowThreads>(at, whole, &token, &own, &whole);
+      } else {
         if (work.large && !ask.k) {
           large = true;
           Large &x = work.large[row];
+          if (tid == 0) work.rows[1 + atomicAdd(work.rows, 1)] = row;
           if (tid == 0) x = Large{ask.p <= 1.0 ? 1 : 2, m, lo, m > lo ? (float)(kBins - 1) / (m - lo) : 0.0f, whole, f.r.infinite, 0};
           for (int i = tid; i < kBins; i += kRowThreads) work.bins[(int64_t)row * kBins + i] = 0;
         } else {
@@ -943,112 +1027,128 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
       token = f.pick(at, Border{0u, 0, 0.0}, &own, &whole);
     }
   }
-  if (large) return;
-  if (work.large && tid == 0) work.large[row].on = 0;
-  answer(row, token, own, whole, tokens, logprobs);
+  if (!large) answer(row, token, own, whole, tokens, logprobs);
 }
 
 // ---- rows of which many elements are kept: the passes over all workgroups ----
 
-// Masses in bins of values, from m down to lo.  grid: rows x parts
+// (each over the listed rows' parts, or rows, by as many workgroups as are useful at once)
+
+// Masses in bins of values, from m down to lo.
 template <typename T>
-__global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, int parts, const float *maxima, Work work) {
-  const int row = blockIdx.x / parts;
-  const Large x = work.large[row];
-  if (x.on != 1) return;
+__global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, int parts, Work work) {
   __shared__ u64 bins[kBins];
-  for (int i = threadIdx.x; i < kBins; i += 64 * kPart) bins[i] = 0;
-  __syncthreads();
-  const int seg = (int)(blockIdx.x % parts) * kPart + (threadIdx.x >> 6);
-  if (seg < l.segs) {
+  const int items = *work.rows * parts;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    const int row = work.rows[1 + item / parts];
+    const Large x = work.large[row];
+    if (x.on != 1) continue;
+    const int seg = item % parts * kPart + (threadIdx.x >> 6);
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
-    const Row ask = row_of(s, row, l.V);
     float v[kLane];
-    load_segment(r, seg, v);
-    const Pow2 pow2;
+    if (seg < l.segs) load_segment(r, seg, v);
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += 64 * kPart) bins[i] = 0;
+    __syncthreads();
+    if (seg < l.segs) {
+      const Row ask = row_of(s, row, l.V);
+      const Pow2 pow2;
 #pragma unroll
-    for (int i = 0; i < kLane; ++i)
-      if (v[i] >= x.lo) atomicAdd(&bins[bin_of(v[i], x.m, x.scale)], whole_number(weight(v[i], x.m, ask.a, pow2)));
+      for (int i = 0; i < kLane; ++i)
+        if (v[i] >= x.lo) atomicAdd(&bins[bin_of(v[i], x.m, x.scale)], whole_number(weight(v[i], x.m, ask.a, pow2)));
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += 64 * kPart)
+      if (bins[i]) atomicAdd(&work.bins[(int64_t)row * kBins + i], bins[i]);
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < kBins; i += 64 * kPart)
-    if (bins[i]) atomicAdd(&work.bins[(int64_t)row * kBins + i], bins[i]);
 }
 
 // The border's bin (each workgroup finds it again); the mass of each segment's elements before it, and the elements in it into a
-// list.  grid: rows x parts
+// list.
 template <typename T>
 __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s, int parts, double *masses, Work work) {
-  const int row = blockIdx.x / parts, tid = threadIdx.x;
-  const Large x = work.large[row];
-  if (!x.on) return;
   __shared__ u64 tmp[kRowWaves];
   __shared__ int tmp_i[kRowWaves];
-  const Row ask = row_of(s, row, l.V);
-  int border = kBins;
-  if (x.on == 1) {
-    constexpr int kEach = kBins / (64 * kPart);
-    static_assert(kPart == kRowWaves, "sums over a workgroup");
-    u64 w[kEach], sum = 0, all;
+  static_assert(kPart == kRowWaves, "sums over a workgroup");
+  const int tid = threadIdx.x, items = *work.rows * parts;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    const int row = work.rows[1 + item / parts];
+    const Large x = work.large[row];
+    const int seg = item % parts * kPart + (tid >> 6);
+    RowAt<T> r = row_at<T>(l, row);
+    r.infinite = x.infinite;
+    float v[kLane];
+    if (seg < l.segs) load_segment(r, seg, v);
+    const Row ask = row_of(s, row, l.V);
+    int border = kBins;
+    if (x.on == 1) {
+      constexpr int kEach = kBins / (64 * kPart);
+      u64 w[kEach], sum = 0, above = 0, all;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += w[i] = work.bins[(int64_t)row * kBins + kEach * tid + i];
-    u64 run = before_thread(sum, tmp, &all);
-    const double want = ask.p * x.whole;
-    int mine = kBins;
+      for (int i = 0; i < kEach; ++i) sum += w[i] = work.bins[(int64_t)row * kBins + kEach * tid + i];
+      u64 run = before_thread(sum, tmp, &all);
+      const double want = ask.p * x.whole;
+      int mine = kBins;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const u64 before = run;
-      run += w[i];
-      if (w[i] && (double)run / kOne >= want && mine == kBins) mine = kEach * tid + i, sum = before;
+      for (int i = 0; i < kEach; ++i) {
+        const u64 before = run;
+        run += w[i];
+        if (w[i] && (double)run / kOne >= want && mine == kBins) mine = kEach * tid + i, above = before;
+      }
+      border = block_min(mine, tmp_i);
+      // (never reached: all is kept)
+      if (border < kBins && border == mine && item % parts == 0) work.above[row] = above;
     }
-    border = block_min(mine, tmp_i);
-    // (never reached: all is kept)
-    if (border < kBins && border == mine && blockIdx.x % parts == 0) work.above[row] = sum;
-  }
-  const int seg = (int)(blockIdx.x % parts) * kPart + (tid >> 6);
-  if (seg >= l.segs) return;
-  RowAt<T> r = row_at<T>(l, row);
-  r.infinite = x.infinite;
-  float v[kLane];
-  load_segment(r, seg, v);
-  constexpr int kPiece = 16 / sizeof(T);
-  const Pow2 pow2;
-  double z = 0.0;
+    if (seg >= l.segs) continue;
+    constexpr int kPiece = 16 / sizeof(T);
+    const Pow2 pow2;
+    double z = 0.0;
+    int mine = 0;
 #pragma unroll
-  for (int i = 0; i < kLane; ++i) {
-    if (!(v[i] >= x.lo)) continue;
-    const int b = bin_of(v[i], x.m, x.scale);
-    if (b < border) {
-      const double w = weight(v[i], x.m, ask.a, pow2);
-      if (w >= ask.q) z += w;
-    } else if (b == border) {
-      const int to = atomicAdd(&work.large[row].listed, 1);
-      if (to < kList)
-        work.list[(int64_t)row * kList + to] =
-            make_key(v[i], (uint32_t)(piece_at<T>(seg, tid & 63, i / kPiece) + i % kPiece - r.before));
+    for (int i = 0; i < kLane; ++i) {
+      if (!(v[i] >= x.lo)) continue;
+      const int b = bin_of(v[i], x.m, x.scale);
+      if (b < border) {
+        const double w = weight(v[i], x.m, ask.a, pow2);
+        if (w >= ask.q) z += w;
+      }
+      mine += b == border;
     }
+    int place = wave_scan(mine, 0, [](int a, int b) { return a + b; });
+    const int listed = last_lane(place);
+    if (listed) {   // (one atomic for the wave)
+      int base = 0;
+      if ((tid & 63) == 0) base = atomicAdd(&work.large[row].listed, listed);
+      place += __builtin_amdgcn_readfirstlane(base) - mine;
+#pragma unroll
+      for (int i = 0; i < kLane; ++i)
+        if (v[i] >= x.lo && bin_of(v[i], x.m, x.scale) == border) {
+          if (place < kList)
+            work.list[(int64_t)row * kList + place] =
+                make_key(v[i], (uint32_t)(piece_at<T>(seg, tid & 63, i / kPiece) + i % kPiece - r.before));
+          ++place;
+        }
+    }
+    z = wave_sum(z);
+    if ((tid & 63) == 0) masses[(int64_t)row * l.segs + seg] = z;
   }
-  z = wave_sum(z);
-  if ((tid & 63) == 0) masses[(int64_t)row * l.segs + seg] = z;
 }
 
-// The border among its bin's elements, and the token.  grid: rows
+// The border among its bin's elements, and the token.
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s, const float *u, const float *maxima,
-                                                            const double *masses, Work work, int32_t *tokens,
-                                                            float *logprobs) {
-  const int row = blockIdx.x, tid = threadIdx.x;
+__device__ void finish_large(Shared &sh, int row, const Logits &l, const Settings &s, const float *u, const float *maxima,
+                             const double *masses, const Work &work, int32_t *tokens, float *logprobs) {
+  const int tid = threadIdx.x;
   const Large x = work.large[row];
-  if (!x.on) return;
-  __shared__ Shared sh;
+  __syncthreads();
   Finish<T> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, x.m};
   f.r.infinite = x.infinite;
   const int64_t first = (int64_t)row * l.segs;
   const double at = number_of(u, row);
   double own = 1.0, whole = x.whole;
   int token;
-  bool fits = x.listed <= kList;
+  const bool fits = x.listed <= kList;
   Border edge{0u, 0, 0.0};
   if (fits) {
     if (tid == 0) sh.n = x.listed;
@@ -1056,10 +1156,8 @@ __global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s
     for (int i = tid; i < l.segs; i += kRowThreads) sh.mass[i] = masses[first + i], sh.ties[i] = 0;
     __syncthreads();
     if (x.listed) {
-      double part;
-      const double want = f.ask.p * x.whole - (double)work.above[row] / kOne;
-      const u64 border = f.among([](float) { return true; }, true, 0, want, &part, &fits);
-      if (fits) {
+      const u64 border = f.last_below(f.ask.p * x.whole - (double)work.above[row] / kOne);
+      {
         // the kept ones of the bin join their segments (whole numbers: in any order); of the border's equals only those
         // up to it are kept
         u64 *const more = sh.bins.mass;
@@ -1076,7 +1174,7 @@ __global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s
           if (bits == edge.key) atomicAdd(&sh.ties[seg], 1);
           if (key < border) continue;
           if (bits == edge.key) atomicAdd(&sh.at, 1);
-          const double w = weight(key_value(key), x.m, f.ask.a);
+          const double w = f.weight_of(key_value(key));
           if (w >= f.ask.q) atomicAdd(&more[seg], whole_number(w));
         }
         __syncthreads();
@@ -1101,10 +1199,20 @@ __global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s
   answer(row, token, own, whole, tokens, logprobs);
 }
 
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s, const float *u, const float *maxima,
+                                                            const double *masses, Work work, int32_t *tokens,
+                                                            float *logprobs) {
+  __shared__ Shared sh;
+  const int rows = *work.rows;
+  for (int i = blockIdx.x; i < rows; i += gridDim.x)
+    finish_large<T>(sh, work.rows[1 + i], l, s, u, maxima, masses, work, tokens, logprobs);
+}
+
 int segments(int V) { return (V + 15 + kSeg - 1) / kSeg; }
 
 struct Layout {
-  size_t sums, maxima, large, above, bins, list, bytes;
+  size_t sums, maxima, large, rows, above, bins, list, bytes;
 };
 Layout layout(int rows, int V) {
   Layout w;
@@ -1118,6 +1226,7 @@ Layout layout(int rows, int V) {
   w.sums = take(segs * sizeof(double));
   w.maxima = take(segs * kGroups * sizeof(float));
   w.large = take(rows * sizeof(Large));
+  w.rows = take((rows + 1) * sizeof(int));
   w.above = take(rows * sizeof(u64));
   w.bins = take((size_t)rows * kBins * sizeof(u64));
   w.list = take((size_t)rows * kList * sizeof(u64));
@@ -1176,18 +1285,21 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   // its row's workgroup's)
   const bool can_be_large = l.segs > kFewSegs && (how->top_ks || how->top_k == 0) &&
                             (how->top_ps || how->top_p < 1.0f || how->min_ps || how->min_p > 0.0f);
-  const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<u64 *>(at + w.bins),
-                  reinterpret_cast<u64 *>(at + w.list), reinterpret_cast<u64 *>(at + w.above)};
+  const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<int *>(at + w.rows),
+                  reinterpret_cast<u64 *>(at + w.bins), reinterpret_cast<u64 *>(at + w.list),
+                  reinterpret_cast<u64 *>(at + w.above)};
   const int groups = (l.segs + kWaves - 1) / kWaves, parts = (l.segs + kPart - 1) / kPart;
   hipStream_t q = static_cast<hipStream_t>(stream);
   auto launch = [&](auto t) {
     using T = decltype(t);
-    segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums);
+    segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums, work.rows);
     row_kernel<T><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
     if (can_be_large) {
-      bins_kernel<T><<<(unsigned)(rows * parts), 64 * kPart, 0, q>>>(l, s, parts, maxima, work);
-      masses_kernel<T><<<(unsigned)(rows * parts), 64 * kPart, 0, q>>>(l, s, parts, sums, work);
-      large_kernel<T><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
+      const int64_t all = (int64_t)rows * parts;
+      const unsigned some = (unsigned)(all < kSpread ? all : kSpread), few = (unsigned)(rows < kSpread ? rows : kSpread);
+      bins_kernel<T><<<some, 64 * kPart, 0, q>>>(l, s, parts, work);
+      masses_kernel<T><<<some, 64 * kPart, 0, q>>>(l, s, parts, sums, work);
+      large_kernel<T><<<few, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
     }
   };
   if (logits_dtype == DT_F32)

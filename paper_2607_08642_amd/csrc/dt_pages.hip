@@ -72,80 +72,116 @@ __device__ int before_thread(int x, int *tmp, int *whole) {
   return first + run - x;
 }
 
-// What other threads of the workgroup wrote to memory is there after it.
-__device__ inline void meet() {
-  __threadfence();
-  __syncthreads();
-  __threadfence();
-}
-
 __device__ inline int held_of(const Book &k, int b) { return min(max(k.held[b], 0), k.width); }
 __device__ inline int len_of(const Book &k, int b) { return min(max(k.lens[b], 0), k.width * k.page_size); }
 
-// The `want` lowest free pages into list[]; how many there are (all of them counted only where they do not suffice)
-__device__ int lowest_free(const Book &k, int want, int32_t *list, int *tmp) {
+// The `want` lowest free pages: the first kTaken of them in LDS, the rest in list[]; how many there are (all
+// of them counted only where they do not suffice).  What the workgroup wrote before is there after a barrier: it is one
+// workgroup's memory.
+constexpr int kTaken = 4096;
+struct Taken {
+  int pages[kTaken];
+  __device__ int at(const int32_t *list, int i) const { return i < kTaken ? pages[i] : list[i]; }
+};
+__device__ int lowest_free(const Book &k, int want, int32_t *list, Taken &taken, int *tmp) {
+  constexpr int kEach = 4;
   int found = 0;
-  for (int p0 = 0; p0 < k.pages && found < want; p0 += 4 * kBookThreads) {
-    const int p = p0 + 4 * (int)threadIdx.x;
+  for (int p0 = 0; p0 < k.pages && found < want; p0 += kEach * kBookThreads) {
+    const int p = p0 + kEach * (int)threadIdx.x;
     int free = 0, all;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kEach; ++i)
       if (p + i < k.pages && k.uses[p + i] <= 0) free |= 1 << i;
     int at = found + before_thread(__popc(free), tmp, &all);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kEach; ++i)
       if (free >> i & 1) {
-        if (at < want) list[at] = p + i;
+        if (at < min(want, kTaken))
+          taken.pages[at] = p + i;
+        else if (at < want)
+          list[at] = p + i;
         ++at;
       }
     found += all;
   }
+  __syncthreads();
   return found;
 }
 
+// Items dealt to sequences: which one item i belongs to (the last whose first item is not after it).
+__device__ inline int owner(const int *first, int n, int i) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= i)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+// One workgroup.  Every step over pages is dealt out evenly, a page a thread, so what counts is the number of times that one
+// step waits for the memory of another: lengths; entries that go; uses; entries that come.
 __global__ __launch_bounds__(kBookThreads) void fit_kernel(Book k, Scratch s) {
   __shared__ int tmp[kBookWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // pages that go, a wave for a sequence; then how many each one lacks
-  for (int b = wave; b < k.batch; b += kBookWaves) {
-    const int want = (len_of(k, b) + k.page_size - 1) / k.page_size, held = held_of(k, b);
-    int32_t *row = k.table + (int64_t)b * k.width;
-    for (int e = want + lane; e < held; e += 64) {
-      const int p = row[e];
-      if (p >= 0 && p < k.pages) atomicSub(k.uses + p, 1);
-      row[e] = -1;
-    }
-  }
+  __shared__ int first[kBookThreads], start[kBookThreads];   // of a sequence: its first item, its first entry
+  __shared__ Taken taken;
+  const int tid = threadIdx.x;
   int total = 0;
   for (int b0 = 0; b0 < k.batch; b0 += kBookThreads) {
-    const int b = b0 + tid;
-    int lacks = 0, all;
-    if (b < k.batch) lacks = max((len_of(k, b) + k.page_size - 1) / k.page_size - held_of(k, b), 0);
-    const int at = before_thread(lacks, tmp, &all);
-    if (b < k.batch) s.first[b] = total + at;
-    total += all;
+    const int b = b0 + tid, n = min(k.batch - b0, kBookThreads);
+    int want = 0, held = 0, goes, lacks;
+    if (b < k.batch) {
+      want = (len_of(k, b) + k.page_size - 1) / k.page_size;
+      held = held_of(k, b);
+    }
+    const int at = before_thread(max(held - want, 0), tmp, &goes);
+    before_thread(max(want - held, 0), tmp, &lacks);
+    first[tid] = at;
+    start[tid] = want;
+    total += lacks;
+    __syncthreads();
+    for (int i = tid; i < goes; i += kBookThreads) {
+      const int q = owner(first, n, i);
+      int32_t &entry = k.table[(int64_t)(b0 + q) * k.width + start[q] + i - first[q]];
+      const int p = entry;
+      if (p >= 0 && p < k.pages) atomicSub(k.uses + p, 1);
+      entry = -1;
+    }
+    if (want < held) k.held[b] = want;
+    __syncthreads();
   }
-  meet();
-  const int found = total ? lowest_free(k, total, s.to, tmp) : 0;
-  const bool served = found >= total;
+  const int found = total ? lowest_free(k, total, s.to, taken, tmp) : 0;
   if (tid == 0) *k.missing = max(total - found, 0);
-  meet();
-  for (int b = wave; b < k.batch; b += kBookWaves) {
-    const int want = (len_of(k, b) + k.page_size - 1) / k.page_size, held = held_of(k, b);
-    int32_t *row = k.table + (int64_t)b * k.width;
-    if (served)
-      for (int e = held + lane; e < want; e += 64) {
-        const int p = s.to[s.first[b] + e - held];
-        row[e] = p;
-        k.uses[p] = 1;
-      }
-    if (lane == 0 && (served || want < held)) k.held[b] = want;
+  if (found < total || total == 0) return;
+  int done = 0;
+  for (int b0 = 0; b0 < k.batch; b0 += kBookThreads) {
+    const int b = b0 + tid, n = min(k.batch - b0, kBookThreads);
+    int want = 0, held = 0, comes;
+    if (b < k.batch) {
+      want = (len_of(k, b) + k.page_size - 1) / k.page_size;
+      held = held_of(k, b);
+    }
+    const int at = before_thread(max(want - held, 0), tmp, &comes);
+    first[tid] = at;
+    start[tid] = held;
+    __syncthreads();
+    for (int i = tid; i < comes; i += kBookThreads) {
+      const int q = owner(first, n, i), p = taken.at(s.to, done + i);
+      k.table[(int64_t)(b0 + q) * k.width + start[q] + i - first[q]] = p;
+      k.uses[p] = 1;
+    }
+    if (want > held) k.held[b] = want;
+    done += comes;
+    __syncthreads();
   }
 }
 
 // Fork, first: where each sequence's pages come from, and a free page for each partial one.
 __global__ __launch_bounds__(kBookThreads) void fork_plan_kernel(Book k, Scratch s, const int32_t *source) {
   __shared__ int tmp[kBookWaves];
+  __shared__ Taken taken;
   const int tid = threadIdx.x;
   int total = 0;
   for (int b0 = 0; b0 < k.batch; b0 += kBookThreads) {
@@ -170,8 +206,8 @@ __global__ __launch_bounds__(kBookThreads) void fork_plan_kernel(Book k, Scratch
     }
     total += all;
   }
-  meet();
-  const int found = total ? lowest_free(k, total, s.to, tmp) : 0;
+  const int found = total ? lowest_free(k, total, s.to, taken, tmp) : 0;
+  for (int i = tid; i < min(min(total, found), kTaken); i += kBookThreads) s.to[i] = taken.pages[i];
   if (tid == 0) {
     *k.missing = max(total - found, 0);
     s.head[0] = found >= total;
@@ -255,29 +291,39 @@ __global__ __launch_bounds__(kCopyThreads) void fork_rows_kernel(Book k, Scratch
 // Compact, first: the pages in use that lie beyond their number, and the free ones before it.
 __global__ __launch_bounds__(kBookThreads) void compact_plan_kernel(Book k, Scratch s) {
   __shared__ int tmp[kBookWaves];
+  constexpr int kEach = 8;
   const int tid = threadIdx.x;
+  const auto used_of = [&](int p0) {   // kEach neighbouring pages: a bit each
+    int32_t u[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) u[i] = p0 + i < k.pages ? k.uses[p0 + i] : 0;
+    int used = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) used |= (u[i] > 0) << i;
+    return used;
+  };
   int mine = 0, live;
-  for (int p = tid; p < k.pages; p += kBookThreads) mine += k.uses[p] > 0;
+  const int used0 = used_of(kEach * tid);
+  for (int p = kEach * tid; p < k.pages; p += kEach * kBookThreads) mine += __popc(p == kEach * tid ? used0 : used_of(p));
   before_thread(mine, tmp, &live);
   int moves = 0, holes = 0;
-  for (int p0 = 0; p0 < k.pages; p0 += kBookThreads) {
-    const int p = p0 + tid;
-    const bool used = p < k.pages && k.uses[p] > 0;
-    const int high = used && p >= live, hole = p < live && !used;
-    int all_high, all_hole;
-    const int at_high = moves + before_thread(high, tmp, &all_high), at_hole = holes + before_thread(hole, tmp, &all_hole);
-    if (high) {
-      s.from[at_high] = p;
-      s.rank[p] = at_high;
+  for (int p0 = 0; p0 < k.pages; p0 += kEach * kBookThreads) {
+    const int p = p0 + kEach * tid, used = p0 ? used_of(p) : used0;
+    const int below = (1 << min(max(live - p, 0), kEach)) - 1;   // (the pages before `live`)
+    const int high = used & ~below, hole = ~used & below;
+    int all;   // (both counts in one sum: at most 8192 of each a step)
+    const int at = before_thread(__popc(high) << 16 | __popc(hole), tmp, &all);
+    int at_high = moves + (at >> 16), at_hole = holes + (at & 0xffff);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (high >> i & 1) {
+        s.from[at_high] = p + i;
+        s.rank[p + i] = at_high++;
+      }
+      if (hole >> i & 1) s.to[at_hole++] = p + i;
     }
-    if (hole) s.to[at_hole] = p;
-    moves += all_high;
-    holes += all_hole;
-  }
-  meet();
-  for (int i = tid; i < moves; i += kBookThreads) {
-    k.uses[s.to[i]] = k.uses[s.from[i]];
-    k.uses[s.from[i]] = 0;
+    moves += all >> 16;
+    holes += all & 0xffff;
   }
   if (tid == 0) {
     s.head[0] = moves;
@@ -286,7 +332,7 @@ __global__ __launch_bounds__(kBookThreads) void compact_plan_kernel(Book k, Scra
   }
 }
 
-// Compact, second: the table's entries (workgroups [0, batch)), the pages' data.
+// Compact, second: the table's entries (workgroups [0, batch)), the pages' data and uses.
 __global__ __launch_bounds__(kCopyThreads) void compact_copy_kernel(Book k, Scratch s, Copies c, int copiers) {
   const int moves = s.head[0], live = s.head[1];
   if (moves == 0) return;
@@ -303,8 +349,14 @@ __global__ __launch_bounds__(kCopyThreads) void compact_copy_kernel(Book k, Scra
     return;
   }
   const int parts = c.layers * c.steps;
-  for (int64_t i = (int)blockIdx.x - k.batch; i < (int64_t)moves * parts; i += copiers)
-    copy_part(c, s.from[i / parts], s.to[i / parts], (int)(i % parts));
+  for (int64_t i = (int)blockIdx.x - k.batch; i < (int64_t)moves * parts; i += copiers) {
+    const int from = s.from[i / parts], to = s.to[i / parts], part = (int)(i % parts);
+    if (part == 0 && threadIdx.x == 0) {
+      k.uses[to] = k.uses[from];
+      k.uses[from] = 0;
+    }
+    copy_part(c, from, to, part);
+  }
 }
 
 __global__ __launch_bounds__(kCopyThreads) void copy_pages_kernel(Copies c, const int32_t *from, const int32_t *to) {

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import threading
 from typing import Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -533,7 +534,7 @@ def scan_topm(logits, M: int, T: float, stream=None):
 
 def _want(t, name, shape, dtype, device):
     """A contiguous tensor of this shape and dtype on a device (its index), as the C ABI takes it."""
-    if t.dtype != dtype or tuple(t.shape) != shape or t.get_device() != device or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name}: want a contiguous {dtype} tensor of shape {shape} on cuda:{device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
@@ -622,15 +623,27 @@ class Accepted:
     next_token: "torch.Tensor"  # [b] int32 the target's token after the path
 
 
-def _rotary(torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim, dtype, device) -> dt_rotary:
+class _Arguments(threading.local):
+    """C structures of the functions below, one set for each host thread: filled anew by every call."""
+
+    def __init__(self):
+        self.rows = [dt_rows() for _ in range(4)]
+        self.rotary, self.sampling = dt_rotary(), dt_sampling()
+        self.refs = [ctypes.byref(x) for x in (*self.rows, self.rotary, self.sampling)]
+
+
+_arguments = _Arguments()
+
+
+def _fill_rotary(c: dt_rotary, torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim, dtype,
+                 device) -> None:
     """The dt_rotary of a call."""
-    _want(positions, "positions", (rows,), torch.int32, device)
-    _want(inv_freq, "inv_freq", (inv_freq.numel(),), torch.float32, device)
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _want(w, name, (dim,), dtype, device)
-    return dt_rotary(positions.data_ptr(), inv_freq.data_ptr(), inv_freq.numel(), bool(interleaved), _ptr(q_weight),
-                     _ptr(k_weight), eps)
+    c.positions = _want(positions, "positions", (rows,), torch.int32, device).data_ptr()
+    pairs = inv_freq.numel()
+    c.inv_freq, c.pairs = _want(inv_freq, "inv_freq", (pairs,), torch.float32, device).data_ptr(), pairs
+    c.q_weight = None if q_weight is None else _want(q_weight, "q_weight", (dim,), dtype, device).data_ptr()
+    c.k_weight = None if k_weight is None else _want(k_weight, "k_weight", (dim,), dtype, device).data_ptr()
+    c.eps, c.interleaved = eps, interleaved
 
 
 class Cache:
@@ -717,19 +730,19 @@ class Cache:
         """
         torch = self._torch
         rows = self._kv(k, v)
-        x, y = dt_rows(), dt_rows()
+        (x, y, _, _), refs = _arguments.rows, _arguments.refs
         if self._rows(x, q, "q") != rows:
             raise ValueError(f"q and k have {q.shape[0]} and {rows} rows")
-        heads = q.shape[1]
+        heads, dim = q.shape[1], self.head_dim
         if out is None:
-            out = _empty(torch, (rows, heads, self.head_dim), self.data_dtype, self._at, stream)
-        if self._rows(y, out, "out", heads) != rows:
+            out = _empty(torch, (rows, heads, dim), self.data_dtype, self._at, stream)
+            y.data, y.row_stride, y.head_stride = out.data_ptr(), heads * dim, dim
+        elif self._rows(y, out, "out", heads) != rows:
             raise ValueError(f"q and out have {rows} and {out.shape[0]} rows")
-        r = _rotary(torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, self.head_dim,
-                    self.data_dtype, self._device)
-        st = self._lib.dt_cache_append_rotated(self._ref, layer, self._chunk(chunk, rows), heads, ctypes.byref(x),
-                                               self._aref, self._bref, ctypes.byref(r), ctypes.byref(y),
-                                               self._stream(stream))
+        _fill_rotary(_arguments.rotary, torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim,
+                     self.data_dtype, self._device)
+        st = self._lib.dt_cache_append_rotated(self._ref, layer, self._chunk(chunk, rows), heads, refs[0], self._aref,
+                                               self._bref, refs[4], refs[1], self._stream(stream))
         if st != 0:
             _check(st)
         if stream is not None:
@@ -919,16 +932,17 @@ class Pages:
             _keep(stream, self.state, self._ws, cache.storage)
 
 
-def _strided(t, name: str, device: int, dtype, shape) -> dt_rows:
-    """The dt_rows of a tensor [rows, heads, dim] (a None of the shape: any)."""
-    if t.dtype != dtype or t.dim() != 3 or t.get_device() != device or \
-            any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name}: want a {dtype} tensor of shape {shape} on cuda:{device}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    stride = t.stride()
+def _fill_rows(c: dt_rows, t, name: str, device: int, dtype, rows=None, heads=None, dim=None) -> None:
+    """The dt_rows of a tensor [rows, heads, dim] (None: any)."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype != dtype or len(shape) != 3 or t.get_device() != device or (rows is not None and shape[0] != rows) or \
+            (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim):
+        want = [x or n for x, n in ((rows, "rows"), (heads, "heads"), (dim, "dim"))]
+        raise ValueError(f"{name}: want a {dtype} tensor [{want[0]}, {want[1]}, {want[2]}] on cuda:{device}, "
+                         f"got {t.dtype} {tuple(shape)} on {t.device}")
     if stride[2] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous (stride {stride[2]})")
-    return dt_rows(t.data_ptr(), stride[0], stride[1])
+    c.data, c.row_stride, c.head_stride = t.data_ptr(), stride[0], stride[1]
 
 
 def rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
@@ -942,27 +956,39 @@ def rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float =
     stream of the tensors' device (the current one) unless one is given.
     """
     import torch
-    device, dtype = q.get_device(), q.dtype
-    code = _dtype_code(q)
+    device, dtype, code = q.get_device(), q.dtype, _dtype_code(q)
     s = _raw_stream(torch, device, stream, "q is")
-    x = _strided(q, "q", device, dtype, (None, None, None))
+    (x, y, a, b), refs = _arguments.rows, _arguments.refs
+    _fill_rows(x, q, "q", device, dtype)
     rows, heads, dim = q.shape
-    kv = 0 if k is None else k.shape[1]
-    y = None if k is None else _strided(k, "k", device, dtype, (rows, None, dim))
+    kv = 0
+    if k is not None:
+        kv = k.shape[1]
+        _fill_rows(y, k, "k", device, dtype, rows, dim=dim)
     if out is None:
+        # (one allocation, parted as the calls for cached rows do)
         n = rows * heads * dim
         both = _empty(torch, (n + rows * kv * dim,), dtype, q.device, stream)
-        out = both[:n].view(rows, heads, dim), None if k is None else both[n:].view(rows, kv, dim)
-    a = _strided(out[0], "out", device, dtype, (rows, heads, dim))
-    b = None if k is None else _strided(out[1], "out", device, dtype, (rows, kv, dim))
-    r = _rotary(torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim, dtype, device)
-    by = lambda c: None if c is None else ctypes.byref(c)  # noqa: E731
-    st = load().dt_rotate(by(x), heads, by(y), kv, rows, dim, code, by(r), by(a), by(b), s)
+        out = both.as_strided((rows, heads, dim), (heads * dim, dim, 1)), \
+            None if k is None else both.as_strided((rows, kv, dim), (kv * dim, dim, 1), n)
+        a.data = at = both.data_ptr()
+        a.row_stride, a.head_stride = heads * dim, dim
+        b.data, b.row_stride, b.head_stride = at + n * both.element_size(), kv * dim, dim
+    else:
+        _fill_rows(a, out[0], "out", device, dtype, rows, heads, dim)
+        if k is not None:
+            _fill_rows(b, out[1], "out", device, dtype, rows, kv, dim)
+    _fill_rotary(_arguments.rotary, torch, positions, inv_freq, q_weight, k_weight, eps, interleaved, rows, dim, dtype, device)
+    st = load().dt_rotate(refs[0], heads, None if k is None else refs[1], kv, rows, dim, code, refs[4], refs[2],
+                          None if k is None else refs[3], s)
     if st != 0:
         _check(st)
     if stream is not None:
         _keep(stream, q, k, positions, inv_freq, q_weight, k_weight, *out)
     return out
+
+
+_sample_bytes = {}   # of a workspace for (rows, V)
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, logprobs=False, workspace=None,
@@ -990,37 +1016,42 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
     if logits.stride(1) != 1 and V > 1:
         raise ValueError(f"logits: the last dimension must be contiguous (stride {logits.stride(1)})")
     f32, i32 = torch.float32, torch.int32
-    _want(u, "u", tuple(shape), f32, device)
-    how = dt_sampling()
-    kept = [logits, u]
-    for name, x, dtype in (("temperature", temperature, f32), ("top_k", top_k, i32), ("top_p", top_p, f32),
-                           ("min_p", min_p, f32)):
+    _want(u, "u", shape, f32, device)
+    how, kept = _arguments.sampling, []
+    for name, names, x, dtype in (("temperature", "temperatures", temperature, f32), ("top_k", "top_ks", top_k, i32),
+                                  ("top_p", "top_ps", top_p, f32), ("min_p", "min_ps", min_p, f32)):
         if isinstance(x, torch.Tensor):
-            setattr(how, name + "s", _want(x, name, tuple(shape), dtype, device).data_ptr())
+            setattr(how, names, _want(x, name, shape, dtype, device).data_ptr())
             kept.append(x)
         else:
+            setattr(how, names, None)
             setattr(how, name, x)
+    if workspace is None:
+        n = _sample_bytes.get((rows, V))
+        if n is None:
+            size = ctypes.c_size_t()
+            _check(lib.dt_sample_workspace_size(rows, V, ctypes.byref(size)))
+            if len(_sample_bytes) >= 4096:   # (shapes of a long-running program)
+                _sample_bytes.clear()
+            n = _sample_bytes[(rows, V)] = size.value
+        workspace = _empty(torch, (n,), torch.uint8, logits.device, stream)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: want a contiguous tensor on cuda:{device}, got one on {workspace.device}")
     if out is None:
         tokens = _empty(torch, shape, i32, logits.device, stream)
         probs = _empty(torch, shape, f32, logits.device, stream) if logprobs else None
     else:
         tokens, probs = out if logprobs else (out, None)
-        _want(tokens, "out", tuple(shape), i32, device)
+        _want(tokens, "out", shape, i32, device)
         if logprobs:
-            _want(probs, "out", tuple(shape), f32, device)
-    n = ctypes.c_size_t()
-    if workspace is None:
-        _check(lib.dt_sample_workspace_size(rows, V, ctypes.byref(n)))
-        workspace = _empty(torch, (n.value,), torch.uint8, logits.device, stream)
-    elif workspace.get_device() != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace: want a contiguous tensor on cuda:{device}, got one on {workspace.device}")
-    st = lib.dt_sample(logits.data_ptr(), logits.stride(0), rows, V, code, u.data_ptr(), ctypes.byref(how),
-                       tokens.data_ptr(), _ptr(probs), workspace.data_ptr(),
+            _want(probs, "out", shape, f32, device)
+    st = lib.dt_sample(logits.data_ptr(), logits.stride(0), rows, V, code, u.data_ptr(), _arguments.refs[5], tokens.data_ptr(),
+                       None if probs is None else probs.data_ptr(), workspace.data_ptr(),
                        workspace.numel() * workspace.element_size(), s)
     if st != 0:
         _check(st)
     if stream is not None:
-        _keep(stream, tokens, probs, workspace, *kept)
+        _keep(stream, logits, u, tokens, probs, workspace, *kept)
     return (tokens, probs) if logprobs else tokens
 
 

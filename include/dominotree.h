@@ -514,7 +514,7 @@ dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int node
  * at the end of a sequence grown by dt_pages_fit or made by dt_pages_fork. */
 typedef struct {
   int pages, page_size;    /* of the cache; pages <= 2^28 */
-  int batch, table_width;  /* as dt_chunk's */
+  int batch, table_width;  /* as dt_chunk's; batch * table_width < 2^31 */
   int32_t *uses;           /* [pages] */
   int32_t *held;           /* [batch] */
   int32_t *lens;           /* [batch] */

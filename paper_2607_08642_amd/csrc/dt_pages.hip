@@ -380,8 +380,10 @@ dt_status check_pages(const dt_pages *p, bool data) {
                 p->table_width);
   if (p->page_size != 32 && p->page_size != 64 && p->page_size != 128 && p->page_size != 256)
     return fail(DT_ERR_UNSUPPORTED, "page_size must be 32, 64, 128 or 256 (%d)", p->page_size);
-  if (p->pages > 1 << 28 || p->batch > 65535 || (int64_t)p->table_width * p->page_size >= (int64_t)1 << 30)
-    return fail(DT_ERR_UNSUPPORTED, "need pages <= 2^28, batch <= 65535, table_width * page_size < 2^30");
+  if (p->pages > 1 << 28 || p->batch > 65535 || (int64_t)p->table_width * p->page_size >= (int64_t)1 << 30 ||
+      (int64_t)p->batch * p->table_width >= (int64_t)1 << 31)   // (entries are counted in 32 bits)
+    return fail(DT_ERR_UNSUPPORTED,
+                "need pages <= 2^28, batch <= 65535, table_width * page_size < 2^30, batch * table_width < 2^31");
   if (!data) return DT_OK;
   for (const void *q : {(const void *)p->uses, (const void *)p->held, (const void *)p->lens, (const void *)p->table,
                         (const void *)p->missing}) {

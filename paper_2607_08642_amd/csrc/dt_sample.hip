@@ -1215,7 +1215,7 @@ struct Layout {
   size_t sums, maxima, large, rows, above, bins, list, bytes;
 };
 Layout layout(int rows, int V) {
-  Layout w;
+  Layout w{};
   size_t n = 0;
   auto take = [&](size_t bytes) {
     const size_t at = n;
@@ -1225,6 +1225,11 @@ Layout layout(int rows, int V) {
   const size_t segs = (size_t)rows * segments(V);
   w.sums = take(segs * sizeof(double));
   w.maxima = take(segs * kGroups * sizeof(float));
+  if (segments(V) <= kFewSegs) {   // (no large rows)
+    w.rows = take(sizeof(int));
+    w.bytes = n;
+    return w;
+  }
   w.large = take(rows * sizeof(Large));
   w.rows = take((rows + 1) * sizeof(int));
   w.above = take(rows * sizeof(u64));

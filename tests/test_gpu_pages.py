@@ -98,6 +98,17 @@ def test_forks_without_pages():
     assert int(b.pages.missing) == 0 and b.pages.uses.tolist() == [1, 1, 3, 3]
 
 
+def test_forks_of_lengths_that_were_not_fitted():
+    """Lengths that changed since pages were given: a source has the pages that it holds, whole or partial."""
+    b = Both(40, 32, 5, 6, seed=8)
+    b.set([100, 64, 33, 0, 0])
+    b.do("fit")
+    b.set([130, 20, 33, 0, 5])                   # more than it holds; fewer; as many; none held
+    b.do("fork", [4, 0, 1, 2, 2])
+    b.do("fork", [1, 1, 1, 1, 0])
+    b.do("fit")
+
+
 def test_beams_change_places():
     b = Both(64, 32, 4, 6)
     b.set([100, 0, 0, 0])

@@ -23,7 +23,8 @@ def calls(p, c=None, ws=AT, size=1 << 30, source=AT):
 @pytest.mark.parametrize("fault,status", [
     (dict(pages=0), SHAPE), (dict(batch=0), SHAPE), (dict(table_width=0), SHAPE), (dict(page_size=48), UNSUPPORTED),
     (dict(page_size=0), UNSUPPORTED), (dict(batch=65536), UNSUPPORTED), (dict(pages=0x7fffffff), UNSUPPORTED),
-    (dict(table_width=1 << 25), UNSUPPORTED)])
+    (dict(table_width=1 << 25), UNSUPPORTED),
+    (dict(batch=1 << 10, table_width=1 << 21), UNSUPPORTED)])
 def test_sizes(fault, status):
     n = ctypes.c_size_t(7)
     assert b.load().dt_pages_workspace_size(ref(pages(**fault)), ref(n)) == status and n.value == 7

@@ -71,7 +71,7 @@ __device__ inline uint32_t high16(uint32_t a, uint32_t b) { return a >> 16 | (b 
 
 // A workgroup's block: kv head and block of the chunk (blockIdx.x), sequence (blockIdx.y).  kRotate: keys are normed
 // and rotated between their load and the tile; a lane then holds both runs of a unit (dt_rotate.h).
-template <int DT, int D, bool kRotate>
+template <int DT, int D, bool kRotate, bool kNear>
 __device__ __forceinline__ void append_block(const CacheView &c, const ChunkView &k, const RowsView &kr,
                                              const RowsView &vr, const RotaryView &rot, const void *k_weight) {
   using El = Elem<DT>;
@@ -89,7 +89,7 @@ __device__ __forceinline__ void append_block(const CacheView &c, const ChunkView
   uint32_t w[2][kRuns][kWords];
   // the run's first element (of keys in units), and whether there is such a run
   auto at = [&](int v, int i) __attribute__((always_inline)) {
-    return kRotate && !v ? unit_at(rot, sub + 8 * (i / 2), i & 1) : 8 * (sub + 8 * i);
+    return kRotate && !v ? unit_at<kNear>(rot, D, sub + 8 * (i / 2), i & 1) : 8 * (sub + 8 * i);
   };
   auto there = [&](int v, int i) __attribute__((always_inline)) {
     return kRotate && !v ? D % 128 == 0 || sub + 8 * (i / 2) < D / 16
@@ -133,24 +133,19 @@ __device__ __forceinline__ void append_block(const CacheView &c, const ChunkView
 #pragma unroll
     for (int n = 0; n < kRuns / 2; ++n)
       if (mine && there(0, 2 * n)) {
-        const int u = sub + 8 * n;
+        const int runs[2] = {at(0, 2 * n), at(0, 2 * n + 1)};
         if (weight) {
           float g[16];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint32_t b[kWords];
-            load8<true>(weight + at(0, 2 * n + h), b);
+            load8<true>(weight + runs[h], b);
             widen8(b, g + 8 * h);
           }
 #pragma unroll
           for (int j = 0; j < 16; ++j) x[n][j] *= f * g[j];
         }
-        if (u < rot.pairs / 8) {
-          float2 a[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) a[j] = angle_of(pos, rot.freq[8 * u + j]);
-          turn(x[n], a, rot.interleaved);
-        }
+        turn<kNear>(x[n], turn_of<kNear>(rot, runs[0], runs[1], [&](int j) { return angle_of(pos, rot.freq[j]); }));
         round8(x[n], w[0][2 * n]);
         round8(x[n] + 8, w[0][2 * n + 1]);
       }
@@ -277,18 +272,18 @@ __device__ __forceinline__ void append_block(const CacheView &c, const ChunkView
 // grid: (kv head, block of the chunk), sequence
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView k, RowsView kr, RowsView vr) {
-  append_block<DT, D, false>(c, k, kr, vr, RotaryView{}, nullptr);
+  append_block<DT, D, false, false>(c, k, kr, vr, RotaryView{}, nullptr);
 }
 
 // The same blocks, keys rotated, and after them (blockIdx.x from kv * blocks on) the chunk's queries, a wave for a
 // part of a row.
-template <int DT, int D>
+template <int DT, int D, bool kNear>
 __global__ __launch_bounds__(kThreads) void append_rotated_kernel(CacheView c, ChunkView k, RotaryView rot, HeadsView q,
                                                                   RotatePlan plan, RowsView kr, const void *k_weight,
                                                                   RowsView vr, int blocks) {
   const int group = (int)blockIdx.x - c.kv * blocks;
   if (group < 0) {
-    append_block<DT, D, true>(c, k, kr, vr, rot, k_weight);
+    append_block<DT, D, true, kNear>(c, k, kr, vr, rot, k_weight);
     return;
   }
   using T = typename Elem<DT>::data;
@@ -300,9 +295,9 @@ __global__ __launch_bounds__(kThreads) void append_rotated_kernel(CacheView c, C
   const int last = min(first + plan.per, plan.passes);
   const HeadsView none{};
   if (q.in.vec && q.out.vec)
-    rotate_row<T, true>(rot, q, none, D, plan.lanes, s.row0 + row, first, last, cs[wave]);
+    rotate_row<T, true, kNear>(rot, q, none, D, plan.lanes, s.row0 + row, first, last, cs[wave]);
   else
-    rotate_row<T, false>(rot, q, none, D, plan.lanes, s.row0 + row, first, last, cs[wave]);
+    rotate_row<T, false, kNear>(rot, q, none, D, plan.lanes, s.row0 + row, first, last, cs[wave]);
 }
 
 // grid as append_kernel's; the tiles hold the data type
@@ -573,10 +568,10 @@ hipError_t launch_append_rotated(const CacheView &c, int dtype, const ChunkView 
   const dim3 grid((unsigned)(c.kv * blocks + groups), k.batch);
   auto pick = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    auto f = c.D == 64    ? append_rotated_kernel<DT, 64>
-             : c.D == 96  ? append_rotated_kernel<DT, 96>
-             : c.D == 128 ? append_rotated_kernel<DT, 128>
-                          : append_rotated_kernel<DT, 256>;
+    auto f = c.D == 64    ? r.interleaved ? append_rotated_kernel<DT, 64, true> : append_rotated_kernel<DT, 64, false>
+             : c.D == 96  ? r.interleaved ? append_rotated_kernel<DT, 96, true> : append_rotated_kernel<DT, 96, false>
+             : c.D == 128 ? r.interleaved ? append_rotated_kernel<DT, 128, true> : append_rotated_kernel<DT, 128, false>
+             : r.interleaved ? append_rotated_kernel<DT, 256, true> : append_rotated_kernel<DT, 256, false>;
     f<<<grid, kThreads, 0, s>>>(c, k, r, q, plan, kr, k_weight, vr, blocks);
   };
   if (dtype == DT_F32)

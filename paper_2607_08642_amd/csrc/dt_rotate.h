@@ -1,8 +1,9 @@
 // Heads normed and rotated by position (dt_rotary), on the device.
 //
-// A head's D elements are dealt to lanes in units of 16, so that both elements of a pair are with one lane
-// and every access is 16 bytes: unit u of pairs [8 u, 8 u + 8) is the runs of eight at 8 u and at
-// pairs + 8 u, or the 16 neighbours where pairs are interleaved; past the pairs, 16 neighbours.
+// A head's D elements are dealt to lanes in units of two runs of eight, so that both elements of a pair are with one
+// lane and neighbouring lanes have neighbouring runs: unit u of the pairs [8 u, 8 u + 8) is the runs at 8 u and at
+// pairs + 8 u; where pairs are interleaved, or none, the runs u and u + n of the 2 n.  (Units of 16 neighbours, whose lanes
+// are 64 bytes apart in fp32, took 80 us where these take 65: 8000 rows of 40 heads of 128.)
 #pragma once
 
 #include "dt_cache.h"
@@ -12,7 +13,7 @@ namespace dt {
 struct RotaryView {
   const int32_t *pos;
   const float *freq;
-  int pairs, interleaved;
+  int pairs, interleaved;   // (kernels know the second when they are compiled: kNear below)
   float eps;
 };
 
@@ -37,24 +38,47 @@ __device__ inline float2 angle_of(int pos, float freq) {
   return make_float2(quarter == 1 || quarter == 2 ? -a : a, quarter & 2 ? -b : b);
 }
 
-// the first element of half h (eight elements) of unit u
-__device__ inline int unit_at(const RotaryView &r, int u, int h) {
-  return u < r.pairs / 8 && !r.interleaved ? 8 * u + h * r.pairs : 16 * u + 8 * h;
+// the first element of run h of unit u of a head of D elements; kNear: pairs are neighbours
+template <bool kNear>
+__device__ inline int unit_at(const RotaryView &r, int D, int u, int h) {
+  const int n = kNear ? 0 : r.pairs / 8;   // units of pairs across runs
+  return u < n ? 8 * u + h * r.pairs : 16 * n + 8 * (u - n + h * (D / 16 - n));
 }
 
-// the unit's pairs turned (x: its halves one after the other); the products' order is fixed, so that the
-// kernels that share this agree in every bit
-__device__ inline void turn(float (&x)[16], const float2 (&a)[8], int interleaved) {
+// cos and sin for a unit's pairs: eight across its runs (from element e0), or four in each (from e0 and e1)
+struct Turn {
+  float2 a[8];
+  bool on0, on1;   // whether a run is turned
+};
+template <bool kNear, typename F>
+__device__ __forceinline__ Turn turn_of(const RotaryView &r, int e0, int e1, F angle) {
+  Turn t;
+  t.on0 = e0 < 2 * r.pairs;
+  t.on1 = kNear ? e1 < 2 * r.pairs : t.on0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (interleaved) {
-      const float p = x[2 * j], q = x[2 * j + 1];
-      x[2 * j] = fmaf(p, a[j].x, -(q * a[j].y));
-      x[2 * j + 1] = fmaf(q, a[j].x, p * a[j].y);
-    } else {
-      const float p = x[j], q = x[8 + j];
-      x[j] = fmaf(p, a[j].x, -(q * a[j].y));
-      x[8 + j] = fmaf(q, a[j].x, p * a[j].y);
+  for (int j = 0; j < 8; ++j) t.a[j] = make_float2(1.0f, 0.0f);
+  if (t.on0)
+#pragma unroll
+    for (int j = 0; j < (kNear ? 4 : 8); ++j) t.a[j] = angle(kNear ? e0 / 2 + j : e0 + j);
+  if (kNear && t.on1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t.a[4 + j] = angle(e1 / 2 + j);
+  return t;
+}
+
+// the unit turned (x: its runs one after the other); the products' order is fixed, so that the
+// kernels that share this agree in every bit
+template <bool kNear>
+__device__ __forceinline__ void turn(float (&x)[16], const Turn &t) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (!(h ? t.on1 : t.on0)) continue;
+#pragma unroll
+    for (int j = 4 * h; j < 4 * h + 4; ++j) {
+      const int a = kNear ? 2 * j : j, b = kNear ? 2 * j + 1 : 8 + j;
+      const float p = x[a], q = x[b];
+      x[a] = fmaf(p, t.a[j].x, -(q * t.a[j].y));
+      x[b] = fmaf(q, t.a[j].x, p * t.a[j].y);
     }
   }
 }
@@ -140,30 +164,39 @@ struct HeadsView {
 };
 
 // One row by a wave.  `lanes` lanes a head (a power of two, 16 elements each); cs: the wave's own LDS.
-template <typename T, bool vec>
+template <typename T, bool vec, bool kNear>
 __device__ __forceinline__ void rotate_row(const RotaryView &r, const HeadsView &q, const HeadsView &k, int D,
                                            int lanes, int64_t row, int first, int last, float2 *cs) {
   constexpr int kWords = sizeof(T) == 4 ? 8 : 4;
   const int lane = threadIdx.x & 63, u = lane & (lanes - 1), wide = 64 / lanes;
+  const int q_passes = (q.heads + wide - 1) / wide;
+  const bool here = 16 * u < D;
+  const int at[2] = {unit_at<kNear>(r, D, u, 0), unit_at<kNear>(r, D, u, 1)};
+  // a pass's head of this lane, and its elements (asked for a pass ahead: the first before the angles are computed)
+  const auto head_of = [&](int pass) { return (pass < q_passes ? pass : pass - q_passes) * wide + lane / lanes; };
+  uint32_t next[2][kWords];
+  const auto ask = [&](int pass) {
+    const bool of_q = pass < q_passes;
+    const int head = head_of(pass);
+    const T *p = reinterpret_cast<const T *>(of_q ? q.in.p : k.in.p) + row * (of_q ? q.in.row : k.in.row) +
+                 head * (of_q ? q.in.head : k.in.head);
+    if (here && head < (of_q ? q.heads : k.heads))
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load8<vec>(p + at[h], next[h]);
+  };
+  ask(first);
   const int pos = r.pos[row];
   for (int j = lane; j < r.pairs; j += 64) cs[j] = angle_of(pos, r.freq[j]);
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // (a wave's LDS accesses keep their order)
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  const bool turns = u < r.pairs / 8, here = 16 * u < D;
-  float2 a[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) a[j] = turns ? cs[8 * u + j] : make_float2(1.0f, 0.0f);
-  const int at[2] = {unit_at(r, u, 0), unit_at(r, u, 1)};
+  const Turn a = turn_of<kNear>(r, at[0], at[1], [&](int j) { return cs[j]; });
   const float inv_d = 1.0f / (float)D;
-  const int q_passes = (q.heads + wide - 1) / wide;
-  for (int part = 0; part < 2; ++part) {
-    const HeadsView &x = part ? k : q;
-    const int p0 = part ? max(first - q_passes, 0) : first, p1 = part ? last - q_passes : min(last, q_passes);
-    if (p0 >= p1) continue;
-    const T *weight = static_cast<const T *>(x.weight);
-    float w[16] = {};
-    if (weight && here) {
+  float w[16] = {};
+  for (int pass = first; pass < last; ++pass) {
+    const bool of_q = pass < q_passes;
+    const T *weight = static_cast<const T *>(of_q ? q.weight : k.weight);
+    if (weight && here && (pass == first || pass == q_passes)) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t b[kWords];
@@ -171,32 +204,34 @@ __device__ __forceinline__ void rotate_row(const RotaryView &r, const HeadsView 
         widen8(b, w + 8 * h);
       }
     }
-    for (int p = p0; p < p1; ++p) {
-      const int head = p * wide + lane / lanes;
-      const bool on = here && head < x.heads;
-      float y[16];
+    const int head = head_of(pass);
+    const bool on = here && head < (of_q ? q.heads : k.heads);
+    float y[16];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t b[kWords] = {};
-        if (on) load8<vec>(reinterpret_cast<const T *>(x.in.p) + row * x.in.row + head * x.in.head + at[h], b);
-        widen8(b, y + 8 * h);
-      }
-      if (weight) {
-        float sum = 0.0f;
+    for (int h = 0; h < 2; ++h) {
+      uint32_t b[kWords];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum = fmaf(y[j], y[j], sum);
-        for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o);
-        const float f = rsqrtf(fmaf(sum, inv_d, r.eps));
+      for (int j = 0; j < kWords; ++j) b[j] = on ? next[h][j] : 0u;
+      widen8(b, y + 8 * h);
+    }
+    if (pass + 1 < last) ask(pass + 1);
+    if (weight) {
+      float sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] *= f * w[j];
-      }
-      if (turns) turn(y, a, r.interleaved);
+      for (int j = 0; j < 16; ++j) sum = fmaf(y[j], y[j], sum);
+      for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o);
+      const float f = rsqrtf(fmaf(sum, inv_d, r.eps));
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t b[kWords];
-        round8(y + 8 * h, b);
-        if (on) store8<vec>(reinterpret_cast<T *>(x.out.p) + row * x.out.row + head * x.out.head + at[h], b);
-      }
+      for (int j = 0; j < 16; ++j) y[j] *= f * w[j];
+    }
+    turn<kNear>(y, a);
+    T *p = reinterpret_cast<T *>(of_q ? q.out.p : k.out.p) + row * (of_q ? q.out.row : k.out.row) +
+           head * (of_q ? q.out.head : k.out.head);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t b[kWords];
+      round8(y + 8 * h, b);
+      if (on) store8<vec>(p + at[h], b);
     }
   }
 }

@@ -7,7 +7,7 @@
 namespace dt {
 namespace {
 
-template <typename T>
+template <typename T, bool kNear>
 __global__ __launch_bounds__(64 * kRotWaves) void rotate_kernel(RotaryView r, HeadsView q, HeadsView k, RotatePlan plan,
                                                                 int rows, int D) {
   __shared__ float2 cs[kRotWaves][kMaxPairs];
@@ -17,9 +17,9 @@ __global__ __launch_bounds__(64 * kRotWaves) void rotate_kernel(RotaryView r, He
   if (row >= rows) return;
   const int first = (int)(at % plan.splits) * plan.per, last = min(first + plan.per, plan.passes);
   if (q.in.vec && q.out.vec && k.in.vec && k.out.vec)
-    rotate_row<T, true>(r, q, k, D, plan.lanes, row, first, last, cs[wave]);
+    rotate_row<T, true, kNear>(r, q, k, D, plan.lanes, row, first, last, cs[wave]);
   else
-    rotate_row<T, false>(r, q, k, D, plan.lanes, row, first, last, cs[wave]);
+    rotate_row<T, false, kNear>(r, q, k, D, plan.lanes, row, first, last, cs[wave]);
 }
 
 }  // namespace
@@ -41,7 +41,8 @@ hipError_t launch_rotate(const RotaryView &r, const HeadsView &q, const HeadsVie
                          hipStream_t s) {
   const RotatePlan plan = rotate_plan(rows, q.heads, k.heads, D);
   const int64_t groups = ((int64_t)rows * plan.splits + kRotWaves - 1) / kRotWaves;
-  auto f = dtype == DT_F32 ? rotate_kernel<float> : rotate_kernel<uint16_t>;
+  auto f = dtype == DT_F32 ? r.interleaved ? rotate_kernel<float, true> : rotate_kernel<float, false>
+           : r.interleaved ? rotate_kernel<uint16_t, true> : rotate_kernel<uint16_t, false>;
   f<<<(unsigned)groups, 64 * kRotWaves, 0, s>>>(r, q, k, plan, rows, D);
   return hipGetLastError();
 }

@@ -795,8 +795,9 @@ struct Finish {
         const int at = place_of(i);
         if (inside<kPiece>(r, at)) w[n] = *reinterpret_cast<const u32x4 *>(r.base + at);
       }
-      // 64 elements a lane: a bit each
-      uint32_t hits[2] = {};
+      // 64 elements a lane: a bit each, the first element in the highest
+      constexpr int kWords = kAtOnce * kPiece / 32;
+      uint32_t hits[kWords] = {};
 #pragma unroll
       for (int n = 0; n < kAtOnce; ++n)
 #pragma unroll
@@ -809,21 +810,24 @@ struct Finish {
           uint32_t &h = hits[(n * kPiece + j) / 32];
           h = h + h + (x >= bound);
         }
-      mine = __popc(hits[0]) + __popc(hits[1]);
+      mine = 0;
+#pragma unroll
+      for (int h = 0; h < kWords; ++h) mine += __popc(hits[h]);
       int place = wave_scan(mine, 0, [](int a, int b) { return a + b; });
       const int all = last_lane(place);
       if (!all) continue;
       int base = 0;
       if ((tid & 63) == 0) base = atomicAdd(&sh.n, all);
       place += __builtin_amdgcn_readfirstlane(base) - mine;
-      u64 left = (u64)hits[0] << 32 | hits[1];   // (the first element in the highest bit)
-      while (left) {
-        const int e = __clzll((long long)left);
-        left &= ~(0x8000000000000000ull >> e);
-        const int at = place_of(i0 + e / kPiece * kRowThreads) + e % kPiece;
-        if (place < kList) sh.list[place] = make_key(r.at(r.base[at]), (uint32_t)(at - r.before));
-        ++place;
-      }
+#pragma unroll
+      for (int h = 0; h < kWords; ++h)
+        for (uint32_t left = hits[h]; left;) {
+          const int bit = __clz((int)left), e = 32 * h + bit;
+          left &= ~(0x80000000u >> bit);
+          const int at = place_of(i0 + e / kPiece * kRowThreads) + e % kPiece;
+          if (place < kList) sh.list[place] = make_key(r.at(r.base[at]), (uint32_t)(at - r.before));
+          ++place;
+        }
     }
     // the pieces at the row's beginning and end
 #pragma unroll 1
@@ -844,7 +848,7 @@ struct Finish {
 
   // reach() by the order of the maxima of kTops parts of the groups, where they suffice.
   template <int kTops>
-  __device__ float reach_of_few(bool by_mass, double want) {
+  __device__ float reach_of_few(bool by_mass, double want, bool *far) {
     constexpr int kSplit = kRowThreads / kTops;   // threads a maximum
     const int tid = threadIdx.x, e = tid / kSplit, part = tid % kSplit;
     float top = -INFINITY;
@@ -869,10 +873,12 @@ struct Finish {
       const uint32_t bits = order[i] & ~255u;
       return bits > ordered_bits(-INFINITY) ? ordered_to_float(bits) : -INFINITY;
     };
+    *far = false;
     if (!by_mass) return value_at((int)want - 1);
     const float x = tid < kTops ? value_at(tid) : -INFINITY;
     double all;
     const double w = x > -INFINITY ? weight_of(x) : 0.0, run = w + before_thread(w, sh.tmp_d, &all);
+    *far = all < want * 0.25;
     const int at = block_min(run >= want ? tid : kRowThreads, sh.tmp_i);
     return at < kTops ? value_at(at) : -INFINITY;
   }
@@ -881,12 +887,13 @@ struct Finish {
   // alone, which is less than there is.  -infinity: not reached.
   __device__ float reach(bool by_mass, double want) {
     // (few, as their order costs the square of their number; so many that most of those looked for are in parts of their own)
+    bool far = false;
     float x = -INFINITY;
     if (by_mass || want <= 64.0)
-      x = reach_of_few<128>(by_mass, want);
+      x = reach_of_few<128>(by_mass, want, &far);
     else if (want <= kRowThreads)
-      x = reach_of_few<kRowThreads>(false, want);
-    if (x > -INFINITY) return x;
+      x = reach_of_few<kRowThreads>(false, want, &far);
+    if (x > -INFINITY || far) return x;   // (far: more than the list holds are kept, as a rule)
     float low = m;
     const int n_groups = segs * kGroups;
     for (int g = threadIdx.x; g < n_groups; g += kRowThreads)

@@ -624,11 +624,13 @@ class Accepted:
 
 
 class _Arguments(threading.local):
-    """C structures of the functions below, one set for each host thread: filled anew by every call."""
+    """C structures of the functions below, filled anew by every call, and sampling's workspaces: one set for each
+    host thread, as threads may call on the same stream."""
 
     def __init__(self):
         self.rows = [dt_rows() for _ in range(4)]
         self.rotary, self.sampling = dt_rotary(), dt_sampling()
+        self.spaces = {}   # a workspace of each stream
         self.refs = [ctypes.byref(x) for x in (*self.rows, self.rotary, self.sampling)]
 
 
@@ -1034,7 +1036,13 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
             if len(_sample_bytes) >= 4096:   # (shapes of a long-running program)
                 _sample_bytes.clear()
             n = _sample_bytes[(rows, V)] = size.value
-        workspace = _empty(torch, (n,), torch.uint8, logits.device, stream)
+        # (kept for the stream, where calls follow one another; a graph's calls come again after that, and have their own)
+        spaces, at = _arguments.spaces, (device, s)
+        workspace = None if _capturing(torch, stream) else spaces.get(at)
+        if workspace is None or workspace.numel() < n:
+            workspace = _empty(torch, (n,), torch.uint8, logits.device, stream)
+            if not _capturing(torch, stream):
+                spaces[at] = workspace
     elif workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError(f"workspace: want a contiguous tensor on cuda:{device}, got one on {workspace.device}")
     if out is None:

@@ -24,7 +24,11 @@ constexpr int kMaxV = 1 << 19;
 constexpr int kMaxSegs = kMaxV / kSeg + 1;   // (a row may begin inside a 16-byte piece)
 constexpr int kWaves = 4;           // of a workgroup of segments_kernel
 constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
-constexpr int kGroupLanes = 4, kGroups = 64 / kGroupLanes;  // a segment's maxima are kept for groups of 128 elements
+// A segment's maxima are kept for groups of elements: those of four lanes (128), or of each lane in a short row.
+template <bool kShort>
+struct Groups {
+  static constexpr int lanes = kShort ? 1 : 4, n = 64 / lanes;   // n in a segment
+};
 constexpr int kFewSegs = 8;  // rows of no more are not large: their workgroup's own passes are short
 constexpr int kBins = 2048;
 constexpr int kPad = 64;
@@ -53,11 +57,11 @@ struct Row {
   double p, q;
   int k;
   bool greedy;
-  __device__ bool filters() const { return k || p <= 1.0 || q > 0.0; }
+  __device__ __forceinline__ bool filters() const { return k || p <= 1.0 || q > 0.0; }
   // whether the weights of all elements are summed: nothing is left out, or top-p is of all
-  __device__ bool sums() const { return !greedy && !k && (p <= 1.0 || !(q > 0.0)); }
+  __device__ __forceinline__ bool sums() const { return !greedy && !k && (p <= 1.0 || !(q > 0.0)); }
 };
-__device__ inline Row row_of(const Settings &s, int row, int V) {
+__device__ __forceinline__ Row row_of(const Settings &s, int row, int V) {
   const float t = s.temperatures ? s.temperatures[row] : s.temperature;
   const float p = s.top_ps ? s.top_ps[row] : s.top_p, q = s.min_ps ? s.min_ps[row] : s.min_p;
   Row r;
@@ -128,7 +132,7 @@ struct RowAt {
   }
 };
 template <typename T, bool raw = false>
-__device__ inline RowAt<T, raw> row_at(const Logits &l, int row) {
+__device__ __forceinline__ RowAt<T, raw> row_at(const Logits &l, int row) {
   const char *p = l.p + row * l.stride;
   RowAt<T, raw> r;
   r.before = (int)(reinterpret_cast<uintptr_t>(p) % 16) / (int)sizeof(T);
@@ -245,30 +249,28 @@ __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readla
 __device__ __forceinline__ double last_lane(double x) {
   return __hiloint2double(last_lane(__double2hiint(x)), last_lane(__double2loint(x)));
 }
-__device__ inline double wave_sum(double x) {
+__device__ __forceinline__ double wave_sum(double x) {
   return last_lane(wave_scan(x, 0.0, [](double a, double b) { return a + b; }));
 }
 
-// grid: rows x groups of kWaves segments
-template <typename T>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(7))) void segments_kernel(
-    Logits l, Settings s, int groups, float *maxima, double *sums, int *large_rows) {
-  if (blockIdx.x == 0 && threadIdx.x == 0) *large_rows = 0;
-  const int row = blockIdx.x / groups, lane = threadIdx.x & 63;
-  const int seg = (int)(blockIdx.x % groups) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (seg >= l.segs) return;
-  const RowAt<T, true> r = row_at<T, true>(l, row);
+// A segment by a wave: the maxima of its groups to maxima[0 .. n), and where the row needs it the sum of its
+// weights against its own maximum to *sum (a short row's segment: its maximum to *top).
+template <bool kShort, typename T>
+__device__ __forceinline__ void summarise(const RowAt<T, true> &r, int seg, const Row &ask, float *maxima, double *sum,
+                                          float *top = nullptr) {
+  constexpr int kGroupLanes = Groups<kShort>::lanes;
+  const int lane = threadIdx.x & 63;
   float x[kLane];
   load_segment(r, seg, x);
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kLane; ++i) m = fmaxf(m, x[i]);
   for (int o = 1; o < kGroupLanes; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const Row ask = row_of(s, row, l.V);
-  const int64_t at = (int64_t)row * l.segs + seg;
-  if (lane % kGroupLanes == 0) maxima[at * kGroups + lane / kGroupLanes] = m;
-  if (!ask.sums()) return;
+  if (lane % kGroupLanes == 0) maxima[lane / kGroupLanes] = m;
+  if (!kShort && !ask.sums()) return;
   for (int o = kGroupLanes; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (kShort && lane == 0) *top = m;
+  if (kShort && !ask.sums()) return;
   double z = 0.0;
   m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m)));
   if (m > -INFINITY) {
@@ -290,12 +292,24 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(7))
     }
     z = wave_sum(z);
   }
-  if (lane == 0) sums[at] = z;
+  if (lane == 0) *sum = z;
+}
+
+// grid: rows x groups of kWaves segments
+template <typename T>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(7))) void segments_kernel(
+    Logits l, Settings s, int groups, float *maxima, double *sums, int *large_rows) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *large_rows = 0;
+  const int row = blockIdx.x / groups;
+  const int seg = (int)(blockIdx.x % groups) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (seg >= l.segs) return;
+  const int64_t at = (int64_t)row * l.segs + seg;
+  summarise<false>(row_at<T, true>(l, row), seg, row_of(s, row, l.V), maxima + at * Groups<false>::n, sums + at);
 }
 
 // Sums over a workgroup in the order of its threads: what comes before a thread, and the whole.
 template <typename N>
-__device__ N before_thread(N x, N *tmp, N *whole) {
+__device__ __forceinline__ N before_thread(N x, N *tmp, N *whole) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const N run = wave_scan(x, (N)0, [](N a, N b) { return a + b; });
   __syncthreads();
@@ -312,7 +326,7 @@ __device__ N before_thread(N x, N *tmp, N *whole) {
   return first + (run - x);
 }
 
-__device__ inline int block_min(int x, int *tmp) {
+__device__ __forceinline__ int block_min(int x, int *tmp) {
   x = last_lane(wave_scan(x, 0x7fffffff, [](int a, int b) { return min(a, b); }));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = x;
@@ -322,11 +336,11 @@ __device__ inline int block_min(int x, int *tmp) {
   return x;
 }
 // floats by their order (no NaN)
-__device__ inline float block_max(float x, int *tmp) {
+__device__ __forceinline__ float block_max(float x, int *tmp) {
   const int top = block_min(~(int)(ordered_bits(x) ^ 0x80000000u), tmp);
   return ordered_to_float((uint32_t)~top ^ 0x80000000u);
 }
-__device__ inline float block_min(float x, int *tmp) {
+__device__ __forceinline__ float block_min(float x, int *tmp) {
   const int low = block_min((int)(ordered_bits(x) ^ 0x80000000u), tmp);
   return ordered_to_float((uint32_t)low ^ 0x80000000u);
 }
@@ -338,8 +352,10 @@ struct Bins {
 };
 
 struct Shared {
-  float groups[kMaxSegs * kGroups];  // maxima
+  float groups[kMaxSegs * Groups<false>::n];  // maxima
   double mass[kMaxSegs];             // of a segment's kept elements
+  double sums[kFewSegs];             // of a short row's segments: sums, maxima
+  float tops[kFewSegs];
   int ties[kMaxSegs];                // its elements at the border
   Bins bins;                         // or arrays of their size
   u64 list[kList + kPad];            // keys (make_key) of candidates
@@ -380,8 +396,9 @@ __device__ __forceinline__ u64 whole_number(double w) { return (u64)(w * kOne + 
 __device__ __forceinline__ int bin_of(float x, float m, float scale) { return min((int)((m - x) * scale), kBins - 1); }
 
 // One workgroup's view of its row.
-template <typename T>
+template <typename T, bool kShort>
 struct Finish {
+  static constexpr int kGroupLanes = Groups<kShort>::lanes, kGroups = Groups<kShort>::n;
   Shared &sh;
   RowAt<T> r;
   Row ask;
@@ -391,9 +408,10 @@ struct Finish {
 
   __device__ __forceinline__ double weight_of(float x) const { return pow2(((double)x - (double)m) * ask.a); }
 
-  __device__ float segment_max(int seg) const {
+  __device__ __forceinline__ float segment_max(int seg) const {
+    if (kShort) return sh.tops[seg];
     float x = sh.groups[seg * kGroups];
-#pragma unroll
+#pragma unroll 8
     for (int g = 1; g < kGroups; ++g) x = fmaxf(x, sh.groups[seg * kGroups + g]);
     return x;
   }
@@ -416,12 +434,12 @@ struct Finish {
     }
   }
 
-  __device__ void clear_bins() {
+  __device__ __forceinline__ void clear_bins() {
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += kRowThreads) sh.bins.count[i] = 0, sh.bins.mass[i] = 0;
     __syncthreads();
   }
-  __device__ void add(int bin, double w) {
+  __device__ __forceinline__ void add(int bin, double w) {
     atomicAdd(&sh.bins.count[bin], 1u);
     atomicAdd(&sh.bins.mass[bin], whole_number(w));
   }
@@ -429,7 +447,7 @@ struct Finish {
   // The first bin (from `first_bin` 0 up) at which f(elements, mass up to and with it) holds; the last that has
   // any, if none.  *n, *w: what lies before it; *all_w: all masses.
   template <typename F>
-  __device__ int find_bin(F f, int *n_before, u64 *w_before, u64 *all) {
+  __device__ __forceinline__ int find_bin(F f, int *n_before, u64 *w_before, u64 *all) {
     __syncthreads();
     constexpr int kEach = kBins / kRowThreads;
     uint32_t n[kEach];
@@ -475,7 +493,7 @@ struct Finish {
   // The border of the first `want` elements (by_mass: of the elements before which the mass is below `want`), known to
   // lie at keys >= key(lo), by passes over the row: bins of equal ranges of keys, then of the border's
   // bin, until a bin is a key.  Right for every row, and the slowest way.
-  __device__ Border select(bool by_mass, double want, float lo_value) {
+  __device__ __forceinline__ Border select(bool by_mass, double want, float lo_value) {
     uint32_t lo = ordered_bits(lo_value), hi = ordered_bits(m);
     int above_n = 0;
     u64 above_w = 0;
@@ -515,7 +533,7 @@ struct Finish {
   }
 
   // The kept mass of every segment: what lies above the border and, in the order of ids, the ties.
-  __device__ void segment_masses(const Border &edge, float lo) {
+  __device__ __forceinline__ void segment_masses(const Border &edge, float lo) {
     __syncthreads();
     for (int i = threadIdx.x; i < segs; i += kRowThreads) sh.mass[i] = 0.0, sh.ties[i] = 0;
     __syncthreads();
@@ -557,7 +575,7 @@ struct Finish {
 
   // The element where the running sum of kept weights, in the order of ids, passes u of the whole: segment masses are in
   // sh.mass, ties in sh.ties.  All threads return it; own: its weight, whole: of all kept.
-  __device__ int pick(double u, const Border &edge, double *own, double *whole) {
+  __device__ __forceinline__ int pick(double u, const Border &edge, double *own, double *whole) {
     double z = 0.0, left = 0.0;
     int tied = 0;
     const int each = (segs + kRowThreads - 1) / kRowThreads, first = (int)threadIdx.x * each;
@@ -631,7 +649,7 @@ struct Finish {
   // ---- rows of which few elements can be kept: a list of them in LDS ----
 
   // Of the list's elements, in their order, the last one before which the mass is below `want`.
-  __device__ u64 last_below(double want) {
+  __device__ __forceinline__ u64 last_below(double want) {
     constexpr int kEach = kList / kRowThreads;
     const int tid = threadIdx.x, n = sh.n;
     put_in_order(sh.list, n, (u64)0, [](u64 a, u64 b) { return a > b; });
@@ -657,7 +675,7 @@ struct Finish {
   // numbers a thread; where there are fewer, several threads share a number's count.  `last`: a number that comes after all,
   // which fills the list up to whole 16-byte reads (kPad numbers more than n).
   template <int kMine, typename N, typename F>
-  __device__ void put_in_order(N *list, int n, N last, F more) {
+  __device__ __forceinline__ void put_in_order(N *list, int n, N last, F more) {
     constexpr int kRead = 16 / sizeof(N);
     const int tid = threadIdx.x;
     int split = 1;
@@ -688,7 +706,7 @@ struct Finish {
     __syncthreads();
   }
   template <typename N, typename F>
-  __device__ void put_in_order(N *list, int n, N last, F more) {
+  __device__ __forceinline__ void put_in_order(N *list, int n, N last, F more) {
     if (n <= kRowThreads)
       put_in_order<1>(list, n, last, more);
     else if (n <= 2 * kRowThreads)
@@ -699,7 +717,7 @@ struct Finish {
 
   // Of the list (all elements >= lo of the row): the token.  kEach elements a thread.
   template <int kEach>
-  __device__ void from_list(double u, double whole, int *token, double *own, double *kept) {
+  __device__ __forceinline__ void from_list(double u, double whole, int *token, double *own, double *kept) {
     const int tid = threadIdx.x, n = sh.n;
     put_in_order(sh.list, n, (u64)0, [](u64 a, u64 b) { return a > b; });
     uint32_t *const by_id = sh.bins.count;
@@ -765,7 +783,7 @@ struct Finish {
   }
 
   // The elements >= lo into the list, from the groups that have any; false: they are too many.
-  __device__ bool gather(float lo) {
+  __device__ __forceinline__ bool gather(float lo) {
     const int tid = threadIdx.x, n_groups = segs * kGroups;
     __syncthreads();
     if (tid == 0) sh.n = 0;
@@ -848,7 +866,7 @@ struct Finish {
 
   // reach() by the order of the maxima of kTops parts of the groups, where they suffice.
   template <int kTops>
-  __device__ float reach_of_few(bool by_mass, double want, bool *far) {
+  __device__ __forceinline__ float reach_of_few(bool by_mass, double want, bool *far) {
     constexpr int kSplit = kRowThreads / kTops;   // threads a maximum
     const int tid = threadIdx.x, e = tid / kSplit, part = tid % kSplit;
     float top = -INFINITY;
@@ -885,7 +903,7 @@ struct Finish {
 
   // A value such that the elements >= it reach `want` (their number, or by_mass their weights): by the groups' maxima
   // alone, which is less than there is.  -infinity: not reached.
-  __device__ float reach(bool by_mass, double want) {
+  __device__ __forceinline__ float reach(bool by_mass, double want) {
     // (few, as their order costs the square of their number; so many that most of those looked for are in parts of their own)
     bool far = false;
     float x = -INFINITY;
@@ -907,64 +925,101 @@ struct Finish {
     u64 w, all;
     const auto holds = [&](int run_n, u64 run_w) { return by_mass ? (double)run_w / kOne >= want : (double)run_n >= want; };
     const int b = find_bin(holds, &n, &w, &all);
-    if (!holds(n + (int)sh.bins.count[b], w + sh.bins.mass[b])) return -INFINITY;
-    float least = m;
-    for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
-      if (sh.groups[g] > -INFINITY && bin_of(sh.groups[g], m, scale) <= b) least = fminf(least, sh.groups[g]);
-    return block_min(least, sh.tmp_i);
+    if (holds(n + (int)sh.bins.count[b], w + sh.bins.mass[b])) {
+      float least = m;
+      for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
+        if (sh.groups[g] > -INFINITY && bin_of(sh.groups[g], m, scale) <= b) least = fminf(least, sh.groups[g]);
+      return block_min(least, sh.tmp_i);
+    }
+    return kShort && !by_mass ? reach_of_all(want) : -INFINITY;
+  }
+
+  // reach() of a number by all elements (of a short row: two passes over it).
+  __device__ __forceinline__ float reach_of_all(double want) {
+    float low = m;
+    each_segment(-INFINITY, [&](const float(&x)[16 / sizeof(T)]) __attribute__((always_inline)) {
+#pragma unroll
+      for (const float v : x) low = v > -INFINITY ? fminf(low, v) : low;
+    }, [](int) {});
+    low = block_min(low, sh.tmp_i);
+    const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
+    clear_bins();
+    each_segment(-INFINITY, [&](const float(&x)[16 / sizeof(T)]) __attribute__((always_inline)) {
+#pragma unroll
+      for (const float v : x)
+        if (v > -INFINITY) atomicAdd(&sh.bins.count[bin_of(v, m, scale)], 1u);
+    }, [](int) {});
+    int n;
+    u64 w, all;
+    const int b = find_bin([&](int run_n, u64) { return (double)run_n >= want; }, &n, &w, &all);
+    // (below every value of the bin: what lies further down only makes the list longer)
+    return scale > 0.0f ? m - (float)(b + 2) / scale : -INFINITY;
   }
 
   // The row by passes over it.
-  __device__ int by_passes(double u, double whole, float lo, double *own, double *kept) {
+  __device__ __forceinline__ int by_passes(double u, double whole, float lo, double *own, double *kept) {
     Border edge{0u, 0, 0.0};
-    if (ask.k) edge = select(false, (double)ask.k, lo);
-    if (ask.k && ask.p <= 1.0) {
-      whole = edge.mass;
-      lo = ordered_to_float(edge.key);
+#pragma unroll 1
+    for (int step = 0; step < 2; ++step) {   // top-k, then top-p (the passes' code once)
+      if (step ? !(ask.p <= 1.0) : !ask.k) continue;
+      edge = select(step, step ? ask.p * whole : (double)ask.k, lo);
+      if (step == 0) {
+        whole = edge.mass;   // (top-p's, after top-k)
+        lo = ordered_to_float(edge.key);
+      }
     }
-    if (ask.p <= 1.0) edge = select(true, ask.p * whole, lo);
     segment_masses(edge, edge.key ? fmaxf(ordered_to_float(edge.key), lo) : lo);
     return pick(u, edge, own, kept);
   }
 };
 
-__device__ inline double number_of(const float *u, int row) { return fmin(fmax((double)u[row], 0.0), 0.99999999999); }
+__device__ __forceinline__ double number_of(const float *u, int row) { return fmin(fmax((double)u[row], 0.0), 0.99999999999); }
 
-__device__ inline void answer(int row, int token, double own, double whole, int32_t *tokens, float *logprobs) {
+__device__ __forceinline__ void answer(int row, int token, double own, double whole, int32_t *tokens, float *logprobs) {
   if (threadIdx.x != 0) return;
   tokens[row] = token;
   if (logprobs) logprobs[row] = (float)log(own / whole);
 }
 
-// grid: rows
-template <typename T>
+// grid: rows.  kShort: the row is read here, and no segments_kernel came before (maxima, sums: not looked at).
+template <typename T, bool kShort>
 __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))) void row_kernel(Logits l, Settings s, const float *u, const float *maxima,
                                                           const double *sums, Work work, int32_t *tokens,
                                                           float *logprobs) {
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x;
-  Finish<T> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, 0.0f};
+  constexpr int kGroups = Groups<kShort>::n;
+  Finish<T, kShort> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, 0.0f};
   Row &ask = f.ask;
   const int64_t first = (int64_t)row * l.segs;
   float m = -INFINITY;
-  for (int i0 = tid; i0 < l.segs * kGroups; i0 += 8 * kRowThreads) {
-    float x[8];
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const int i = i0 + n * kRowThreads;
-      x[n] = i < l.segs * kGroups ? maxima[first * kGroups + i] : -INFINITY;
-    }
-#pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      const int i = i0 + n * kRowThreads;
-      if (i < l.segs * kGroups) sh.groups[i] = x[n];
-      m = fmaxf(m, x[n]);
+  if constexpr (kShort) {
+    const RowAt<T, true> raw = row_at<T, true>(l, row);
+    for (int seg = __builtin_amdgcn_readfirstlane(tid >> 6); seg < l.segs; seg += kRowWaves)
+      summarise<kShort>(raw, seg, ask, sh.groups + seg * kGroups, sh.sums + seg, sh.tops + seg);
+    __syncthreads();
+    if (tid < l.segs) m = sh.tops[tid];
+  } else {
+    for (int i0 = tid; i0 < l.segs * kGroups; i0 += 8 * kRowThreads) {
+      float x[8];
+  #pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int i = i0 + n * kRowThreads;
+        x[n] = i < l.segs * kGroups ? maxima[first * kGroups + i] : -INFINITY;
+      }
+  #pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int i = i0 + n * kRowThreads;
+        if (i < l.segs * kGroups) sh.groups[i] = x[n];
+        m = fmaxf(m, x[n]);
+      }
     }
   }
   m = block_max(m, sh.tmp_i);
   if (m == INFINITY) {
     f.r.infinite = true;
     for (int i = tid; i < l.segs * kGroups; i += kRowThreads) sh.groups[i] = sh.groups[i] == INFINITY ? 0.0f : -INFINITY;
+    if (kShort && tid < l.segs) sh.tops[tid] = sh.tops[tid] == INFINITY ? 0.0f : -INFINITY;
     m = 0.0f;
   }
   f.m = m;
@@ -993,7 +1048,7 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
       double z = 0.0;
       for (int i = tid; i < l.segs; i += kRowThreads) {
         const float top = f.segment_max(i);
-        const double x = top > -INFINITY ? sums[first + i] * f.weight_of(top) : 0.0;
+        const double x = top > -INFINITY ? (kShort ? sh.sums[i] : sums[first + i]) * f.weight_of(top) : 0.0;
         sh.mass[i] = x;
         sh.ties[i] = 0;
         z += x;
@@ -1149,7 +1204,8 @@ __device__ void finish_large(Shared &sh, int row, const Logits &l, const Setting
   const int tid = threadIdx.x;
   const Large x = work.large[row];
   __syncthreads();
-  Finish<T> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, x.m};
+  constexpr int kGroups = Groups<false>::n;
+  Finish<T, false> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, x.m};
   f.r.infinite = x.infinite;
   const int64_t first = (int64_t)row * l.segs;
   const double at = number_of(u, row);
@@ -1231,7 +1287,7 @@ Layout layout(int rows, int V) {
   };
   const size_t segs = (size_t)rows * segments(V);
   w.sums = take(segs * sizeof(double));
-  w.maxima = take(segs * kGroups * sizeof(float));
+  w.maxima = take(segs * Groups<false>::n * sizeof(float));
   if (segments(V) <= kFewSegs) {   // (no large rows)
     w.rows = take(sizeof(int));
     w.bytes = n;
@@ -1304,8 +1360,12 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   hipStream_t q = static_cast<hipStream_t>(stream);
   auto launch = [&](auto t) {
     using T = decltype(t);
+    if (l.segs <= kFewSegs) {
+      row_kernel<T, true><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
+      return;
+    }
     segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums, work.rows);
-    row_kernel<T><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
+    row_kernel<T, false><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
     if (can_be_large) {
       const int64_t all = (int64_t)rows * parts;
       const unsigned some = (unsigned)(all < kSpread ? all : kSpread), few = (unsigned)(rows < kSpread ? rows : kSpread);

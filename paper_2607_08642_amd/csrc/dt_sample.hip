@@ -29,7 +29,10 @@ template <bool kShort>
 struct Groups {
   static constexpr int lanes = kShort ? 1 : 4, n = 64 / lanes;   // n in a segment
 };
-constexpr int kFewSegs = 8;  // rows of no more are not large: their workgroup's own passes are short
+// Rows of no more segments are read by the workgroup that finishes them, in one launch (graph-captured calls, two launches / one:
+// 8,000 logits 13 / 10 us for a row, 47 / 32 for 2,048 of them with top-k 20; 32,000: 13 / 12, 47 / 46, with top-p 0.9 141 / 97;
+// one row of 32,000 as it is 11 / 14), and are not large: their workgroup's own passes are short.
+constexpr int kFewSegs = 16;
 constexpr int kBins = 2048;
 constexpr int kPad = 64;
 constexpr int kList = 1024;  // elements that a row's end is found among in LDS
@@ -298,8 +301,8 @@ __device__ __forceinline__ void summarise(const RowAt<T, true> &r, int seg, cons
 // grid: rows x groups of kWaves segments
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(7))) void segments_kernel(
-    Logits l, Settings s, int groups, float *maxima, double *sums, int *large_rows) {
-  if (blockIdx.x == 0 && threadIdx.x == 0) *large_rows = 0;
+    Logits l, Settings s, int groups, float *maxima, double *sums, int *large) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *large = 0;
   const int row = blockIdx.x / groups;
   const int seg = (int)(blockIdx.x % groups) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (seg >= l.segs) return;
@@ -367,8 +370,9 @@ struct Shared {
   double before;
 };
 
-// What the large rows of a call pass from one launch to the next.
+// What the large rows of a call pass from one launch to the next, in the order in which they are found.
 struct Large {
+  int row;
   int on;            // 1: the border is looked for in bins; 2: all from `lo` on is kept
   float m, lo, scale;
   double whole;
@@ -377,10 +381,10 @@ struct Large {
 
 struct Work {
   Large *large;  // [rows], NULL: no row of the call can be one
-  int *rows;     // [1 + rows] how many there are, which
-  u64 *bins;     // [rows][kBins]
-  u64 *list;     // [rows][kList] the elements in the border's bin
-  u64 *above;    // [rows] the mass before that bin
+  int *count;    // of them
+  u64 *bins;     // of each: [kBins]
+  u64 *list;     // [kList] the elements in the border's bin
+  u64 *above;    // the mass before that bin
 };
 
 // Where an order's prefix ends: elements above `key` are kept, and `ties` of those equal to it.
@@ -1077,10 +1081,14 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
       } else {
         if (work.large && !ask.k) {
           large = true;
-          Large &x = work.large[row];
-          if (tid == 0) work.rows[1 + atomicAdd(work.rows, 1)] = row;
-          if (tid == 0) x = Large{ask.p <= 1.0 ? 1 : 2, m, lo, m > lo ? (float)(kBins - 1) / (m - lo) : 0.0f, whole, f.r.infinite, 0};
-          for (int i = tid; i < kBins; i += kRowThreads) work.bins[(int64_t)row * kBins + i] = 0;
+          __syncthreads();
+          if (tid == 0) sh.at = atomicAdd(work.count, 1);
+          __syncthreads();
+          const int at_large = sh.at;
+          if (tid == 0)
+            work.large[at_large] = Large{row,  ask.p <= 1.0 ? 1 : 2, m, lo, m > lo ? (float)(kBins - 1) / (m - lo) : 0.0f, whole,
+                                         f.r.infinite, 0};
+          for (int i = tid; i < kBins; i += kRowThreads) work.bins[(int64_t)at_large * kBins + i] = 0;
         } else {
           token = f.by_passes(at, whole, lo, &own, &whole);
         }
@@ -1094,17 +1102,27 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
 
 // ---- rows of which many elements are kept: the passes over all workgroups ----
 
-// (each over the listed rows' parts, or rows, by as many workgroups as are useful at once)
+// (each over the parts of the rows found, or the rows, by as many workgroups as are useful at once)
+
+// The i-th of them; false: there are fewer.  (Asked for together with their number.)
+__device__ __forceinline__ bool large_at(const Work &work, int rows, int i, Large *x) {
+  if (i >= rows) return false;
+  const int count = *work.count;
+  *x = work.large[i];
+  asm volatile("" : "+v"(x->row), "+v"(x->on), "+v"(x->lo));
+  return i < count;
+}
 
 // Masses in bins of values, from m down to lo.
 template <typename T>
 __global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, int parts, Work work) {
   __shared__ u64 bins[kBins];
-  const int items = *work.rows * parts;
-  for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    const int row = work.rows[1 + item / parts];
-    const Large x = work.large[row];
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    Large x;
+    const int at = item / parts;
+    if (!large_at(work, l.rows, at, &x)) return;
     if (x.on != 1) continue;
+    const int row = x.row;
     const int seg = item % parts * kPart + (threadIdx.x >> 6);
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
@@ -1122,7 +1140,7 @@ __global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, 
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += 64 * kPart)
-      if (bins[i]) atomicAdd(&work.bins[(int64_t)row * kBins + i], bins[i]);
+      if (bins[i]) atomicAdd(&work.bins[(int64_t)at * kBins + i], bins[i]);
   }
 }
 
@@ -1133,10 +1151,12 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
   __shared__ u64 tmp[kRowWaves];
   __shared__ int tmp_i[kRowWaves];
   static_assert(kPart == kRowWaves, "sums over a workgroup");
-  const int tid = threadIdx.x, items = *work.rows * parts;
-  for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    const int row = work.rows[1 + item / parts];
-    const Large x = work.large[row];
+  const int tid = threadIdx.x;
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    Large x;
+    const int at = item / parts;
+    if (!large_at(work, l.rows, at, &x)) return;
+    const int row = x.row;
     const int seg = item % parts * kPart + (tid >> 6);
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
@@ -1148,7 +1168,7 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
       constexpr int kEach = kBins / (64 * kPart);
       u64 w[kEach], sum = 0, above = 0, all;
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) sum += w[i] = work.bins[(int64_t)row * kBins + kEach * tid + i];
+      for (int i = 0; i < kEach; ++i) sum += w[i] = work.bins[(int64_t)at * kBins + kEach * tid + i];
       u64 run = before_thread(sum, tmp, &all);
       const double want = ask.p * x.whole;
       int mine = kBins;
@@ -1160,7 +1180,7 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
       }
       border = block_min(mine, tmp_i);
       // (never reached: all is kept)
-      if (border < kBins && border == mine && item % parts == 0) work.above[row] = above;
+      if (border < kBins && border == mine && item % parts == 0) work.above[at] = above;
     }
     if (seg >= l.segs) continue;
     constexpr int kPiece = 16 / sizeof(T);
@@ -1181,13 +1201,13 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
     const int listed = last_lane(place);
     if (listed) {   // (one atomic for the wave)
       int base = 0;
-      if ((tid & 63) == 0) base = atomicAdd(&work.large[row].listed, listed);
+      if ((tid & 63) == 0) base = atomicAdd(&work.large[at].listed, listed);
       place += __builtin_amdgcn_readfirstlane(base) - mine;
 #pragma unroll
       for (int i = 0; i < kLane; ++i)
         if (v[i] >= x.lo && bin_of(v[i], x.m, x.scale) == border) {
           if (place < kList)
-            work.list[(int64_t)row * kList + place] =
+            work.list[(int64_t)at * kList + place] =
                 make_key(v[i], (uint32_t)(piece_at<T>(seg, tid & 63, i / kPiece) + i % kPiece - r.before));
           ++place;
         }
@@ -1199,10 +1219,9 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
 
 // The border among its bin's elements, and the token.
 template <typename T>
-__device__ void finish_large(Shared &sh, int row, const Logits &l, const Settings &s, const float *u, const float *maxima,
+__device__ __forceinline__ void finish_large(Shared &sh, int index, const Large &x, const Logits &l, const Settings &s, const float *u, const float *maxima,
                              const double *masses, const Work &work, int32_t *tokens, float *logprobs) {
-  const int tid = threadIdx.x;
-  const Large x = work.large[row];
+  const int tid = threadIdx.x, row = x.row;
   __syncthreads();
   constexpr int kGroups = Groups<false>::n;
   Finish<T, false> f{sh, row_at<T>(l, row), row_of(s, row, l.V), l.segs, x.m};
@@ -1215,11 +1234,11 @@ __device__ void finish_large(Shared &sh, int row, const Logits &l, const Setting
   Border edge{0u, 0, 0.0};
   if (fits) {
     if (tid == 0) sh.n = x.listed;
-    for (int i = tid; i < x.listed; i += kRowThreads) sh.list[i] = work.list[(int64_t)row * kList + i];
+    for (int i = tid; i < x.listed; i += kRowThreads) sh.list[i] = work.list[(int64_t)index * kList + i];
     for (int i = tid; i < l.segs; i += kRowThreads) sh.mass[i] = masses[first + i], sh.ties[i] = 0;
     __syncthreads();
     if (x.listed) {
-      const u64 border = f.last_below(f.ask.p * x.whole - (double)work.above[row] / kOne);
+      const u64 border = f.last_below(f.ask.p * x.whole - (double)work.above[index] / kOne);
       {
         // the kept ones of the bin join their segments (whole numbers: in any order); of the border's equals only those
         // up to it are kept
@@ -1267,15 +1286,17 @@ __global__ __launch_bounds__(kRowThreads) void large_kernel(Logits l, Settings s
                                                             const double *masses, Work work, int32_t *tokens,
                                                             float *logprobs) {
   __shared__ Shared sh;
-  const int rows = *work.rows;
-  for (int i = blockIdx.x; i < rows; i += gridDim.x)
-    finish_large<T>(sh, work.rows[1 + i], l, s, u, maxima, masses, work, tokens, logprobs);
+  for (int i = blockIdx.x;; i += gridDim.x) {
+    Large x;
+    if (!large_at(work, l.rows, i, &x)) return;
+    finish_large<T>(sh, i, x, l, s, u, maxima, masses, work, tokens, logprobs);
+  }
 }
 
 int segments(int V) { return (V + 15 + kSeg - 1) / kSeg; }
 
 struct Layout {
-  size_t sums, maxima, large, rows, above, bins, list, bytes;
+  size_t sums, maxima, count, large, above, bins, list, bytes;
 };
 Layout layout(int rows, int V) {
   Layout w{};
@@ -1288,13 +1309,12 @@ Layout layout(int rows, int V) {
   const size_t segs = (size_t)rows * segments(V);
   w.sums = take(segs * sizeof(double));
   w.maxima = take(segs * Groups<false>::n * sizeof(float));
+  w.count = take(sizeof(int));
   if (segments(V) <= kFewSegs) {   // (no large rows)
-    w.rows = take(sizeof(int));
     w.bytes = n;
     return w;
   }
   w.large = take(rows * sizeof(Large));
-  w.rows = take((rows + 1) * sizeof(int));
   w.above = take(rows * sizeof(u64));
   w.bins = take((size_t)rows * kBins * sizeof(u64));
   w.list = take((size_t)rows * kList * sizeof(u64));
@@ -1353,7 +1373,7 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   // its row's workgroup's)
   const bool can_be_large = l.segs > kFewSegs && (how->top_ks || how->top_k == 0) &&
                             (how->top_ps || how->top_p < 1.0f || how->min_ps || how->min_p > 0.0f);
-  const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<int *>(at + w.rows),
+  const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<int *>(at + w.count),
                   reinterpret_cast<u64 *>(at + w.bins), reinterpret_cast<u64 *>(at + w.list),
                   reinterpret_cast<u64 *>(at + w.above)};
   const int groups = (l.segs + kWaves - 1) / kWaves, parts = (l.segs + kPart - 1) / kPart;
@@ -1364,7 +1384,7 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
       row_kernel<T, true><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
       return;
     }
-    segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums, work.rows);
+    segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums, work.count);
     row_kernel<T, false><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
     if (can_be_large) {
       const int64_t all = (int64_t)rows * parts;

@@ -223,6 +223,43 @@ __device__ __forceinline__ void load_segment(const RowAt<T, raw> &r, int seg, fl
   }
 }
 
+// A segment by a wave, piece by piece from the wave's own LDS: for kernels that run once on most CUs, where fetching the
+// instructions of a loop over 32 elements takes longer than the loop (bins_kernel, 17 rows of 151,936 in fp32: see there).
+template <typename T>
+struct Staged {
+  static constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece;
+  u32x4 *at;   // [kPieces][64]
+
+  __device__ __forceinline__ Staged(u32x4 *lds, const RowAt<T> &r, int seg) : at(lds + (threadIdx.x & 63)) {
+    u32x4 w[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int place = piece_at<T>(seg, threadIdx.x & 63, j);
+      w[j] = u32x4{r.none, r.none, r.none, r.none};
+      if (inside<kPiece>(r, place)) w[j] = *reinterpret_cast<const u32x4 *>(r.base + place);
+    }
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) at[j * 64] = w[j];
+    if (seg * kSeg >= r.before && (seg + 1) * kSeg <= r.before + r.V) return;
+#pragma unroll 1
+    for (int j = 0; j < kPieces; ++j) {
+      const int place = piece_at<T>(seg, threadIdx.x & 63, j);
+      if (!inside<kPiece>(r, place)) at[j * 64] = edge_piece(r, place);
+    }
+  }
+  // f(element, its place) for all of the lane's
+  template <typename F>
+  __device__ __forceinline__ void each(const RowAt<T> &r, int seg, F f) const {
+#pragma unroll 1
+    for (int j = 0; j < kPieces; ++j) {
+      float x[kPiece];
+      unpack<kPiece>(r, at[j * 64], x);
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) f(x[i], piece_at<T>(seg, threadIdx.x & 63, j) + i);
+    }
+  }
+};
+
 // ---- over a wave, by moves between its lanes ----
 template <int ctrl, int rows>
 __device__ __forceinline__ int moved(int x, int none) {
@@ -1117,6 +1154,7 @@ __device__ __forceinline__ bool large_at(const Work &work, int rows, int i, Larg
 template <typename T>
 __global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, int parts, Work work) {
   __shared__ u64 bins[kBins];
+  __shared__ u32x4 staged[kPart][kSeg * sizeof(T) / 16];
   for (int item = blockIdx.x;; item += gridDim.x) {
     Large x;
     const int at = item / parts;
@@ -1126,17 +1164,16 @@ __global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, 
     const int seg = item % parts * kPart + (threadIdx.x >> 6);
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
-    float v[kLane];
-    if (seg < l.segs) load_segment(r, seg, v);
+    const Staged<T> v(staged[threadIdx.x >> 6], r, min(seg, l.segs - 1));
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += 64 * kPart) bins[i] = 0;
     __syncthreads();
     if (seg < l.segs) {
       const Row ask = row_of(s, row, l.V);
       const Pow2 pow2;
-#pragma unroll
-      for (int i = 0; i < kLane; ++i)
-        if (v[i] >= x.lo) atomicAdd(&bins[bin_of(v[i], x.m, x.scale)], whole_number(weight(v[i], x.m, ask.a, pow2)));
+      v.each(r, seg, [&](float y, int) __attribute__((always_inline)) {
+        if (y >= x.lo) atomicAdd(&bins[bin_of(y, x.m, x.scale)], whole_number(weight(y, x.m, ask.a, pow2)));
+      });
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += 64 * kPart)
@@ -1150,6 +1187,7 @@ template <typename T>
 __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s, int parts, double *masses, Work work) {
   __shared__ u64 tmp[kRowWaves];
   __shared__ int tmp_i[kRowWaves];
+  __shared__ u32x4 staged[kPart][kSeg * sizeof(T) / 16];
   static_assert(kPart == kRowWaves, "sums over a workgroup");
   const int tid = threadIdx.x;
   for (int item = blockIdx.x;; item += gridDim.x) {
@@ -1160,8 +1198,7 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
     const int seg = item % parts * kPart + (tid >> 6);
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
-    float v[kLane];
-    if (seg < l.segs) load_segment(r, seg, v);
+    const Staged<T> v(staged[tid >> 6], r, min(seg, l.segs - 1));
     const Row ask = row_of(s, row, l.V);
     int border = kBins;
     if (x.on == 1) {
@@ -1183,34 +1220,29 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
       if (border < kBins && border == mine && item % parts == 0) work.above[at] = above;
     }
     if (seg >= l.segs) continue;
-    constexpr int kPiece = 16 / sizeof(T);
     const Pow2 pow2;
     double z = 0.0;
     int mine = 0;
-#pragma unroll
-    for (int i = 0; i < kLane; ++i) {
-      if (!(v[i] >= x.lo)) continue;
-      const int b = bin_of(v[i], x.m, x.scale);
+    v.each(r, seg, [&](float y, int) __attribute__((always_inline)) {
+      if (!(y >= x.lo)) return;
+      const int b = bin_of(y, x.m, x.scale);
       if (b < border) {
-        const double w = weight(v[i], x.m, ask.a, pow2);
+        const double w = weight(y, x.m, ask.a, pow2);
         if (w >= ask.q) z += w;
       }
       mine += b == border;
-    }
+    });
     int place = wave_scan(mine, 0, [](int a, int b) { return a + b; });
     const int listed = last_lane(place);
     if (listed) {   // (one atomic for the wave)
       int base = 0;
       if ((tid & 63) == 0) base = atomicAdd(&work.large[at].listed, listed);
       place += __builtin_amdgcn_readfirstlane(base) - mine;
-#pragma unroll
-      for (int i = 0; i < kLane; ++i)
-        if (v[i] >= x.lo && bin_of(v[i], x.m, x.scale) == border) {
-          if (place < kList)
-            work.list[(int64_t)at * kList + place] =
-                make_key(v[i], (uint32_t)(piece_at<T>(seg, tid & 63, i / kPiece) + i % kPiece - r.before));
-          ++place;
-        }
+      v.each(r, seg, [&](float y, int where) __attribute__((always_inline)) {
+        if (!(y >= x.lo) || bin_of(y, x.m, x.scale) != border) return;
+        if (place < kList) work.list[(int64_t)at * kList + place] = make_key(y, (uint32_t)(where - r.before));
+        ++place;
+      });
     }
     z = wave_sum(z);
     if ((tid & 63) == 0) masses[(int64_t)row * l.segs + seg] = z;

@@ -276,7 +276,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(CacheView c, ChunkView
 }
 
 // The same blocks, keys rotated, and after them (blockIdx.x from kv * blocks on) the chunk's queries, a wave for a
-// part of a row.
+// part of a row.  One pass over queries, keys and values where rotation and append would take two over the keys, and
+// one launch: four prompts of 4,915 to 8,192 tokens (32 heads, 8 kv heads of 128 in bf16) 141 us, 4.6 TB/s; 32 tokens 5 us.
 template <int DT, int D, bool kNear>
 __global__ __launch_bounds__(kThreads) void append_rotated_kernel(CacheView c, ChunkView k, RotaryView rot, HeadsView q,
                                                                   RotatePlan plan, RowsView kr, const void *k_weight,

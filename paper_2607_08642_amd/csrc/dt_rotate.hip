@@ -1,5 +1,10 @@
-// Heads normed and rotated by position, as rows (dt_rotate): the argument checks, how rows are dealt to waves, the kernel.
+// Heads normed and rotated by position, as rows (dt_rotate): how rows are dealt to waves, the kernel.
 // (With the pages of a cache: append_rotated_kernel of dt_cache.hip.)
+//
+// y = w x / sqrt(mean x^2 + eps), then pairs turned by pos f_j: a copy with some forty instructions an access, bound by memory
+// for prompts (16,000 rows of 40 heads of 128 in bf16 66 us, 5.0 TB/s; 8,000 in fp32 64, 5.1; a copy of 1 GiB: 5.0) and by
+// latency for few rows (3.1 us for one row of a small model).  A wave takes a row, so that its angles are computed once, a pair a
+// lane, in 64 bits up to the turn's remainder, and are read from LDS for all heads.
 #include <math.h>
 
 #include "dt_rotate.h"
@@ -30,6 +35,9 @@ RotatePlan rotate_plan(int64_t rows, int heads, int kv_heads, int D) {
   while (16 * p.lanes < D) p.lanes *= 2;
   const int wide = 64 / p.lanes;
   p.passes = (heads + wide - 1) / wide + (kv_heads + wide - 1) / wide;
+  // Few rows: a row's passes are dealt to several waves, each of which computes the angles again.  40 heads of 128 in bf16,
+  // graph-captured, a wave a row / up to 4,096 waves / up to 16,384: 1 row 6.9 / 3.7 / 3.8 us, 544 8.5 / 5.3 / 5.4, 2,000
+  // 11.5 / 12.2 / 11.5, 4,000 16.6 / 17.2 / 19.7.
   p.splits = 1;
   while (p.splits < p.passes && rows * p.splits < 4096) ++p.splits;
   p.per = (p.passes + p.splits - 1) / p.splits;

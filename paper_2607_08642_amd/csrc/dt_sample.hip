@@ -440,7 +440,6 @@ struct Work {
 struct Border {
   uint32_t key;
   int ties;
-  double mass;  // of what is kept
 };
 
 __device__ __forceinline__ u64 whole_number(double w) { return (u64)(w * kOne + 0.5); }
@@ -469,18 +468,32 @@ struct Finish {
     return x;
   }
 
-  // By the waves, for every segment with an element >= lo: piece(its elements) by every lane, piece after piece (few
-  // registers: these are the slow rows' loops, and share a kernel with the others), then done(segment).
+  // By the waves, for every segment with an element >= lo: piece(its elements) by every lane, piece after piece, then
+  // done(segment).  All pieces are asked for first; they are kept apart, so that few registers are in use at once (these are
+  // the slow rows' loops, and share a kernel with the others).
   template <typename F, typename G>
   __device__ __forceinline__ void each_segment(float lo, F piece, G done) {
-    constexpr int kPiece = 16 / sizeof(T);
+    constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece;
     for (int seg = threadIdx.x >> 6; seg < segs; seg += kRowWaves) {
       const float top = segment_max(seg);
       if (top < lo || top == -INFINITY) continue;
+      u32x4 w[kPieces];
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        const int place = piece_at<T>(seg, threadIdx.x & 63, j);
+        w[j] = u32x4{r.none, r.none, r.none, r.none};
+        if (inside<kPiece>(r, place)) w[j] = *reinterpret_cast<const u32x4 *>(r.base + place);
+      }
+      const bool whole = seg * kSeg >= r.before && (seg + 1) * kSeg <= r.before + r.V;
 #pragma unroll 1
-      for (int j = 0; j < kLane / kPiece; ++j) {
+      for (int j = 0; j < kPieces; ++j) {
+        u32x4 now = w[0];
+#pragma unroll
+        for (int i = 0; i + 1 < kPieces; ++i) w[i] = w[i + 1];   // (the next one's turn)
+        const int place = piece_at<T>(seg, threadIdx.x & 63, j);
+        if (!whole && !inside<kPiece>(r, place)) now = edge_piece(r, place);
         float x[kPiece];
-        load_run<kPiece>(r, piece_at<T>(seg, threadIdx.x & 63, j), x);
+        unpack<kPiece>(r, now, x);
         piece(x);
       }
       done(seg);
@@ -495,6 +508,17 @@ struct Finish {
   __device__ __forceinline__ void add(int bin, double w) {
     atomicAdd(&sh.bins.count[bin], 1u);
     atomicAdd(&sh.bins.mass[bin], whole_number(w));
+  }
+  // The same by all lanes of a wave that are here, whose elements may be equal: the equals of the first lane's are added once
+  // (a row of equal logits would have its lanes wait for one another: 870 us for 151,936).
+  __device__ __forceinline__ void add_equals(uint32_t key, int bin, bool by_mass, float x) {
+    const u64 same = __ballot(key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key));
+    const int lane = threadIdx.x & 63;
+    int n = 1;
+    if (same >> lane & 1) n = lane == __ffsll((long long)same) - 1 ? __popcll(same) : 0;
+    if (n == 0) return;
+    atomicAdd(&sh.bins.count[bin], (uint32_t)n);
+    if (by_mass) atomicAdd(&sh.bins.mass[bin], (u64)n * whole_number(weight_of(x)));
   }
 
   // The first bin (from `first_bin` 0 up) at which f(elements, mass up to and with it) holds; the last that has
@@ -558,7 +582,7 @@ struct Finish {
         for (const float v : x) {
           const uint32_t key = ordered_bits(v);
           if (key < lo || key > hi || v == -INFINITY) continue;
-          add((int)((hi - key) >> shift), weight_of(v));
+          add_equals(key, (int)((hi - key) >> shift), by_mass, v);
         }
       }, [](int) {});
       int n;
@@ -579,7 +603,6 @@ struct Finish {
         double ties = by_mass ? ceil((want - mass) / w1) : want - above_n;
         if (!(ties < (double)here)) ties = here;   // (NaN: a weight of 0)
         o.ties = max((int)ties, above_n > 0 ? 0 : 1);
-        o.mass = mass + o.ties * w1;
         return o;
       }
     }
@@ -1011,17 +1034,23 @@ struct Finish {
 
   // The row by passes over it.
   __device__ __forceinline__ int by_passes(double u, double whole, float lo, double *own, double *kept) {
-    Border edge{0u, 0, 0.0};
+    Border edge{0u, 0};
 #pragma unroll 1
     for (int step = 0; step < 2; ++step) {   // top-k, then top-p (the passes' code once)
       if (step ? !(ask.p <= 1.0) : !ask.k) continue;
       edge = select(step, step ? ask.p * whole : (double)ask.k, lo);
-      if (step == 0) {
-        whole = edge.mass;   // (top-p's, after top-k)
-        lo = ordered_to_float(edge.key);
+      lo = fmaxf(ordered_to_float(edge.key), lo);
+      if (step == 0 && ask.p <= 1.0) {   // (top-p's whole: the mass of all k, whatever min_p leaves of it)
+        const double q = ask.q;
+        ask.q = 0.0;
+        segment_masses(edge, lo);
+        ask.q = q;
+        double x = 0.0;
+        for (int i = threadIdx.x; i < segs; i += kRowThreads) x += sh.mass[i];
+        before_thread(x, sh.tmp_d, &whole);
       }
     }
-    segment_masses(edge, edge.key ? fmaxf(ordered_to_float(edge.key), lo) : lo);
+    segment_masses(edge, lo);
     return pick(u, edge, own, kept);
   }
 };
@@ -1139,11 +1168,11 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
                                          f.r.infinite, 0};
           for (int i = tid; i < kBins; i += kRowThreads) work.bins[(int64_t)at_large * kBins + i] = 0;
         } else {
-          token = f.by_passes(at, whole, lo, &own, &whole);
+          token = f.by_passes(at, whole, near, &own, &whole);
         }
       }
     } else {
-      token = f.pick(at, Border{0u, 0, 0.0}, &own, &whole);
+      token = f.pick(at, Border{0u, 0}, &own, &whole);
     }
   }
   if (!large) answer(row, token, own, whole, tokens, logprobs);
@@ -1276,7 +1305,7 @@ __device__ __forceinline__ void finish_large(Shared &sh, int index, const Large 
   double own = 1.0, whole = x.whole;
   int token;
   const bool fits = x.listed <= kList;
-  Border edge{0u, 0, 0.0};
+  Border edge{0u, 0};
   if (fits) {
     if (tid == 0) sh.n = x.listed;
     for (int i = tid; i < x.listed; i += kRowThreads) sh.list[i] = work.list[(int64_t)index * kList + i];
@@ -1312,7 +1341,7 @@ __device__ __forceinline__ void finish_large(Shared &sh, int index, const Large 
     }
   }
   if (fits) {
-    if (!edge.key) edge = Border{ordered_bits(x.lo), 1 << 30, 0.0};   // (all from lo on)
+    if (!edge.key) edge = Border{ordered_bits(x.lo), 1 << 30};   // (all from lo on)
     token = f.pick(at, edge, &own, &whole);
   } else {
     __syncthreads();

@@ -48,7 +48,7 @@ constexpr int kFewSegs = 16;
 constexpr int kBins = 2048;
 constexpr int kPad = 64;
 constexpr int kList = 1024;  // elements that a row's end is found among in LDS
-constexpr int kPart = 4;     // segments (waves) of a workgroup of the passes for large rows
+constexpr int kPart = 4;     // waves of a workgroup of the passes for large rows
 constexpr int kMaxGroups = 1 << 24;
 constexpr int kSpread = 1024;   // workgroups of the passes for large rows (four a CU): launches that find no such row end soon
 constexpr double kOne = 17592186044416.0;  // 2^44: masses in the bins are whole numbers of 2^-44 (2^19 of them fit 63 bits)
@@ -235,18 +235,20 @@ __device__ __forceinline__ void load_segment(const RowAt<T, raw> &r, int seg, fl
   }
 }
 
-// A segment by a wave, piece by piece from the wave's own LDS: short code for kernels that run once on most CUs
+// A segment, or a part of it, by a wave, piece by piece from the wave's own LDS: short code for kernels that run once on most CUs
 // (bins_kernel at 17 rows of 151,936 in fp32: 12.2 -> 11.0 us).
-template <typename T>
+template <typename T, int kWavesEach>
 struct Staged {
-  static constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece;
+  static constexpr int kPiece = 16 / sizeof(T), kPieces = kLane / kPiece / kWavesEach;
   u32x4 *at;   // [kPieces][64]
+  int first;   // piece
 
-  __device__ __forceinline__ Staged(u32x4 *lds, const RowAt<T> &r, int seg) : at(lds + (threadIdx.x & 63)) {
+  __device__ __forceinline__ Staged(u32x4 *lds, const RowAt<T> &r, int seg, int part)
+      : at(lds + (threadIdx.x & 63)), first(part * kPieces) {
     u32x4 w[kPieces];
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
-      const int place = piece_at<T>(seg, threadIdx.x & 63, j);
+      const int place = piece_at<T>(seg, threadIdx.x & 63, first + j);
       w[j] = u32x4{r.none, r.none, r.none, r.none};
       if (inside<kPiece>(r, place)) w[j] = *reinterpret_cast<const u32x4 *>(r.base + place);
     }
@@ -255,7 +257,7 @@ struct Staged {
     if (seg * kSeg >= r.before && (seg + 1) * kSeg <= r.before + r.V) return;
 #pragma unroll 1
     for (int j = 0; j < kPieces; ++j) {
-      const int place = piece_at<T>(seg, threadIdx.x & 63, j);
+      const int place = piece_at<T>(seg, threadIdx.x & 63, first + j);
       if (!inside<kPiece>(r, place)) at[j * 64] = edge_piece(r, place);
     }
   }
@@ -267,7 +269,7 @@ struct Staged {
       float x[kPiece];
       unpack<kPiece>(r, at[j * 64], x);
 #pragma unroll
-      for (int i = 0; i < kPiece; ++i) f(x[i], piece_at<T>(seg, threadIdx.x & 63, j) + i);
+      for (int i = 0; i < kPiece; ++i) f(x[i], piece_at<T>(seg, threadIdx.x & 63, first + j) + i);
     }
   }
 };
@@ -1203,10 +1205,10 @@ __global__ __launch_bounds__(64 * kPart) void bins_kernel(Logits l, Settings s, 
     if (!large_at(work, l.rows, at, &x)) return;
     if (x.on != 1) continue;
     const int row = x.row;
-    const int seg = item % parts * kPart + (threadIdx.x >> 6);
+    const int wave = threadIdx.x >> 6, seg = item % parts * kPart + wave;
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
-    const Staged<T> v(staged[threadIdx.x >> 6], r, min(seg, l.segs - 1));
+    const Staged<T, 1> v(staged[wave], r, min(seg, l.segs - 1), 0);
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += 64 * kPart) bins[i] = 0;
     __syncthreads();
@@ -1229,7 +1231,8 @@ template <typename T>
 __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s, int parts, double *masses, Work work) {
   __shared__ u64 tmp[kRowWaves];
   __shared__ int tmp_i[kRowWaves];
-  __shared__ u32x4 staged[kPart][kSeg * sizeof(T) / 16];
+  __shared__ double halves[kPart];
+  __shared__ u32x4 staged[kPart][kSeg * sizeof(T) / 32];
   static_assert(kPart == kRowWaves, "sums over a workgroup");
   const int tid = threadIdx.x;
   for (int item = blockIdx.x;; item += gridDim.x) {
@@ -1237,10 +1240,10 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
     const int at = item / parts;
     if (!large_at(work, l.rows, at, &x)) return;
     const int row = x.row;
-    const int seg = item % parts * kPart + (tid >> 6);
+    const int wave = tid >> 6, seg = item % parts * (kPart / 2) + wave / 2;
     RowAt<T> r = row_at<T>(l, row);
     r.infinite = x.infinite;
-    const Staged<T> v(staged[tid >> 6], r, min(seg, l.segs - 1));
+    const Staged<T, 2> v(staged[wave], r, min(seg, l.segs - 1), wave & 1);   // (few rows: more SIMDs at work, 14.4 -> 12.0 us)
     const Row ask = row_of(s, row, l.V);
     int border = kBins;
     if (x.on == 1) {
@@ -1261,33 +1264,37 @@ __global__ __launch_bounds__(64 * kPart) void masses_kernel(Logits l, Settings s
       // (never reached: all is kept)
       if (border < kBins && border == mine && item % parts == 0) work.above[at] = above;
     }
-    if (seg >= l.segs) continue;
-    const Pow2 pow2;
     double z = 0.0;
-    int mine = 0;
-    v.each(r, seg, [&](float y, int) __attribute__((always_inline)) {
-      if (!(y >= x.lo)) return;
-      const int b = bin_of(y, x.m, x.scale);
-      if (b < border) {
-        const double w = weight(y, x.m, ask.a, pow2);
-        if (w >= ask.q) z += w;
-      }
-      mine += b == border;
-    });
-    int place = wave_scan(mine, 0, [](int a, int b) { return a + b; });
-    const int listed = last_lane(place);
-    if (listed) {   // (one atomic for the wave)
-      int base = 0;
-      if ((tid & 63) == 0) base = atomicAdd(&work.large[at].listed, listed);
-      place += __builtin_amdgcn_readfirstlane(base) - mine;
-      v.each(r, seg, [&](float y, int where) __attribute__((always_inline)) {
-        if (!(y >= x.lo) || bin_of(y, x.m, x.scale) != border) return;
-        if (place < kList) work.list[(int64_t)at * kList + place] = make_key(y, (uint32_t)(where - r.before));
-        ++place;
+    if (seg < l.segs) {
+      const Pow2 pow2;
+      int mine = 0;
+      v.each(r, seg, [&](float y, int) __attribute__((always_inline)) {
+        if (!(y >= x.lo)) return;
+        const int b = bin_of(y, x.m, x.scale);
+        if (b < border) {
+          const double w = weight(y, x.m, ask.a, pow2);
+          if (w >= ask.q) z += w;
+        }
+        mine += b == border;
       });
+      int place = wave_scan(mine, 0, [](int a, int b) { return a + b; });
+      const int listed = last_lane(place);
+      if (listed) {   // (one atomic for the wave)
+        int base = 0;
+        if ((tid & 63) == 0) base = atomicAdd(&work.large[at].listed, listed);
+        place += __builtin_amdgcn_readfirstlane(base) - mine;
+        v.each(r, seg, [&](float y, int where) __attribute__((always_inline)) {
+          if (!(y >= x.lo) || bin_of(y, x.m, x.scale) != border) return;
+          if (place < kList) work.list[(int64_t)at * kList + place] = make_key(y, (uint32_t)(where - r.before));
+          ++place;
+        });
+      }
+      z = wave_sum(z);
     }
-    z = wave_sum(z);
-    if ((tid & 63) == 0) masses[(int64_t)row * l.segs + seg] = z;
+    __syncthreads();   // (the last item's halves have been read)
+    if ((tid & 63) == 0) halves[wave] = z;
+    __syncthreads();
+    if ((tid & 127) == 0 && seg < l.segs) masses[(int64_t)row * l.segs + seg] = halves[wave] + halves[wave + 1];
   }
 }
 
@@ -1450,7 +1457,8 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<int *>(at + w.count),
                   reinterpret_cast<u64 *>(at + w.bins), reinterpret_cast<u64 *>(at + w.list),
                   reinterpret_cast<u64 *>(at + w.above)};
-  const int groups = (l.segs + kWaves - 1) / kWaves, parts = (l.segs + kPart - 1) / kPart;
+  const int groups = (l.segs + kWaves - 1) / kWaves, parts = (l.segs + kPart - 1) / kPart,
+            halves = (l.segs + kPart / 2 - 1) / (kPart / 2);
   hipStream_t q = static_cast<hipStream_t>(stream);
   auto launch = [&](auto t) {
     using T = decltype(t);
@@ -1461,11 +1469,10 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
     segments_kernel<T><<<(unsigned)(rows * groups), 64 * kWaves, 0, q>>>(l, s, groups, maxima, sums, work.count);
     row_kernel<T, false><<<rows, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
     if (can_be_large) {
-      const int64_t all = (int64_t)rows * parts;
-      const unsigned some = (unsigned)(all < kSpread ? all : kSpread), few = (unsigned)(rows < kSpread ? rows : kSpread);
-      bins_kernel<T><<<some, 64 * kPart, 0, q>>>(l, s, parts, work);
-      masses_kernel<T><<<some, 64 * kPart, 0, q>>>(l, s, parts, sums, work);
-      large_kernel<T><<<few, kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
+      const auto some = [&](int64_t all) { return (unsigned)(all < kSpread ? all : kSpread); };
+      bins_kernel<T><<<some((int64_t)rows * parts), 64 * kPart, 0, q>>>(l, s, parts, work);
+      masses_kernel<T><<<some((int64_t)rows * halves), 64 * kPart, 0, q>>>(l, s, halves, sums, work);
+      large_kernel<T><<<some(rows), kRowThreads, 0, q>>>(l, s, u, maxima, sums, work, tokens, logprobs);
     }
   };
   if (logits_dtype == DT_F32)

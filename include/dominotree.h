@@ -511,7 +511,8 @@ dt_status dt_cache_commit(const dt_cache *cache, const dt_chunk *chunk, int node
  * of a common beginning), uses says by how many; 0: it is free.  uses and held start as zeros, table as -1.  The books
  * have to be consistent and lens[b] <= table_width * page_size; where they are not, no access
  * leaves the tensors.  table and lens may be a dt_chunk's: a chunk has to lie in pages of its own, as it does
- * at the end of a sequence grown by dt_pages_fit or made by dt_pages_fork. */
+ * at the end of a sequence grown by dt_pages_fit or made by dt_pages_fork.  A sequence whose lens is cut back into a page
+ * that others hold has none there: fork it into another place of the batch and append to that. */
 typedef struct {
   int pages, page_size;    /* of the cache; pages <= 2^28 */
   int batch, table_width;  /* as dt_chunk's; batch * table_width < 2^31 */

@@ -884,6 +884,7 @@ class Pages:
     Chunk's.  All are int32 tensors on the cache's device, views of `state`, which holds the whole books (to be saved and
     copied back): missing [1], uses [pages], held [batch], lens, table [batch, width].
     missing: pages that the last call lacked; it then grew and forked nothing.
+    A sequence that is cut back into a page that others hold is forked into another place before it is appended to.
     Calls run on torch's current stream of the cache's device unless one is given; they use one workspace, so calls of one
     Pages (captured ones too) must not overlap, as they change the same books.
     """

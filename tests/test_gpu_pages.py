@@ -190,6 +190,30 @@ def test_a_fork_attends_as_its_source():
                               atol=2.0 ** -7 * float(wv.abs().max()))
 
 
+def test_a_cut_into_a_shared_page():
+    """Forked on, a sequence that was cut back into a page of another has that page for itself."""
+    b = Both(40, 32, 4, 5, kv=2, D=64, layers=1, seed=10)
+    p, c = b.pages, b.cache
+    g = torch.Generator().manual_seed(2)
+    rnd = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()  # noqa: E731
+    k, v, x, y = rnd(100, 2, 64), rnd(100, 2, 64), rnd(1, 2, 64), rnd(1, 2, 64)
+    p.lens.copy_(i32([100, 0, 0, 0]))
+    p.fit()
+    c.append(binding.Chunk(i32([0, 100, 100, 100, 100]), p.lens, p.table, 100, 160), k, v)
+    p.fork(i32([-1, 0, -1, -1]))
+    p.lens.copy_(i32([100, 70, 0, 0]))
+    p.fit()
+    p.fork(i32([-1, -1, 1, -1]))
+    p.lens.copy_(i32([100, 70, 71, 0]))
+    p.fit()
+    c.append(binding.Chunk(i32([0, 0, 0, 1, 1]), p.lens, p.table, 1, 160), x, y)
+    table = p.table.tolist()
+    assert table[0][:3] == table[1][:3] and table[2][:2] == table[0][:2] and table[2][2] != table[0][2]
+    gk, gv = c.read(binding.Chunk(i32([0, 100, 170, 241, 241]), p.lens, p.table, 100, 160), 241)
+    for got, old, one in ((gk, k, x), (gv, v, y)):
+        assert same(got[:100], old) and same(got[100:170], old[:70]) and same(got[170:], torch.cat([old[:70], one]))
+
+
 def test_streams_and_graphs():
     """A captured round (lengths grow, pages follow, sequences fork) replayed, between calls on another stream."""
     b = Both(300, 32, 6, 12, seed=4)

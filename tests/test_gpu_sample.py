@@ -208,3 +208,64 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         assert all(torch.equal(g, w) for g, w in zip(got, want)) and all(bool((f == 7).all()) for f in fill)
         assert math.isfinite(float(lp.sum()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [32752, 32753, 32754, 32768, 32769])
+def test_where_a_row_takes_another_launch(dtype, V):
+    """Sizes about the largest row that one launch reads, also where rows begin inside a 16-byte piece."""
+    x, u = rows_of(3, V, dtype, seed=V)
+    for how in SETTINGS:
+        check(x, u, **how)
+    for pad in (1, 7):
+        wide = torch.full((3, V + pad), 50.0, dtype=x.dtype, device="cuda")
+        wide[:, :V] = x.cuda()
+        for how in (dict(), dict(k=20, p=0.95), dict(p=0.9), dict(p=0.999999), dict(T=0.0)):
+            check(x, u, dev=wide[:, :V], **how)
+
+
+@pytest.mark.parametrize("how", [dict(k=1023), dict(k=1024), dict(k=1025), dict(k=2400, p=0.9), dict(k=5000, q=0.01),
+                                 dict(k=60000, p=0.99, q=0.001), dict(k=100000)], ids=str)
+def test_many_of_a_large_vocabulary(how):
+    for spread in (0.7, 2.2):
+        x, u = rows_of(3, 100003, "f32", seed=40, spread=spread, high=2)
+        check(x, u, **how)
+
+
+@pytest.mark.parametrize("how", [dict(p=0.9), dict(p=0.3, q=0.5), dict(q=0.9), dict(k=3000), dict(k=3000, p=0.5), dict()], ids=str)
+def test_ties_of_a_large_vocabulary(how):
+    """Thousands of equal logits at the border, more than a list holds; rows that are and are not so in one call."""
+    g = torch.Generator().manual_seed(41)
+    x = torch.randn(6, 70001, generator=g)
+    x[0] = 1.0
+    x[1] = torch.randint(0, 3, (70001,), generator=g).float()
+    x[2, 100:60000] = 0.25
+    x[3, ::2] = -INF
+    x[3, 1::2] = 2.0
+    x[4, 5:4000] = INF
+    check(x, torch.rand(6, generator=g), **how)
+
+
+def test_host_threads_on_one_stream():
+    """Calls of different sizes by several threads on the same stream: each thread's workspace is its own."""
+    import threading
+    cases = []
+    for n, (R, V, how) in enumerate([(3, 151936, dict(p=0.9)), (40, 2003, dict(k=20)), (1, 60001, dict(k=50, p=0.8)), (17, 40000, dict())]):
+        x, u = rows_of(R, V, "bf16", seed=50 + n, spread=0.9, high=3)
+        args = x.cuda(), u.cuda(), 1.0, how.get("k", 0), how.get("p", 1.0)
+        cases.append((args, binding.sample(*args).cpu()))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(first):
+        for n in range(24):
+            args, want = cases[(first + n) % 4]
+            if not torch.equal(binding.sample(*args).cpu(), want):
+                wrong.append((first, n))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong

@@ -18,8 +18,8 @@
 // Measured, 151,936 logits in bf16, kernels alone: segments_kernel over 544 rows 26 us without sums (6.4 TB/s: memory), 65 with
 // sums (64-bit arithmetic: 15 instructions of about five cycles an element); row_kernel at one row 3 us for the
 // largest, 6 for all, 9 for top-k 20, 11 for top-p 0.9, 19 for top-k 200; at 544 rows 4, 9, 12, 17, 28: bound by latency, of
-// memory (two reads that wait for one another) and of instructions, which a workgroup runs once.  The launches for large rows take
-// 5 us in all where there is none at one row, 9 at 544, and 34 for 17 flat rows of fp32.
+// memory (two reads that wait for one another) and of instructions, which a workgroup runs once.  The launches for large rows add
+// 5 us where there is none (1, 32 and 544 rows with top-k 20, graph-captured), and take 34 for 17 flat rows of fp32.
 #include <cmath>
 #include <type_traits>
 

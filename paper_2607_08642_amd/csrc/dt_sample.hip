@@ -446,8 +446,15 @@ struct Border {
 
 __device__ __forceinline__ u64 whole_number(double w) { return (u64)(w * kOne + 0.5); }
 
-// bins of equal ranges of values from m down, monotone in x
-__device__ __forceinline__ int bin_of(float x, float m, float scale) { return min((int)((m - x) * scale), kBins - 1); }
+// bins of equal ranges of values from m down, monotone in x (differences past fp32's range, which meet a scale of 0: the last)
+__device__ __forceinline__ int bin_of(float x, float m, float scale) {
+  return (int)fminf((m - x) * scale, (float)(kBins - 1));
+}
+// the scale with which they reach down to lo: 2^100 at most, so that it is finite and a bin's range a normal number where
+// all values lie within a hair of m
+__device__ __forceinline__ float scale_of(float m, float lo) {
+  return m > lo ? fminf((float)(kBins - 1) / (m - lo), 0x1p100f) : 0.0f;
+}
 
 // One workgroup's view of its row.
 template <typename T, bool kShort>
@@ -995,7 +1002,7 @@ struct Finish {
     for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
       if (sh.groups[g] > -INFINITY) low = fminf(low, sh.groups[g]);
     low = block_min(low, sh.tmp_i);
-    const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
+    const float scale = scale_of(m, low);
     clear_bins();
     for (int g = threadIdx.x; g < n_groups; g += kRowThreads)
       if (sh.groups[g] > -INFINITY) add(bin_of(sh.groups[g], m, scale), by_mass ? weight_of(sh.groups[g]) : 0.0);
@@ -1020,7 +1027,7 @@ struct Finish {
       for (const float v : x) low = v > -INFINITY ? fminf(low, v) : low;
     }, [](int) {});
     low = block_min(low, sh.tmp_i);
-    const float scale = m > low ? (float)(kBins - 1) / (m - low) : 0.0f;
+    const float scale = scale_of(m, low);
     clear_bins();
     each_segment(-INFINITY, [&](const float(&x)[16 / sizeof(T)]) __attribute__((always_inline)) {
 #pragma unroll
@@ -1166,8 +1173,7 @@ __global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(3))
           __syncthreads();
           const int at_large = sh.at;
           if (tid == 0)
-            work.large[at_large] = Large{row,  ask.p <= 1.0 ? 1 : 2, m, lo, m > lo ? (float)(kBins - 1) / (m - lo) : 0.0f, whole,
-                                         f.r.infinite, 0};
+            work.large[at_large] = Large{row, ask.p <= 1.0 ? 1 : 2, m, lo, scale_of(m, lo), whole, f.r.infinite, 0};
           for (int i = tid; i < kBins; i += kRowThreads) work.bins[(int64_t)at_large * kBins + i] = 0;
         } else {
           token = f.by_passes(at, whole, near, &own, &whole);

@@ -1,0 +1,49 @@
+"""Sampling at limits of its numbers: rows whose values lie within a hair of one another, or further apart than fp32
+reaches.  Tokens and log-probabilities against the definition in 64 bits, with the tolerances of test_gpu_sample.py."""
+import pytest
+import torch
+
+from test_gpu_sample import check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,ks", [(20, (2, 5, 10, 19)), (2003, (10, 64, 65, 100, 1000, 2002)), (20011, (100, 900, 4000)),
+                                  (70001, (100, 1025, 30000))])
+def test_values_that_lie_close(dtype, V, ks):
+    """Rows of zeros but for a few values of 1e-37 and less: their differences times the bins' number pass fp32's range when
+    divided by one another."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.zeros(7, V)
+    at = torch.randperm(V, generator=g)
+    x[0, at[0]] = 1e-37
+    x[1, at[:3]] = torch.tensor([1e-37, -1e-37, 2e-37])
+    x[2, at[:V // 3]] = -1e-37
+    x[3, at[:9]] = 1e-37 * torch.arange(-4, 5)
+    x[4] = 1e-38 * torch.randint(-9, 10, (V,), generator=g)
+    x[5] = 1e-44 * torch.randint(-9, 10, (V,), generator=g)     # (bf16: all zero)
+    x[6] = 1e-30 * torch.randn(V, generator=g)
+    x, u = x.to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype]), torch.rand(7, generator=g)
+    for k in ks:
+        check(x, u, k=k)
+        check(x, u, k=k, p=0.9, q=0.5)
+        check(x, u, k=k, T=1e-37)
+    for how in (dict(p=0.9), dict(p=0.3, q=0.9), dict(q=0.5), dict(p=0.9, T=1e-37), dict(q=0.1, T=1e-37)):
+        check(x, u, **how)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 20011, 70001])
+def test_values_that_lie_far_apart(dtype, V):
+    """Differences past fp32's largest number, and temperatures at which they count."""
+    g = torch.Generator().manual_seed(V + 1)
+    x = 3e38 * (2 * torch.rand(4, V, generator=g) - 1)
+    x[1] = 3e38 * torch.randint(-1, 2, (V,), generator=g)
+    x[2, V // 2:] = -float("inf")
+    x[3] = -3e38
+    x[3, V // 3] = 3.2e38
+    x, u = x.to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype]), torch.rand(4, generator=g)
+    for T in (1.0, 1e37, 2e38, float("inf")):
+        for how in (dict(), dict(k=100), dict(k=V // 2, p=0.9), dict(p=0.9), dict(q=0.2), dict(p=0.99, q=0.1)):
+            check(x, u, T=T, **how)

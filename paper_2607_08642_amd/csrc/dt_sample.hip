@@ -1458,7 +1458,7 @@ dt_status dt_sample(const void *logits, int64_t row_stride, int rows, int V, int
   float *maxima = reinterpret_cast<float *>(at + w.maxima);
   // (thousands of tokens are kept by top-p or min-p, if by anything; top-k's passes, where its elements are too many, are
   // its row's workgroup's)
-  const bool can_be_large = l.segs > kFewSegs && (how->top_ks || how->top_k == 0) &&
+  const bool can_be_large = l.segs > kFewSegs && (how->top_ks || how->top_k == 0 || how->top_k >= V) &&
                             (how->top_ps || how->top_p < 1.0f || how->min_ps || how->min_p > 0.0f);
   const Work work{can_be_large ? reinterpret_cast<Large *>(at + w.large) : nullptr, reinterpret_cast<int *>(at + w.count),
                   reinterpret_cast<u64 *>(at + w.bins), reinterpret_cast<u64 *>(at + w.list),

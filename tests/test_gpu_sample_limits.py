@@ -1,9 +1,13 @@
 """Sampling at limits of its numbers: rows whose values lie within a hair of one another, or further apart than fp32
-reaches.  Tokens and log-probabilities against the definition in 64 bits, with the tolerances of test_gpu_sample.py."""
+reaches; a top-k of the whole vocabulary.  Tokens and log-probabilities against the definition in 64 bits, with the
+tolerances of test_gpu_sample.py."""
+import ctypes
+
 import pytest
 import torch
 
-from test_gpu_sample import check
+from paper_2607_08642_amd import binding
+from test_gpu_sample import check, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +51,28 @@ def test_values_that_lie_far_apart(dtype, V):
     for T in (1.0, 1e37, 2e38, float("inf")):
         for how in (dict(), dict(k=100), dict(k=V // 2, p=0.9), dict(p=0.9), dict(q=0.2), dict(p=0.99, q=0.1)):
             check(x, u, T=T, **how)
+
+
+def nodes(call):
+    """How many nodes a graph of the call has."""
+    graph, n = torch.cuda.CUDAGraph(keep_graph=True), ctypes.c_size_t()
+    call()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call()
+    assert binding.load().hipGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), None, ctypes.byref(n)) == 0
+    return n.value
+
+
+def test_top_k_of_the_whole_vocabulary_is_off():
+    """As a number, too: the launches and bits of top_k = 0."""
+    V = 40011
+    x, u = rows_of(3, V, "f32", seed=60, spread=0.7, high=2)
+    a, v = x.cuda(), u.cuda()
+    for how in (dict(top_p=0.9), dict(min_p=0.05), dict(top_p=0.97, min_p=0.01)):
+        want = binding.sample(a, v, logprobs=True, **how)
+        for k in (V, V + 1, 2 ** 31 - 1):
+            got = binding.sample(a, v, top_k=k, logprobs=True, **how)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+            assert nodes(lambda: binding.sample(a, v, top_k=k, **how)) == nodes(lambda: binding.sample(a, v, **how))
+    check(x, u, k=V, p=0.9)

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import operator
 import os
 import threading
 from typing import Optional
@@ -1028,7 +1029,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
             kept.append(x)
         else:
             setattr(how, names, None)
-            setattr(how, name, x)
+            # (top_k: a C int drops the bits above its 32; V is as good as more, and -1 is refused as less is)
+            setattr(how, name, max(-1, min(operator.index(x), V)) if name == "top_k" else x)
     if workspace is None:
         n = _sample_bytes.get((rows, V))
         if n is None:

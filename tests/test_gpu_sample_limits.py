@@ -1,5 +1,5 @@
 """Sampling at limits of its numbers: rows whose values lie within a hair of one another, or further apart than fp32
-reaches; a top-k of the whole vocabulary.  Tokens and log-probabilities against the definition in 64 bits, with the
+reaches; a top-k of the whole vocabulary and beyond.  Tokens and log-probabilities against the definition in 64 bits, with the
 tolerances of test_gpu_sample.py."""
 import ctypes
 
@@ -76,3 +76,19 @@ def test_top_k_of_the_whole_vocabulary_is_off():
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
             assert nodes(lambda: binding.sample(a, v, top_k=k, **how)) == nodes(lambda: binding.sample(a, v, **how))
     check(x, u, k=V, p=0.9)
+
+
+def test_top_k_beyond_32_bits():
+    """Off, as every top_k >= V; a negative one is refused, and one that is no whole number."""
+    x, u = rows_of(8, 3001, "f32", seed=61)
+    x, u = x.cuda(), u.cuda()
+    want = binding.sample(x, u)
+    assert not torch.equal(want, binding.sample(x, u, top_k=1))
+    for k in (2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 40 + 5, 10 ** 18 + 1, 2 ** 63 - 1, 2 ** 64 + 1):
+        assert torch.equal(binding.sample(x, u, top_k=k), want), k
+    for k in (-1, -2 ** 31, -2 ** 32 + 1, -2 ** 32, -2 ** 64 + 5):
+        with pytest.raises(binding.DTError):
+            binding.sample(x, u, top_k=k)
+    for k in (5.0, float("inf"), "5"):
+        with pytest.raises(TypeError):
+            binding.sample(x, u, top_k=k)

@@ -993,6 +993,7 @@ def rotate(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float =
 
 
 _sample_bytes = {}   # of a workspace for (rows, V)
+_SPACE_BYTES, _SPACES = 32 << 20, 8   # workspaces that a host thread keeps: their largest size, how many
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, logprobs=False, workspace=None,
@@ -1005,6 +1006,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
     within what is kept: (tokens, logprobs).  out takes given tensors: tokens, or with logprobs both.  The last
     dimension is contiguous, the others lie at one stride (padded rows do).  Runs on torch's current
     stream of the tensors' device (the current one) unless one is given.
+    A host thread keeps the workspaces of a few streams, up to 32 MiB each; larger ones (from about 1,100 rows of a large
+    vocabulary on) are allocated by each call, unless `workspace` gives one (of dt_sample_workspace_size's bytes).
     """
     import torch
     lib = load()
@@ -1039,12 +1042,15 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
             if len(_sample_bytes) >= 4096:   # (shapes of a long-running program)
                 _sample_bytes.clear()
             n = _sample_bytes[(rows, V)] = size.value
-        # (kept for the stream, where calls follow one another; a graph's calls come again after that, and have their own)
+        # (kept for the stream, where calls follow one another; a graph's calls come again after that, and have their own.
+        # Kept up to a bound: a call of more rows takes far longer than an allocation)
         spaces, at = _arguments.spaces, (device, s)
         workspace = None if _capturing(torch, stream) else spaces.get(at)
         if workspace is None or workspace.numel() < n:
             workspace = _empty(torch, (n,), torch.uint8, logits.device, stream)
-            if not _capturing(torch, stream):
+            if n <= _SPACE_BYTES and not _capturing(torch, stream):
+                if len(spaces) >= _SPACES:
+                    spaces.clear()
                 spaces[at] = workspace
     elif workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError(f"workspace: want a contiguous tensor on cuda:{device}, got one on {workspace.device}")

@@ -1,6 +1,6 @@
 """Sampling at limits of its numbers: rows whose values lie within a hair of one another, or further apart than fp32
-reaches; a top-k of the whole vocabulary and beyond.  Tokens and log-probabilities against the definition in 64 bits, with the
-tolerances of test_gpu_sample.py."""
+reaches; a top-k of the whole vocabulary and beyond; calls of very many rows.  Tokens and log-probabilities against the
+definition in 64 bits, with the tolerances of test_gpu_sample.py."""
 import ctypes
 
 import pytest
@@ -92,3 +92,26 @@ def test_top_k_beyond_32_bits():
     for k in (5.0, float("inf"), "5"):
         with pytest.raises(TypeError):
             binding.sample(x, u, top_k=k)
+
+
+def test_large_workspaces_are_not_kept():
+    """A call of many rows leaves no memory behind but its results; calls on many streams leave a bounded number."""
+    x, u = rows_of(1, 40000, "bf16", seed=62)
+    x, u = x.cuda().expand(1 << 14, -1), torch.rand(1 << 14, device="cuda")
+    binding.sample(x[:2], u[:2], top_k=20)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    tokens = binding.sample(x, u, top_k=20)
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() - before <= 64 << 20
+    want = binding.sample(x[:640], u[:640], top_k=20)
+    assert torch.equal(tokens[:640], want)
+    before = torch.cuda.memory_allocated()
+    for s in [torch.cuda.Stream() for _ in range(32)]:
+        s.wait_stream(torch.cuda.current_stream())
+        got = binding.sample(x[:640], u[:640], top_k=20, stream=s)
+        s.synchronize()
+        assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    del got
+    assert torch.cuda.memory_allocated() - before <= 256 << 20

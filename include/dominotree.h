@@ -570,14 +570,14 @@ typedef struct {
 
 /* Queries q [rows, heads, D] and keys k [rows, kv_heads, D] into q_out and k_out (k and k_out NULL and
  * kv_heads 0: queries alone).  dtype: DT_F32 or DT_BF16; D a multiple of 16, 16 .. 512; heads +
- * kv_heads < 2^20; rows < 2^26.  An output may be its input (the same address and strides), else tensors must not overlap. */
+ * kv_heads < 2^20; rows < 2^26 - 4.  An output may be its input (the same address and strides), else tensors must not overlap. */
 dt_status dt_rotate(const dt_rows *q, int heads, const dt_rows *k, int kv_heads, int rows, int D, int dtype,
                     const dt_rotary *rotary, const dt_rows *q_out, const dt_rows *k_out, void *stream);
 
 /* dt_rotate and dt_cache_append in one: the chunk's queries q [rows, heads, D] normed and rotated into q_out, its
  * keys normed, rotated and written into the layer (DT_F8: rounded to bf16 first, so the cache holds what the
  * two calls leave in it), its values written as they are.  Rows that belong to no chunk are not touched.
- * 1 <= heads < 2^20, and max_chunk * heads / 4 + (max_chunk / 32 + 3) * kv_heads < 2^24. */
+ * 1 <= heads < 2^20, and max_chunk * heads / 4 + (max_chunk / 32 + 3) * kv_heads < 2^24 - 1. */
 dt_status dt_cache_append_rotated(const dt_cache *cache, int layer, const dt_chunk *chunk, int heads, const dt_rows *q,
                                   const dt_rows *k, const dt_rows *v, const dt_rotary *rotary, const dt_rows *q_out,
                                   void *stream);

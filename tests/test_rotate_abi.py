@@ -67,3 +67,10 @@ def test_appends():
     assert b.load().dt_cache_append_rotated(ref(cache()), 0, ref(chunk()), 8, ref(ROWS), ref(ROWS), ref(ROWS), None,
                                             ref(ROWS), None) == NULL
     assert b.load().dt_rotate(ref(ROWS), 8, None, 0, 12, 64, b.DT_F32, None, ref(ROWS), None, None) == NULL
+
+
+def test_the_first_sizes_past_the_limits():
+    assert rotate(rows=(1 << 26) - 4) == UNSUPPORTED
+    n = 621378 * 32                               # n * 3 / 4 + (n / 32 + 3) * 3 = 2^24 - 1
+    wide = chunk(batch=1, rows=n, max_chunk=n, max_len=n, table_width=1 << 20)
+    assert append(cache(kv_heads=3), k=wide, heads=3) == UNSUPPORTED
